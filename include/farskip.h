@@ -93,7 +93,9 @@ typedef enum {
   FS_OP_BLOCK = 3,
   FS_OP_GROUPED_FFN_FP8 = 4,
   FS_OP_BLOCK_FP8 = 5,
-  FS_OP_DISPATCH_PACK_FP8 = 6
+  FS_OP_DISPATCH_PACK_FP8 = 6,
+  FS_OP_LINEAR = 7,          /* fs_linear_workspace */
+  FS_OP_LINEAR_BACKWARD = 8  /* fs_linear_workspace */
 } fs_op;
 
 /* One MoE block on one EP rank (Section 2.1).  A plain host struct, read
@@ -586,6 +588,133 @@ fs_status fs_moe_block_forward(const fs_moe_desc* desc, int32_t phase,
 fs_status fs_dense_linear(int32_t dtype, int32_t m, int32_t n, int32_t kdim, const void* a,
                           const void* w, void* out, fs_stream stream);
 
+/* ---- The dense sublayer that runs in the far-skip window (Section 4.1: the
+ * next layer's computation, between FS_PHASE_BEGIN and FS_PHASE_FINISH): the
+ * linear with its epilogue, layer norm, their backward passes, and 8-bit
+ * checkpoints of the activations that the backward passes read.
+ *
+ * Conventions of these entry points, where they differ from the others'
+ *   Matrices    Every matrix has a row stride in elements, at least its
+ *               columns.  Pointers are aligned to their elements; 16-byte
+ *               aligned bases and strides are faster.  Any sizes.
+ *   Vectors     bias, gamma, beta, mean, rstd and the gradients of the first
+ *               three are fp32.
+ *   Rounding    Sums and everything between input and output are fp32; each
+ *               output is rounded once.
+ *   Overlap     Outputs do not overlap inputs except where stated.
+ *   Devices     A non-NULL stream must belong to the current device
+ *               (FS_ERR_INVALID otherwise).
+ *   Order       No result depends on the order of atomics: the same call gives
+ *               the same bits.
+ *   Graphs      Calls can be captured.  A workspace holds nothing from one
+ *               call to the next; calls whose work may run at the same time
+ *               (two streams, two graphs) need one each. */
+
+/* A saved activation [rows, cols]: its rows, or an 8-bit checkpoint of them.
+ * The checkpoint cuts a row into blocks of 32 columns (the last may be
+ * short).  A block is E4M3 codes and a scale byte e + 127, e the least integer
+ * in [-117, 119] with max |x| <= 448 * 2^e: code = E4M3(x * 2^-e) to nearest,
+ * ties to even (values above 448 * 2^119 become that).  It stands for
+ * dec(code) * 2^e, which fp32 and bf16 hold exactly.  A block with an infinity
+ * or a NaN (byte 255) stands for NaNs. */
+typedef struct {
+  void* rows;       /* [rows, cols] dtype with row stride ld, or NULL */
+  int64_t ld;
+  uint8_t* codes;   /* [rows, cols], or NULL */
+  uint8_t* scales;  /* [rows, ceil(cols / 32)] */
+} fs_saved;
+
+/* Rows to a checkpoint, and back (dst gets the values it stands for).
+ *   src, dst  [rows, cols] dtype with row stride lds, ldd */
+fs_status fs_checkpoint_fp8(int32_t dtype, int64_t rows, int32_t cols, const void* src, int64_t lds,
+                            uint8_t* codes, uint8_t* scales, fs_stream stream);
+fs_status fs_checkpoint_restore(int32_t dtype, int64_t rows, int32_t cols, const uint8_t* codes,
+                                const uint8_t* scales, void* dst, int64_t ldd, fs_stream stream);
+
+typedef enum {
+  FS_ACT_NONE = 0,
+  FS_ACT_RELU = 1,  /* max(z, 0); slope 0 at 0 */
+  FS_ACT_GELU = 2,  /* z Phi(z), Phi the normal distribution function */
+  FS_ACT_SILU = 3   /* z / (1 + exp(-z)) */
+} fs_act;
+
+typedef struct {
+  int32_t abi_version; /* FS_ABI_VERSION */
+  int32_t dtype;       /* fs_dtype of a, w, residual, out, z and their gradients */
+  int32_t act;         /* fs_act */
+  int32_t m, n, k;     /* m tokens, n outputs, k inputs */
+} fs_linear_desc;
+
+/* Bytes of workspace: op FS_OP_LINEAR for fs_linear, FS_OP_LINEAR_BACKWARD for
+ * fs_linear_backward.  The workspace is 16-byte aligned. */
+fs_status fs_linear_workspace(const fs_linear_desc* desc, int32_t op, size_t* bytes);
+
+/* The linear with its epilogue (fs_dense_linear and fs_farskip_residual in one
+ * pass, any widths):
+ *   z = a w^T + bias;  out = act(z) + residual
+ *   a [m, k], w [n, k], residual [m, n] or NULL, out [m, n]; bias [n] or NULL
+ *   out       may be residual itself (same pointer and stride)
+ *   save_z    NULL, or receives z (its rows, a checkpoint of them, or both)
+ *   save_out  NULL, or receives a checkpoint of out (codes only)
+ * m == 0 is a valid no-op. */
+fs_status fs_linear(const fs_linear_desc* desc, const void* a, int64_t lda, const void* w, int64_t ldw,
+                    const float* bias, const void* residual, int64_t ldr, void* out, int64_t ldo,
+                    const fs_saved* save_z, const fs_saved* save_out, void* ws, size_t ws_bytes,
+                    fs_stream stream);
+
+/* Its backward pass, from dout [m, n] (row stride ldo), the input a and the
+ * pre-activation z as saved (rows or codes, not both):
+ *   dz = dout * act'(z) rounded to dtype (dout itself without an activation)
+ *   da [m, k] = dz w;  dw [n, k] = dz^T a
+ *   dbias [n] = sums over the rows of dout * act'(z), before the rounding
+ * Each of da, dw, dbias may be NULL, not all.  a is read for dw, w for da, z
+ * only with an activation.  The residual's gradient is dout itself.  With m ==
+ * 0 dw and dbias are set to 0. */
+fs_status fs_linear_backward(const fs_linear_desc* desc, const void* dout, int64_t ldo,
+                             const fs_saved* a, const void* w, int64_t ldw, const fs_saved* z, void* da,
+                             int64_t ldda, void* dw, int64_t lddw, float* dbias, void* ws,
+                             size_t ws_bytes, fs_stream stream);
+
+typedef struct {
+  int32_t abi_version; /* FS_ABI_VERSION */
+  int32_t dtype;       /* fs_dtype of the rows */
+  int32_t rows, cols;  /* rows <= 2^21, cols <= 32768 */
+  int32_t center;      /* 1: layer norm; 0: root-mean-square norm (mean 0) */
+  float eps;           /* > 0 */
+} fs_norm_desc;
+
+/* Bytes of workspace of fs_layer_norm_backward. */
+fs_status fs_layer_norm_workspace(const fs_norm_desc* desc, size_t* bytes);
+
+/* Layer norm of the residual stream after its deferred add (Eq. 7):
+ *   s = x + add, rounded to dtype;  mean and var = mean((s - mean)^2) of a row
+ *   rstd = 1 / sqrt(var + eps);  y = (s - mean) rstd gamma + beta
+ *   add, gamma (1), beta (0): NULL to leave out
+ *   sum_out  [rows, cols] or NULL: receives s; may be x or add itself
+ *   y        [rows, cols]; may be x or add itself
+ *   mean, rstd  [rows] or NULL (center == 0: mean is 0)
+ *   save_in, save_y  NULL, or receive a checkpoint of s, of y (codes only) */
+fs_status fs_layer_norm(const fs_norm_desc* desc, const void* x, int64_t ldx, const void* add,
+                        int64_t ldadd, const float* gamma, const float* beta, void* sum_out,
+                        int64_t ldsum, void* y, int64_t ldy, float* mean, float* rstd,
+                        const fs_saved* save_in, const fs_saved* save_y, fs_stream stream);
+
+/* Its backward pass, from dy, the normalised rows' input s as saved (rows or
+ * codes, not both) and the forward's statistics:
+ *   h = (s - mean) rstd;  u = gamma dy
+ *   dx = dres + rstd (u - mean(u) - h mean(u h))   (center == 0: no mean(u))
+ *   dgamma [cols] = sums over the rows of dy h;  dbeta [cols] of dy
+ *   mean     read only with center == 1
+ *   dres     [rows, cols] or NULL: the gradient that reaches s on other ways
+ *   dx       may be dy or dres itself
+ *   dgamma, dbeta  NULL to leave out (without both no workspace is needed)
+ * With rows == 0 dgamma and dbeta are set to 0. */
+fs_status fs_layer_norm_backward(const fs_norm_desc* desc, const void* dy, int64_t lddy,
+                                 const fs_saved* x, const float* mean, const float* rstd,
+                                 const float* gamma, const void* dres, int64_t lddres, void* dx,
+                                 int64_t lddx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                                 fs_stream stream);
+
 /* Per-kernel timing with HIP events recorded on the launch stream around
  * selected kernels.  fs_profile_read synchronises those events.
  * FS_K_GATE_UP / FS_K_DOWN time the routed experts' passes (and
@@ -596,7 +725,7 @@ fs_status fs_dense_linear(int32_t dtype, int32_t m, int32_t n, int32_t kdim, con
  * experts' passes inside fs_moe_block_forward and fs_grouped_expert_ffn
  * without group_offsets (one group of max_rows rows);
  * FS_K_DISPATCH_COPY / FS_K_COMBINE_COPY the Dispatch and Combine stand-in
- * copies on the stream they run on; FS_K_DENSE fs_dense_linear;
+ * copies on the stream they run on; FS_K_DENSE fs_dense_linear and fs_linear;
  * FS_K_ALLREDUCE_COPY fs_allreduce_standin; FS_K_QUANTIZE the activation
  * quantisation of the block's FP8 experts. */
 typedef enum {

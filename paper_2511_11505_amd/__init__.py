@@ -23,3 +23,9 @@ from ._lib import (  # noqa: F401
 )
 from .block import (MoEBlock, fp8_row_views, fragment_ordered, fragment_ordered_fp8,  # noqa: F401
                     prepare_remote_sources)
+from ._lib import (  # noqa: F401
+    FS_F32, FS_BF16, FS_OP_LINEAR, FS_OP_LINEAR_BACKWARD, fs_saved, fs_checkpoint_fp8,
+    fs_checkpoint_restore, fs_linear_workspace, fs_linear, fs_linear_backward,
+    fs_layer_norm_workspace, fs_layer_norm, fs_layer_norm_backward,
+)
+from .sublayer import DenseSublayer, checkpoint_buffers, linear_desc, norm_desc  # noqa: F401

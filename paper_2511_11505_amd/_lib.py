@@ -18,7 +18,8 @@ FS_SOFTMAX, FS_SIGMOID = 0, 1
 (FS_PHASE_ALL, FS_PHASE_BEGIN, FS_PHASE_FINISH, FS_PHASE_GATE, FS_PHASE_SHARED, FS_PHASE_EXPERTS,
  FS_PHASE_COMBINE) = range(7)
 (FS_OP_ROUTER_TOPK, FS_OP_DISPATCH_PACK, FS_OP_GROUPED_FFN, FS_OP_BLOCK, FS_OP_GROUPED_FFN_FP8,
- FS_OP_BLOCK_FP8, FS_OP_DISPATCH_PACK_FP8) = range(7)
+ FS_OP_BLOCK_FP8, FS_OP_DISPATCH_PACK_FP8, FS_OP_LINEAR, FS_OP_LINEAR_BACKWARD) = range(9)
+FS_ACT_NONE, FS_ACT_RELU, FS_ACT_GELU, FS_ACT_SILU = range(4)
 (FS_K_ROUTER, FS_K_TOPK, FS_K_PLAN, FS_K_PACK, FS_K_GATE_UP, FS_K_DOWN,
  FS_K_COMBINE, FS_K_SHARED_GATE_UP, FS_K_SHARED_DOWN, FS_K_DISPATCH_COPY, FS_K_DENSE,
  FS_K_COMBINE_COPY, FS_K_ALLREDUCE_COPY, FS_K_QUANTIZE, FS_K_COUNT) = range(15)
@@ -56,6 +57,20 @@ class fs_block_buffers(ctypes.Structure):
                                    "group_rows", "group_offsets", "y", "shared_out", "ret")]
 
 
+class fs_linear_desc(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("abi_version", "dtype", "act", "m", "n", "k")]
+
+
+class fs_norm_desc(ctypes.Structure):
+    _fields_ = [("abi_version", _i32), ("dtype", _i32), ("rows", _i32), ("cols", _i32),
+                ("center", _i32), ("eps", _f32)]
+
+
+class fs_saved(ctypes.Structure):
+    _fields_ = [("rows", _vp), ("ld", _i64), ("codes", _vp), ("scales", _vp)]
+
+
+_pld, _pnd, _psv = (ctypes.POINTER(t) for t in (fs_linear_desc, fs_norm_desc, fs_saved))
 _SIGS = {
     "fs_status_string": (ctypes.c_char_p, [_i32]),
     "fs_last_error_message": (ctypes.c_char_p, []),
@@ -95,6 +110,17 @@ _SIGS = {
                                     _vp, _vp, _vp, ctypes.POINTER(fs_block_buffers), _i64, _vp, _sz,
                                     _vp, _vp, _vp]),
     "fs_dense_linear": (_i32, [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "fs_checkpoint_fp8": (_i32, [_i32, _i64, _i32, _vp, _i64, _vp, _vp, _vp]),
+    "fs_checkpoint_restore": (_i32, [_i32, _i64, _i32, _vp, _vp, _vp, _i64, _vp]),
+    "fs_linear_workspace": (_i32, [_pld, _i32, ctypes.POINTER(_sz)]),
+    "fs_linear": (_i32, [_pld, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _psv, _psv, _vp, _sz, _vp]),
+    "fs_linear_backward": (_i32, [_pld, _vp, _i64, _psv, _vp, _i64, _psv, _vp, _i64, _vp, _i64, _vp,
+                                  _vp, _sz, _vp]),
+    "fs_layer_norm_workspace": (_i32, [_pnd, ctypes.POINTER(_sz)]),
+    "fs_layer_norm": (_i32, [_pnd, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _psv,
+                             _psv, _vp]),
+    "fs_layer_norm_backward": (_i32, [_pnd, _vp, _i64, _psv, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp,
+                                      _vp, _vp, _sz, _vp]),
     "fs_profile_enable": (_i32, [_i32]),
     "fs_profile_select": (_i32, [ctypes.c_uint32]),
     "fs_profile_read": (_i32, [_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i64)]),
@@ -361,6 +387,140 @@ def fs_moe_block_forward(desc, phase, weights, residual_in, partial_out, residua
                                        ctypes.byref(buffers), max_recv_rows, wp, wb, sync,
                                        stream_handle(compute),
                                        None if comm is None else stream_handle(comm)))
+
+
+# ------------------------------------------------- the dense sublayer's entries
+# Matrices are 2-D tensors with unit column stride (row strides are passed on)
+# or int addresses of gapless rows; a checkpoint is its (codes, scales) pair.
+# Types, shapes and devices are checked here, since the C side sees addresses.
+_ELEM = {}
+
+
+def _bad(name, what):
+    raise FsError(FS_ERR_INVALID, f"{name} must be {what}")
+
+
+def _elem_types():
+    if not _ELEM:
+        import torch
+        _ELEM.update({FS_F32: torch.float32, FS_BF16: torch.bfloat16, "f32": torch.float32,
+                      "u8": torch.uint8})
+    return _ELEM
+
+
+def _here(t, name):
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        _bad(name, "on the current GPU")
+
+
+def _mat(t, name, dtype, rows, cols):
+    """(address, row stride) of a matrix argument."""
+    if t is None or isinstance(t, int):
+        return t, cols
+    if t.dtype != _elem_types().get(dtype) or tuple(t.shape) != (rows, cols):
+        _bad(name, f"[{rows}, {cols}] of the descriptor's type, not {list(t.shape)} of {t.dtype}")
+    if cols > 1 and t.stride(1) != 1:
+        _bad(name, "of unit column stride")
+    _here(t, name)
+    return t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+
+
+def _vec(t, name, size):
+    """Address of an fp32 vector argument."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype != _elem_types()["f32"] or tuple(t.shape) != (size,) or not t.is_contiguous():
+        _bad(name, f"[{size}] contiguous fp32, not {list(t.shape)} of {t.dtype}")
+    _here(t, name)
+    return t.data_ptr()
+
+
+def _codes(pair, name, rows, cols):
+    """Addresses of a checkpoint's codes and scales."""
+    out = []
+    for t, what, shape in zip(pair, ("codes", "scales"), ((rows, cols), (rows, (cols + 31) // 32))):
+        if t is not None and not isinstance(t, int):
+            if t.dtype != _elem_types()["u8"] or tuple(t.shape) != shape or not t.is_contiguous():
+                _bad(f"{name} {what}", f"{list(shape)} contiguous uint8, not {list(t.shape)} of {t.dtype}")
+            _here(t, name)
+            t = t.data_ptr()
+        out.append(t)
+    return out
+
+
+def _saved(s, name, dtype, rows, cols):
+    """fs_saved of a tensor, a (codes, scales) pair, an fs_saved, or None."""
+    if s is None or isinstance(s, fs_saved):
+        return s
+    if isinstance(s, (tuple, list)):
+        return fs_saved(None, 0, *_codes(s, name, rows, cols))
+    return fs_saved(*_mat(s, name, dtype, rows, cols), None, None)
+
+
+def fs_checkpoint_fp8(dtype, rows, cols, src, codes, scales, stream=None):
+    _check(load().fs_checkpoint_fp8(dtype, rows, cols, *_mat(src, "src", dtype, rows, cols),
+                                    *_codes((codes, scales), "checkpoint", rows, cols),
+                                    stream_handle(stream)))
+
+
+def fs_checkpoint_restore(dtype, rows, cols, codes, scales, dst, stream=None):
+    _check(load().fs_checkpoint_restore(dtype, rows, cols,
+                                        *_codes((codes, scales), "checkpoint", rows, cols),
+                                        *_mat(dst, "dst", dtype, rows, cols), stream_handle(stream)))
+
+
+def fs_linear_workspace(desc, op):
+    out = _sz(0)
+    _check(load().fs_linear_workspace(ctypes.byref(desc), op, ctypes.byref(out)))
+    return out.value
+
+
+def fs_linear(desc, a, w, bias, residual, out, ws, save_z=None, save_out=None, stream=None):
+    wp, wb = _ws(ws)
+    dt, m, n, k = desc.dtype, desc.m, desc.n, desc.k
+    _check(load().fs_linear(ctypes.byref(desc), *_mat(a, "a", dt, m, k), *_mat(w, "w", dt, n, k),
+                            _vec(bias, "bias", n), *_mat(residual, "residual", dt, m, n),
+                            *_mat(out, "out", dt, m, n), _saved(save_z, "save_z", dt, m, n),
+                            _saved(save_out, "save_out", dt, m, n), wp, wb, stream_handle(stream)))
+
+
+def fs_linear_backward(desc, dout, a, w, z, da, dw, dbias, ws, stream=None):
+    wp, wb = _ws(ws)
+    dt, m, n, k = desc.dtype, desc.m, desc.n, desc.k
+    _check(load().fs_linear_backward(ctypes.byref(desc), *_mat(dout, "dout", dt, m, n),
+                                     _saved(a, "a", dt, m, k), *_mat(w, "w", dt, n, k),
+                                     _saved(z, "z", dt, m, n), *_mat(da, "da", dt, m, k),
+                                     *_mat(dw, "dw", dt, n, k), _vec(dbias, "dbias", n), wp, wb,
+                                     stream_handle(stream)))
+
+
+def fs_layer_norm_workspace(desc):
+    out = _sz(0)
+    _check(load().fs_layer_norm_workspace(ctypes.byref(desc), ctypes.byref(out)))
+    return out.value
+
+
+def fs_layer_norm(desc, x, add, gamma, beta, sum_out, y, mean, rstd, save_in=None, save_y=None,
+                  stream=None):
+    dt, r, c = desc.dtype, desc.rows, desc.cols
+    _check(load().fs_layer_norm(ctypes.byref(desc), *_mat(x, "x", dt, r, c), *_mat(add, "add", dt, r, c),
+                                _vec(gamma, "gamma", c), _vec(beta, "beta", c),
+                                *_mat(sum_out, "sum_out", dt, r, c), *_mat(y, "y", dt, r, c),
+                                _vec(mean, "mean", r), _vec(rstd, "rstd", r),
+                                _saved(save_in, "save_in", dt, r, c),
+                                _saved(save_y, "save_y", dt, r, c), stream_handle(stream)))
+
+
+def fs_layer_norm_backward(desc, dy, x, mean, rstd, gamma, dres, dx, dgamma, dbeta, ws, stream=None):
+    wp, wb = _ws(ws)
+    dt, r, c = desc.dtype, desc.rows, desc.cols
+    _check(load().fs_layer_norm_backward(ctypes.byref(desc), *_mat(dy, "dy", dt, r, c),
+                                         _saved(x, "x", dt, r, c), _vec(mean, "mean", r),
+                                         _vec(rstd, "rstd", r), _vec(gamma, "gamma", c),
+                                         *_mat(dres, "dres", dt, r, c), *_mat(dx, "dx", dt, r, c),
+                                         _vec(dgamma, "dgamma", c), _vec(dbeta, "dbeta", c), wp, wb,
+                                         stream_handle(stream)))
 
 
 def fs_profile_enable(on=True):

@@ -10,53 +10,10 @@
 #include <vector>
 
 #include "../../include/farskip.h"
+#include "api_common.hpp"
 #include "internal.hpp"
 
 namespace {
-
-thread_local std::string g_msg;
-
-fs_status fail(fs_status st, const std::string& m) {
-  g_msg = m;
-  return st;
-}
-fs_status hip_fail(hipError_t e, const char* where) {
-  g_msg = std::string(where) + ": " + hipGetErrorString(e);
-  return FS_ERR_HIP;
-}
-#define FS_HIP(expr, where)                     \
-  do {                                          \
-    hipError_t e_ = (expr);                     \
-    if (e_ != hipSuccess) return hip_fail(e_, where); \
-  } while (0)
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
-
-#define NEED(ptr, name)                                                                      \
-  do {                                                                                       \
-    if (!(ptr)) return fail(FS_ERR_INVALID, std::string(name) + " must not be NULL");        \
-    if (!aligned16(ptr)) return fail(FS_ERR_INVALID, std::string(name) + " must be 16-byte aligned"); \
-  } while (0)
-// int32 index arrays and fp32 gate arrays are read element by element
-#define NEED4(ptr, name)                                                                     \
-  do {                                                                                       \
-    if (!(ptr)) return fail(FS_ERR_INVALID, std::string(name) + " must not be NULL");        \
-    if (!aligned4(ptr)) return fail(FS_ERR_INVALID, std::string(name) + " must be 4-byte aligned"); \
-  } while (0)
-#define OPT4(ptr, name)                                                                      \
-  do {                                                                                       \
-    if ((ptr) && !aligned4(ptr))                                                             \
-      return fail(FS_ERR_INVALID, std::string(name) + " must be 4-byte aligned");            \
-  } while (0)
-#define OPT(ptr, name)                                                                       \
-  do {                                                                                       \
-    if ((ptr) && !aligned16(ptr))                                                            \
-      return fail(FS_ERR_INVALID, std::string(name) + " must be 16-byte aligned");           \
-  } while (0)
-
-size_t elem(int dtype) { return dtype == FS_F32 ? 4 : 2; }
-size_t align256(size_t b) { return (b + 255) / 256 * 256; }
 
 fs_status check_desc(const fs_moe_desc* d) {
   if (!d) return fail(FS_ERR_INVALID, "desc must not be NULL");
@@ -98,8 +55,6 @@ fs_status check_desc(const fs_moe_desc* d) {
     return fail(FS_ERR_UNSUPPORTED, "ep_size * n_tokens * top_k must be < 2^31");
   return FS_OK;
 }
-
-hipStream_t S(fs_stream s) { return reinterpret_cast<hipStream_t>(s); }
 
 // ---------------------------------------------------------------- profiling
 // A timing window per (kernel id, stream).  Kernels launched on the stream
@@ -215,6 +170,10 @@ hipError_t standin_copy(void* dst, const void* src, size_t bytes, double factor,
 }  // namespace
 
 namespace fs {
+std::string& last_message() {
+  static thread_local std::string msg;
+  return msg;
+}
 void prof_begin(int kernel, hipStream_t s) {
   ProfState& p = prof();
   std::lock_guard<std::mutex> g(p.mu);
@@ -272,7 +231,7 @@ const char* fs_status_string(int32_t status) {
   }
 }
 
-const char* fs_last_error_message(void) { return g_msg.c_str(); }
+const char* fs_last_error_message(void) { return fs::last_message().c_str(); }
 
 int32_t fs_abi_version(void) { return FS_ABI_VERSION; }
 

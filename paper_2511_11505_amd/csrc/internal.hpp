@@ -144,6 +144,92 @@ hipError_t launch_combine(int dtype, const void* y_ret, const int32_t* slot_to_r
 hipError_t launch_residual(int dtype, void* out, const void* a, const void* b, const void* c,
                            int64_t n_elems, hipStream_t s);
 
+// ---- 8-bit checkpoints (checkpoint.hip; the format is in saved.hpp)
+hipError_t launch_checkpoint(int dtype, const void* x, int64_t ld, int64_t rows, int cols,
+                             uint8_t* codes, uint8_t* scales, hipStream_t s);
+hipError_t launch_restore(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t rows,
+                          int cols, void* x, int64_t ld, hipStream_t s);
+
+// ---- layer norm (norm.hip)
+constexpr int kNormMaxCols = 32768;
+struct NormArgs {
+  int64_t rows;
+  int cols;
+  int center;
+  float eps;
+  const void* x;
+  int64_t ldx;
+  const void* add;   // or null
+  int64_t ldadd;
+  const float *gamma, *beta;   // or null: 1, 0
+  void* sum;         // or null
+  int64_t ldsum;
+  void* y;
+  int64_t ldy;
+  float *mean, *rstd;          // or null
+  uint8_t *in_codes, *in_scales, *y_codes, *y_scales;   // or null
+};
+hipError_t launch_norm(int dtype, const NormArgs& a, hipStream_t s);
+struct NormBackArgs {
+  int64_t rows;
+  int cols;
+  int center;
+  const void* dy;
+  int64_t lddy;
+  const void* x;     // the normalised rows, or their checkpoint
+  int64_t ldx;
+  const uint8_t *x_codes, *x_scales;
+  const float *mean, *rstd;    // mean null: 0
+  const float* gamma;          // or null
+  const void* dres;            // or null
+  int64_t lddres;
+  void* dx;
+  int64_t lddx;
+  float* part;       // norm_ws_bytes, or null: no dgamma, dbeta
+};
+size_t norm_ws_bytes(int64_t rows, int cols);
+hipError_t launch_norm_backward(int dtype, const NormBackArgs& a, float* dgamma, float* dbeta,
+                                hipStream_t s);
+// out0[c] = sum of part[p][c] over p < P, out1 of the P rows after them (either
+// may be null), in a fixed order.
+hipError_t launch_colsum(const float* part, int P, int cols, float* out0, float* out1, hipStream_t s);
+
+// ---- the linear with its epilogue (linear.hip)
+struct LinearOut {
+  const float* bias;
+  int act;
+  const void* res;
+  int64_t ldr;
+  void* out;
+  int64_t ldo;
+  void* z;
+  int64_t ldz;
+  uint8_t *z_codes, *z_scales, *out_codes, *out_scales;
+};
+struct LinearBack {
+  int act, m, n, k;
+  const void* dout;
+  int64_t ldo;
+  const void* a;
+  int64_t lda;
+  const uint8_t *a_codes, *a_scales;
+  const void* w;
+  int64_t ldw;
+  const void* z;
+  int64_t ldz;
+  const uint8_t *z_codes, *z_scales;
+  void* da;
+  int64_t ldda;
+  void* dw;
+  int64_t lddw;
+  float* dbias;
+};
+size_t linear_ws_bytes(int dtype, int m, int n, int k);
+size_t linear_backward_ws_bytes(int dtype, int act, int m, int n, int k);
+hipError_t launch_linear(int dtype, int m, int n, int k, const void* a, int64_t lda, const void* w,
+                         int64_t ldw, const LinearOut& o, void* ws, hipStream_t s);
+hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipStream_t s);
+
 // ---- stand-in collectives (standin.hip)
 // Copy `bytes` from src to dst with `workgroups` workgroups, taking at least
 // `seconds` (0: unpaced); see the kernel's comment for the schedule.

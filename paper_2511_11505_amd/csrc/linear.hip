@@ -1,0 +1,365 @@
+// The linear with its epilogue and its backward pass.
+//
+//   z = a w^T + bias;  out = act(z) + residual
+//   dz = round(dout * act'(z));  da = dz w;  dw = dz^T a
+//   dbias = column sums of dout * act'(z), before the rounding
+//
+// The three products differ in which way their operands lie (linear.hpp):
+// forward along/along, da along/across, dw across/across.
+
+#include <algorithm>
+
+#include "linear.hpp"
+
+namespace fs {
+namespace {
+
+typedef __attribute__((address_space(3))) short lds_i16;
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+
+// 16 bytes of a row at element p, the first n (of 16 / sizeof(T)) elements;
+// the rest 0.
+template <typename T>
+__device__ __forceinline__ uint4 load16(const T* p, int n) {
+  constexpr int V = 16 / sizeof(T);
+  if (n >= V) {
+    const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p);
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  }
+  uint32_t w[4] = {0, 0, 0, 0};
+  int z = 0;   // as in load8
+  asm volatile("" : "+v"(z));
+  p += z;
+#pragma unroll
+  for (int i = 0; i < V - 1; ++i)
+    if (i < n) {
+      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
+      else w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// One operand's 64 rows x 128 bytes of K in LDS, as it lies in memory: along,
+// 64 rows of 128 bytes; across, BK rows (of k) of 64 elements.  Padding
+// spreads the rows over the banks.
+template <typename T, bool ALONG>
+struct Panel {
+  static constexpr int V = 16 / sizeof(T), BK = 128 / sizeof(T);
+  static constexpr int ROWS = ALONG ? 64 : BK, PIECES = ALONG ? 8 : 64 / V;
+  static constexpr int STRIDE = (ALONG ? 128 : 64 * (int)sizeof(T)) + 16;   // bytes
+  static constexpr int BYTES = ROWS * STRIDE;
+  // the two 16-byte pieces of this thread for the K block at kb
+  static __device__ __forceinline__ void fetch(const T* p, int64_t ld, int row0, int rows, int kb,
+                                               int kend, uint4 (&st)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int q = (int)threadIdx.x + 256 * i, r = q / PIECES, e = (q % PIECES) * V;
+      const int row = ALONG ? row0 + r : kb + r;      // memory row
+      const int col = ALONG ? kb + e : row0 + e;
+      const int n = row < (ALONG ? rows : kend) ? (ALONG ? kend : rows) - col : 0;
+      st[i] = n > 0 ? load16<T>(p + (int64_t)row * ld + col, n) : make_uint4(0, 0, 0, 0);
+    }
+  }
+  static __device__ __forceinline__ void put(unsigned char* lds, const uint4 (&st)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int q = (int)threadIdx.x + 256 * i;
+      st16(lds + (q / PIECES) * STRIDE + (q % PIECES) * 16, st[i]);
+    }
+  }
+  // 16 rows from r0 of the step's K (32 for bf16, 16 for fp32): lane l row
+  // l % 16; bf16: k 8 (l / 16) .. + 7; fp32: k 4 (l / 16) .. + 3
+  static __device__ __forceinline__ uint4 frag(const unsigned char* lds, int r0, int step) {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    if constexpr (ALONG) {
+      return *reinterpret_cast<const uint4*>(lds + (r0 + r) * STRIDE + step * 64 + g * 16);
+    } else if constexpr (sizeof(T) == 4) {
+      uint4 f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        (&f.x)[i] = *reinterpret_cast<const uint32_t*>(lds + (step * 16 + 4 * g + i) * STRIDE + (r0 + r) * 4);
+      return f;
+    } else {
+      // a transposing read: in each 16-lane group lane p gives the address
+      // of 4 elements of row p / 4, columns 4 (p % 4) .., and gets the 4 rows
+      // of column p
+      const unsigned char* p = lds + (step * 32 + 8 * g + (r >> 2)) * STRIDE + (r0 + 4 * (r & 3)) * 2;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
+      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 4 * STRIDE));
+      const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+      return make_uint4(a.x, a.y, b.x, b.y);
+    }
+  }
+};
+
+// 64 x 64 tiles, four waves of 32 x 32, staged through registers: any type,
+// alignment, stride and size.  Grid (tiles, K slices); with more than one
+// slice the fp32 sums go to part[slice][M][np].
+template <typename T, bool LA, bool LB>
+__global__ __launch_bounds__(256) void linear_any_kernel(Product p, Epilogue e, int kper,
+                                                         float* __restrict__ part, int np) {
+  using PA = Panel<T, LA>;
+  using PB = Panel<T, LB>;
+  constexpr int BK = 128 / sizeof(T);
+  __shared__ __align__(16) unsigned char sa[2][PA::BYTES], sb[2][PB::BYTES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
+  const int tiles_n = (p.N + 63) / 64;
+  const int n0 = (int)(blockIdx.x % tiles_n) * 64, m0 = (int)(blockIdx.x / tiles_n) * 64;
+  const int k0 = blockIdx.y * kper, kend = min(p.K, k0 + kper);
+  const T *A = (const T*)p.A, *B = (const T*)p.B;
+  floatx4 acc[2][2] = {};
+  uint4 ra[2], rb[2];
+  PA::fetch(A, p.lda, m0, p.M, k0, kend, ra);
+  PB::fetch(B, p.ldb, n0, p.N, k0, kend, rb);
+  int buf = 0;
+  for (int kb = k0; kb < kend; kb += BK, buf ^= 1) {
+    PA::put(sa[buf], ra);
+    PB::put(sb[buf], rb);
+    __syncthreads();
+    if (kb + BK < kend) {
+      PA::fetch(A, p.lda, m0, p.M, kb + BK, kend, ra);
+      PB::fetch(B, p.ldb, n0, p.N, kb + BK, kend, rb);
+    }
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+      uint4 fa[2], fb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fa[i] = PA::frag(sa[buf], wm + 16 * i, step);
+        fb[i] = PB::frag(sb[buf], wn + 16 * i, step);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if constexpr (sizeof(T) == 2) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, fb[j]), __builtin_bit_cast(bf16x8, fa[i]), acc[i][j], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                  __uint_as_float((&fb[j].x)[k]), __uint_as_float((&fa[i].x)[k]), acc[i][j], 0, 0, 0);
+          }
+        }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float v[8];
+    join8(acc[i][0], acc[i][1], v);
+    const int64_t r = m0 + wm + 16 * i + (lane & 15);
+    const int c = n0 + wn + col8(lane);
+    if (part) {
+      if (r < p.M && c < p.N) store8<float>(part + ((int64_t)blockIdx.y * p.M + r) * np + c, v, 8);
+    } else {
+      epilogue8<T, 16, 32>(e, p.M, p.N, r, c, v);
+    }
+  }
+}
+
+// Sum of the K slices, in slice order, and the epilogue.  A thread holds 8
+// columns, four neighbours a checkpoint's block.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_reduce_kernel(const float* __restrict__ part, int slices,
+                                                            int M, int N, int np, Epilogue e) {
+  const int cpr = (N + 31) / 32 * 4;   // chunks of 8 columns per row
+  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t r = q / cpr;
+  const int c = (int)(q - r * cpr) * 8;
+  float v[8] = {};
+  if (r < M && c < N)
+    for (int s = 0; s < slices; ++s) {
+      const Raw8<float> x = load8<float>(part + ((int64_t)s * M + r) * np + c, 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += x.get(i);
+    }
+  epilogue8<T, 1, 2>(e, M, N, r, c, v);
+}
+
+// dz = round(dout * act'(z)) (when dz is given: [m, ldz8], columns past n are
+// 0) and the column sums of 64 rows of it before the rounding (when part is
+// given: [m / 64 rounded up][n]).  32 threads of 8 columns by 8 rows.
+template <typename T>
+__global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dout, int64_t ldo, int m,
+                                                       int n, int act, const T* __restrict__ z,
+                                                       int64_t ldz, const uint8_t* __restrict__ codes,
+                                                       const uint8_t* __restrict__ scales,
+                                                       T* __restrict__ dz, int64_t ld8,
+                                                       float* __restrict__ part) {
+  __shared__ float sm[8][256 + 4];
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const int panels = (n + 255) / 256, panel = (int)(blockIdx.x % panels);
+  const int64_t rb = blockIdx.x / panels;
+  const int c = panel * 256 + tx * 8, nv = min(8, n - c);
+  float sum[8] = {};
+  if (nv > 0) {
+#pragma unroll 4
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = rb * 64 + 8 * i + ty;
+      if (r >= m) break;
+      const Raw8<T> d = load8<T>(dout + r * ldo + c, nv);
+      float g[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) g[j] = d.get(j);
+      if (act != ACT_NONE) {
+        float x[8];
+        saved_load8<T>(z, ldz, codes, scales, r, c, n, nv, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = j < nv ? g[j] * act_slope<T>(act, x[j]) : 0.f;
+      }
+      if (dz) store8<T>(dz + r * ld8 + c, g, 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += g[j];
+    }
+  }
+  if (!part) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sm[ty][tx * 8 + j] = sum[j];
+  __syncthreads();
+  const int col = panel * 256 + threadIdx.x;
+  if (col < n) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += sm[i][threadIdx.x];
+    part[(size_t)rb * n + col] = s;
+  }
+}
+
+int pad8(int n) { return (n + 7) / 8 * 8; }
+
+// K slices of the 64 x 64 tiles: enough workgroups for two per CU, at least
+// four K blocks each, and partial sums of at most 64 MB.
+int any_slices(int dtype, int M, int N, int K) {
+  if (M == 0 || N == 0) return 1;
+  const int64_t tiles = cdiv64(M, 64) * cdiv64(N, 64);
+  const int bk = dtype == 0 ? 32 : 64;
+  int64_t s = std::min<int64_t>({cdiv64(512, tiles), cdiv64(K, 4 * bk), 32});
+  while (s > 1 && s * M * pad8(N) * 4 > ((int64_t)64 << 20)) --s;
+  if (s <= 1) return 1;
+  const int64_t kper = cdiv64(cdiv64(K, s), bk) * bk;
+  return (int)cdiv64(K, kper);
+}
+
+size_t product_ws_bytes(int dtype, int M, int N, int K) {
+  const int s = any_slices(dtype, M, N, K);
+  return s > 1 ? (size_t)s * M * pad8(N) * 4 : 0;
+}
+
+template <typename T>
+void run_any(const Product& p, const Epilogue& e, int slices, float* part, hipStream_t s) {
+  const int bk = 128 / sizeof(T);
+  const int kper = (int)(cdiv64(cdiv64(p.K, slices), bk) * bk), np = pad8(p.N);
+  const dim3 grid((unsigned)(cdiv64(p.N, 64) * cdiv64(p.M, 64)), (unsigned)slices);
+  float* dst = slices > 1 ? part : nullptr;
+  if (p.a_along && p.b_along)
+    launch_k(linear_any_kernel<T, true, true>, grid, 256, 0, s, p, e, kper, dst, np);
+  else if (p.a_along)
+    launch_k(linear_any_kernel<T, true, false>, grid, 256, 0, s, p, e, kper, dst, np);
+  else
+    launch_k(linear_any_kernel<T, false, false>, grid, 256, 0, s, p, e, kper, dst, np);
+  if (slices > 1) {
+    const int64_t chunks = (int64_t)p.M * ((p.N + 31) / 32 * 4);
+    launch_k(linear_reduce_kernel<T>, (unsigned)cdiv64(chunks, 256), 256, 0, s, (const float*)part,
+             slices, p.M, p.N, np, e);
+  }
+}
+
+hipError_t run_product(int dtype, const Product& p, const Epilogue& e, void* ws, hipStream_t s) {
+  const int slices = any_slices(dtype, p.M, p.N, p.K);
+  if (dtype == 0) run_any<float>(p, e, slices, (float*)ws, s);
+  else run_any<bf16_t>(p, e, slices, (float*)ws, s);
+  return hipGetLastError();
+}
+
+size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+
+// Workspace of the backward pass: dz, the bias gradient's partial sums, a
+// restored from its checkpoint, the products' K slices.
+struct BackSpace {
+  size_t dz, part, a, prod, bytes;
+  BackSpace(int dtype, int act, int m, int n, int k) {
+    const size_t es = dtype == 0 ? 4 : 2;
+    dz = 0;
+    part = dz + (act == ACT_NONE ? 0 : up256((size_t)m * pad8(n) * es));
+    a = part + up256((size_t)cdiv64(m, 64) * n * 4);
+    prod = a + up256((size_t)m * pad8(k) * es);
+    bytes = prod + up256(std::max(product_ws_bytes(dtype, m, k, n), product_ws_bytes(dtype, n, k, m)));
+  }
+};
+
+}  // namespace
+
+size_t linear_ws_bytes(int dtype, int m, int n, int k) { return up256(product_ws_bytes(dtype, m, n, k)); }
+
+size_t linear_backward_ws_bytes(int dtype, int act, int m, int n, int k) {
+  return BackSpace(dtype, act, m, n, k).bytes;
+}
+
+hipError_t launch_linear(int dtype, int m, int n, int k, const void* a, int64_t lda, const void* w,
+                         int64_t ldw, const LinearOut& o, void* ws, hipStream_t s) {
+  const Product p{a, lda, true, w, ldw, true, m, n, k};
+  const Epilogue e{o.bias, o.res, o.ldr, o.out, o.ldo, o.z, o.ldz, o.z_codes, o.z_scales,
+                   o.out_codes, o.out_scales, o.act};
+  return run_product(dtype, p, e, ws, s);
+}
+
+hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipStream_t s) {
+  const BackSpace sp(dtype, b.act, b.m, b.n, b.k);
+  char* base = static_cast<char*>(ws);
+  const void* dz = b.dout;
+  int64_t lddz = b.ldo;
+  float* part = b.dbias ? (float*)(base + sp.part) : nullptr;
+  const bool need_dz = b.act != ACT_NONE && (b.da || b.dw);
+  if (b.m == 0) {
+    // no rows: the weight's gradients are 0
+    if (b.dbias) {
+      const hipError_t err = launch_colsum(part, 0, b.n, b.dbias, nullptr, s);
+      if (err != hipSuccess) return err;
+    }
+  } else if (need_dz || part) {
+    const unsigned grid = (unsigned)(cdiv64(b.n, 256) * cdiv64(b.m, 64));
+    void* dst = need_dz ? base + sp.dz : nullptr;
+    const int64_t ld8 = pad8(b.n);
+    if (dtype == 0)
+      launch_k(act_grad_kernel<float>, grid, 256, 0, s, (const float*)b.dout, b.ldo, b.m, b.n, b.act,
+               (const float*)b.z, b.ldz, b.z_codes, b.z_scales, (float*)dst, ld8, part);
+    else
+      launch_k(act_grad_kernel<bf16_t>, grid, 256, 0, s, (const bf16_t*)b.dout, b.ldo, b.m, b.n, b.act,
+               (const bf16_t*)b.z, b.ldz, b.z_codes, b.z_scales, (bf16_t*)dst, ld8, part);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    if (need_dz) dz = dst, lddz = ld8;
+    if (part) {
+      err = launch_colsum(part, (int)cdiv64(b.m, 64), b.n, b.dbias, nullptr, s);
+      if (err != hipSuccess) return err;
+    }
+  }
+  Epilogue e{};
+  if (b.da && b.m > 0) {
+    e.out = b.da;
+    e.ldo = b.ldda;
+    const hipError_t err =
+        run_product(dtype, Product{dz, lddz, true, b.w, b.ldw, false, b.m, b.k, b.n}, e, base + sp.prod, s);
+    if (err != hipSuccess) return err;
+  }
+  if (b.dw) {
+    const void* a = b.a;
+    int64_t lda = b.lda;
+    if (b.a_codes && b.m > 0) {
+      a = base + sp.a;
+      lda = pad8(b.k);
+      const hipError_t err =
+          launch_restore(dtype, b.a_codes, b.a_scales, b.m, b.k, base + sp.a, lda, s);
+      if (err != hipSuccess) return err;
+    }
+    e.out = b.dw;
+    e.ldo = b.lddw;
+    return run_product(dtype, Product{dz, lddz, false, a, lda, false, b.n, b.k, b.m}, e, base + sp.prod, s);
+  }
+  return hipSuccess;
+}
+
+}  // namespace fs

@@ -1,0 +1,598 @@
+"""The dense sublayer's operators on the GPU against the fp64 oracle.
+
+Tolerances are bounds, from the operations that round.  A sum of K fp32
+products errs by at most K * 2^-23 of the sum of their absolute values (a
+product and an add each round once, 2^-24); a stored value by half a step of
+its type (bf16 2^-8 of it, fp32 2^-24); the activations' hardware exponential
+and reciprocal by at most 2^-20 of the value.  |act'| is at most 1.13."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_11505_amd as fs
+from oracle import layer as O
+from paper_2511_11505_amd import _lib as L
+from tests._util import f64
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+DEV = "cuda"
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
+CODE = {"f32": L.FS_F32, "bf16": L.FS_BF16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+U = 2.0 ** -23
+ACT = 2.0 ** -20
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def mat(g, m, n, dtype, pad=0, scale=1.0, poison=float("nan"), lead=0):
+    """[m, n] view with row stride n + pad; what is around it is NaN, so that a
+    read past a row's end shows."""
+    full = torch.full((m + 2, n + pad), poison, dtype=TORCH[dtype], device=DEV)
+    v = full.view(-1)[lead:lead + (m + 1) * (n + pad)].view(m + 1, n + pad)[:m, :n]
+    v.copy_(scale * torch.randn((m, n), generator=g, device=DEV))
+    return v
+
+
+class Out:
+    """An output [m, n] inside a buffer of a sentinel, which has to stay."""
+
+    def __init__(self, m, n, dtype, pad=0):
+        self.full = torch.full((m + 2, n + pad), -77.0, dtype=TORCH[dtype], device=DEV)
+        self.view = self.full[1:m + 1, :n]
+        self.m, self.n = m, n
+
+    def get(self):
+        rest = self.full.clone()
+        rest[1:self.m + 1, :self.n] = -77.0
+        assert bool((rest == -77.0).all()), "wrote outside the output"
+        return f64(self.view)
+
+
+class Codes:
+    def __init__(self, m, n):
+        self.pair = fs.checkpoint_buffers(m, n)
+        for t in self.pair:
+            t.fill_(0x5A)
+
+    def get(self):
+        return tuple(t.cpu().numpy() for t in self.pair)
+
+
+def workspace(nbytes):
+    """Exactly nbytes of 0xFF (NaNs), with a guard behind."""
+    ws = torch.full((nbytes + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+    return ws, (ws.data_ptr(), nbytes)
+
+
+def guard(ws, pair):
+    assert bool((ws[pair[1]:] == 0xFF).all()), "wrote past the workspace"
+
+
+def near(got, want, tol):
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), (np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4], np.asarray(tol)[bad][:4])
+    assert np.isfinite(got).all()
+
+
+def act_tol(z, zerr, name, value):
+    """Error of act(z) from z's and its own."""
+    return zerr if name == "none" else 1.13 * zerr + ACT * (np.abs(value) + np.abs(z) * 1e-3)
+
+
+# ------------------------------------------------------------------- linear
+SIZES = [(1, 1, 1), (1, 64, 64), (3, 5, 7), (17, 33, 31), (64, 64, 64), (65, 129, 130), (1, 300, 4096),
+         (8, 96, 520), (130, 72, 1000), (200, 264, 96), (5, 1000, 2049), (257, 520, 328), (520, 260, 200)]
+
+
+def check_linear(m, n, k, dtype, act, bias, residual, pad, seed=0, lead=0, scale_w=None, save=True):
+    g = gen(seed + m + 3 * n + 7 * k)
+    a = mat(g, m, k, dtype, pad, lead=lead)
+    w = mat(g, n, k, dtype, pad, scale_w or k ** -0.5, lead=lead)
+    b = torch.randn((n,), generator=g, device=DEV) if bias else None
+    r = mat(g, m, n, dtype, pad) if residual else None
+    desc = fs.linear_desc(m, n, k, dtype, act)
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR))
+    out, z, zc, oc = Out(m, n, dtype, pad), Out(m, n, dtype, pad), Codes(m, n), Codes(m, n)
+    save_z = fs.fs_saved(z.view.data_ptr(), z.view.stride(0), zc.pair[0].data_ptr(), zc.pair[1].data_ptr())
+    fs.fs_linear(desc, a, w, b, r, out.view, wp, save_z=save_z if save else None,
+                 save_out=oc.pair if save else None)
+    torch.cuda.synchronize()
+    guard(ws, wp)
+    A, W = f64(a), f64(w)
+    Z, want = O.linear(A, W, None if b is None else f64(b), None if r is None else f64(r), act)
+    zerr = (k + 2) * U * (np.abs(A) @ np.abs(W).T + (0 if b is None else np.abs(f64(b))))
+    value = O.act(Z, act)
+    tol = act_tol(Z, zerr, act, value) + (0 if r is None else U * np.abs(want)) + HALF[dtype] * np.abs(want)
+    near(out.get(), want, tol + HALF[dtype] * tol)
+    if save:
+        near(z.get(), Z, zerr + HALF[dtype] * (np.abs(Z) + zerr))
+        # the checkpoints are those of the stored rows, code for code
+        for rows, c in ((z, zc), (out, oc)):
+            want_c = O.checkpoint(f64(rows.view))
+            assert all(np.array_equal(x, y) for x, y in zip(c.get(), want_c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_linear(m, n, k, dtype):
+    check_linear(m, n, k, dtype, "none", False, False, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("m,n,k,pad", [(33, 70, 45, 0), (33, 70, 45, 3), (96, 128, 192, 8), (2, 40, 2048, 0)])
+def test_linear_epilogue(m, n, k, pad, act, dtype):
+    check_linear(m, n, k, dtype, act, True, True, pad)
+
+
+@pytest.mark.parametrize("m,n,k", [(64, 128, 128), (3, 40, 1000), (300, 130, 264)])
+def test_linear_unaligned_base(m, n, k):
+    """Bases that only their element aligns."""
+    check_linear(m, n, k, "bf16", "silu", True, False, 0, lead=1)
+    check_linear(m, n, k, "f32", "silu", True, False, 0, lead=3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_adds_into_the_residual(dtype):
+    """out may be the residual itself, split over K or not."""
+    for m, n, k in ((4, 40, 4096), (70, 96, 64)):
+        g = gen(m)
+        a, w, r = mat(g, m, k, dtype), mat(g, n, k, dtype, 0, k ** -0.5), mat(g, m, n, dtype)
+        desc = fs.linear_desc(m, n, k, dtype)
+        ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR))
+        want = torch.empty_like(r)
+        fs.fs_linear(desc, a, w, None, r, want, wp)
+        got = r.clone()
+        fs.fs_linear(desc, a, w, None, got, got, wp)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(5, 70, 100), (300, 520, 264)])
+def test_linear_keeps_non_finite_values_in_their_rows(m, n, k, dtype):
+    """A NaN or infinity in one token or output reaches its own row or column
+    only, and reaches all of that."""
+    g = gen(1)
+    a, w = mat(g, m, k, dtype), mat(g, n, k, dtype, 0, k ** -0.5)
+    a[m - 1, k - 1] = float("nan")
+    w[n - 2, 0] = float("inf")
+    desc = fs.linear_desc(m, n, k, dtype)
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR))
+    out, oc = Out(m, n, dtype), Codes(m, n)
+    fs.fs_linear(desc, a, w, None, None, out.view, wp, save_out=oc.pair)
+    torch.cuda.synchronize()
+    o = out.get()
+    assert np.isnan(o[m - 1]).all() and np.isinf(o[:m - 1, n - 2]).all()
+    assert np.isfinite(np.delete(o[:m - 1], n - 2, axis=1)).all()
+    assert all(np.array_equal(x, y) for x, y in zip(oc.get(), O.checkpoint(o)))
+
+
+def check_backward(m, n, k, dtype, act, pad, coded, seed=0, lead=0):
+    g = gen(seed + m + 3 * n + 7 * k)
+    a, z, dout = mat(g, m, k, dtype, pad, lead=lead), mat(g, m, n, dtype, pad, 1.3, lead=lead), mat(g, m, n, dtype, pad, lead=lead)
+    w = mat(g, n, k, dtype, pad, n ** -0.5, lead=lead)
+    desc = fs.linear_desc(m, n, k, dtype, act)
+    A, Z = f64(a), f64(z)
+    sa, sz = a, z
+    if coded:
+        sa, sz = Codes(m, k), Codes(m, n)
+        fs.fs_checkpoint_fp8(CODE[dtype], m, k, a, *sa.pair)
+        fs.fs_checkpoint_fp8(CODE[dtype], m, n, z, *sz.pair)
+        A, Z = O.restore(*sa.get()), O.restore(*sz.get())
+        sa, sz = sa.pair, sz.pair
+    da, dw = Out(m, k, dtype, pad), Out(n, k, dtype, pad)
+    db = torch.full((n,), float("nan"), device=DEV)
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR_BACKWARD))
+    fs.fs_linear_backward(desc, dout, sa, w, None if act == "none" else sz, da.view, dw.view, db, wp)
+    torch.cuda.synchronize()
+    guard(ws, wp)
+    G, W = f64(dout), f64(w)
+    wa, ww, wb, dz = O.linear_backward(G, A, W, Z, act)
+    # dz: the slope's error (its terms are at most 1 + |z|), then the rounding
+    serr = 0.0 if act == "none" else ACT * (1 + np.abs(Z)) * np.abs(G)
+    zerr = serr if act == "none" else serr + HALF[dtype] * (np.abs(dz) + serr)
+    zerr = zerr + np.zeros_like(dz)
+    hd = HALF[dtype]
+    ta = zerr @ np.abs(W) + (n + 2) * U * (np.abs(dz) @ np.abs(W))
+    tw = zerr.T @ np.abs(A) + (m + 2) * U * (np.abs(dz).T @ np.abs(A))
+    near(da.get(), wa, ta * (1 + hd) + hd * np.abs(wa))
+    near(dw.get(), ww, tw * (1 + hd) + hd * np.abs(ww))
+    near(f64(db), wb, (serr + np.zeros_like(dz)).sum(0) + (m + 2) * U * np.abs(dz).sum(0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_linear_backward(m, n, k, dtype):
+    check_backward(m, n, k, dtype, "none", 0, False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("m,n,k,pad", [(33, 70, 45, 3), (96, 128, 192, 8), (130, 40, 2048, 0), (1, 33, 40, 0)])
+def test_linear_backward_epilogue(m, n, k, pad, coded, act, dtype):
+    check_backward(m, n, k, dtype, act, pad, coded)
+
+
+def test_linear_backward_unaligned_base():
+    check_backward(70, 136, 264, "bf16", "gelu", 0, False, lead=1)
+    check_backward(70, 136, 264, "f32", "gelu", 0, False, lead=3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_backward_parts(dtype):
+    """Each gradient alone is what it is beside the others."""
+    m, n, k = 70, 136, 200
+    g = gen(9)
+    a, z, dout, w = mat(g, m, k, dtype), mat(g, m, n, dtype), mat(g, m, n, dtype), mat(g, n, k, dtype)
+    desc = fs.linear_desc(m, n, k, dtype, "silu")
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR_BACKWARD))
+
+    def run(ia, iw, ib):
+        da, dw = torch.empty((m, k), dtype=TORCH[dtype], device=DEV), torch.empty((n, k), dtype=TORCH[dtype], device=DEV)
+        db = torch.empty((n,), device=DEV)
+        fs.fs_linear_backward(desc, dout, a if iw else None, w if ia else None, z, da if ia else None,
+                              dw if iw else None, db if ib else None, wp)
+        return da, dw, db
+
+    every = run(1, 1, 1)
+    for i in range(3):
+        assert torch.equal(run(*(int(i == j) for j in range(3)))[i], every[i])
+
+
+def test_linear_backward_without_tokens():
+    desc = fs.linear_desc(0, 40, 24, "bf16", "gelu")
+    dw, db = torch.ones((40, 24), dtype=torch.bfloat16, device=DEV), torch.ones((40,), device=DEV)
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR_BACKWARD))
+    fs.fs_linear_backward(desc, None, None, None, None, None, dw, db, wp)
+    torch.cuda.synchronize()
+    assert float(dw.float().abs().sum() + db.abs().sum()) == 0.0
+
+
+# --------------------------------------------------------------- layer norm
+NORM_SIZES = [(1, 1), (3, 7), (5, 64), (2, 515), (9, 1000), (4, 2048), (7, 2056), (3, 5120), (6, 7169),
+              (2, 12345), (1, 32768)]
+
+
+def depth(d):
+    """Adds in the longest chain of a row's sum: a thread's 8 columns of at
+    most 4 chunks, the lanes, the waves."""
+    return 32 + 6 + 16
+
+
+def check_norm(m, d, dtype, center, add, affine, pad, offset=0.0, eps=1e-5):
+    g = gen(m + d)
+    x = mat(g, m, d, dtype, pad)
+    x += offset
+    e = mat(g, m, d, dtype, pad) if add else None
+    gam = 1 + 0.3 * torch.randn((d,), generator=g, device=DEV) if affine else None
+    bet = torch.randn((d,), generator=g, device=DEV) if affine else None
+    desc = fs.norm_desc(m, d, dtype, center, eps)
+    s, y = Out(m, d, dtype, pad), Out(m, d, dtype, pad)
+    mean, rstd = torch.full((m,), float("nan"), device=DEV), torch.full((m,), float("nan"), device=DEV)
+    xc, yc = Codes(m, d), Codes(m, d)
+    fs.fs_layer_norm(desc, x, e, gam, bet, s.view, y.view, mean, rstd, save_in=xc.pair, save_y=yc.pair)
+    torch.cuda.synchronize()
+    S = s.get()
+    if add:
+        exact = f64(x) + f64(e)
+        near(S, exact, HALF[dtype] * np.abs(exact) + U * np.abs(exact))
+    else:
+        assert np.array_equal(S, f64(x))
+    G, B = (None if t is None else f64(t) for t in (gam, bet))
+    Y, M, R = O.layer_norm(S, G, B, center, eps)
+    # mean: its sum's chain; then var, from differences that err by the mean's
+    # error and a rounding; rstd by half of var's relative error and three
+    # roundings
+    merr = (depth(d) * U * np.abs(S).mean(1) + U * np.abs(M)) if center else np.zeros(m)
+    dev = S - M[:, None]
+    derr = merr[:, None] + U * np.abs(dev)
+    verr = (2 * np.abs(dev) * derr + derr ** 2).mean(1) + (depth(d) + 2) * U * (dev ** 2).mean(1)
+    rrel = 0.5 * verr * R ** 2 + verr ** 2 * R ** 4 + 4 * U
+    near(f64(mean), M if center else np.zeros(m), merr + 1e-30)
+    near(f64(rstd), R, rrel * R)
+    yerr = (derr * R[:, None] + np.abs(dev) * (R * rrel)[:, None]) * (1 if G is None else np.abs(G))
+    yerr = yerr + 3 * U * (np.abs(Y) + (0 if B is None else 2 * np.abs(B)))
+    near(y.get(), Y, yerr * (1 + HALF[dtype]) + HALF[dtype] * np.abs(Y))
+    for rows, c in ((S, xc), (y.get(), yc)):
+        assert all(np.array_equal(p, q) for p, q in zip(c.get(), O.checkpoint(rows)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,d", NORM_SIZES)
+def test_norm(m, d, dtype):
+    check_norm(m, d, dtype, True, True, True, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("add,affine,pad", [(False, True, 0), (True, False, 1), (False, False, 8)])
+def test_norm_forms(add, affine, pad, center, dtype):
+    for m, d in ((5, 77), (3, 4096)):
+        check_norm(m, d, dtype, center, add, affine, pad)
+
+
+def test_norm_of_far_and_flat_rows():
+    """A mean a thousand times the spread, and rows without spread."""
+    check_norm(4, 1000, "f32", True, False, True, 0, offset=1000.0)
+    for dtype in ("f32", "bf16"):
+        x = torch.full((3, 100), 2.5, dtype=TORCH[dtype], device=DEV)
+        x[1] = 0
+        y, rstd = torch.empty_like(x), torch.empty((3,), device=DEV)
+        fs.fs_layer_norm(fs.norm_desc(3, 100, dtype, True, 1e-2), x, None, None, None, None, y, None, rstd)
+        torch.cuda.synchronize()
+        assert float(y.float().abs().max()) == 0.0
+        assert np.allclose(f64(rstd), 10.0, rtol=1e-6)
+
+
+def test_norm_in_place_and_non_finite_rows():
+    g = gen(2)
+    for m, d in ((5, 200), (4, 3000)):
+        x, e = mat(g, m, d, "bf16"), mat(g, m, d, "bf16")
+        desc = fs.norm_desc(m, d, "bf16")
+        s, y = torch.empty_like(x), torch.empty_like(x)
+        fs.fs_layer_norm(desc, x, e, None, None, s, y, None, None)
+        x2, e2 = x.clone(), e.clone()
+        fs.fs_layer_norm(desc, x2, e2, None, None, x2, e2, None, None)
+        torch.cuda.synchronize()
+        assert torch.equal(x2, s) and torch.equal(e2, y)
+        x[1, 3], x[2, 0] = float("inf"), float("nan")
+        bad = torch.empty_like(x)
+        fs.fs_layer_norm(desc, x, e, None, None, None, bad, None, None)
+        torch.cuda.synchronize()
+        assert bool(bad[1:3].isnan().all())
+        keep = [0, *range(3, m)]
+        assert torch.equal(bad[keep], y[keep])
+
+
+def check_norm_backward(m, d, dtype, center, coded, dres, affine, pad):
+    g = gen(m + d)
+    x, dy = mat(g, m, d, dtype, pad), mat(g, m, d, dtype, pad)
+    r = mat(g, m, d, dtype, pad) if dres else None
+    gam = 1 + 0.3 * torch.randn((d,), generator=g, device=DEV) if affine else None
+    S = f64(x)
+    sx = x
+    if coded:
+        c = Codes(m, d)
+        fs.fs_checkpoint_fp8(CODE[dtype], m, d, x, *c.pair)
+        S, sx = O.restore(*c.get()), c.pair
+    _, M, R = O.layer_norm(f64(x), None, None, center)
+    mean, rstd = (torch.tensor(t, dtype=torch.float32, device=DEV) for t in (M, R))
+    M, R = f64(mean), f64(rstd)
+    desc = fs.norm_desc(m, d, dtype, center)
+    dx = Out(m, d, dtype, pad)
+    dg, db = torch.full((d,), float("nan"), device=DEV), torch.full((d,), float("nan"), device=DEV)
+    ws, wp = workspace(fs.fs_layer_norm_workspace(desc))
+    fs.fs_layer_norm_backward(desc, dy, sx, mean if center else None, rstd, gam, r, dx.view, dg, db, wp)
+    torch.cuda.synchronize()
+    guard(ws, wp)
+    DY, RES = f64(dy), None if r is None else f64(r)
+    G = None if gam is None else f64(gam)
+    wx, wg, wb = O.layer_norm_backward(DY, S, M, R, G, RES, center)
+    h = (S - M[:, None]) * R[:, None]
+    u = DY if G is None else DY * G
+    herr, uerr = 2 * U * (np.abs(h) + np.abs(M * R)[:, None]), U * np.abs(u)
+    chain = (depth(d) + 2) * U
+    m1, m2 = np.abs(u).mean(1), (np.abs(u * h)).mean(1)
+    e1 = chain * m1
+    e2 = chain * m2 + (herr * np.abs(u) + uerr * np.abs(h)).mean(1)
+    terr = uerr + e1[:, None] + herr * m2[:, None] + np.abs(h) * e2[:, None]
+    terr = terr + 4 * U * (np.abs(u) + m1[:, None] + np.abs(h) * m2[:, None])
+    xerr = terr * R[:, None] + 2 * U * (np.abs(wx) + (0 if RES is None else np.abs(RES)))
+    near(dx.get(), wx, xerr * (1 + HALF[dtype]) + HALF[dtype] * np.abs(wx))
+    near(f64(dg), wg, (m + 34) * U * np.abs(DY * h).sum(0) + (np.abs(DY) * herr).sum(0))
+    near(f64(db), wb, (m + 34) * U * np.abs(DY).sum(0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("m,d", NORM_SIZES + [(700, 40), (1100, 300), (600, 2100)])
+def test_norm_backward(m, d, coded, dtype):
+    check_norm_backward(m, d, dtype, True, coded, True, True, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("dres,affine,pad", [(False, True, 0), (True, False, 1), (False, False, 8)])
+def test_norm_backward_forms(dres, affine, pad, center, dtype):
+    for m, d in ((5, 77), (9, 4096)):
+        check_norm_backward(m, d, dtype, center, pad == 1, dres, affine, pad)
+
+
+def test_norm_backward_parts_in_place_and_without_rows():
+    m, d = 40, 600
+    g = gen(5)
+    x, dy, r = (mat(g, m, d, "bf16") for _ in range(3))
+    mean, rstd = torch.zeros((m,), device=DEV), torch.ones((m,), device=DEV)
+    desc = fs.norm_desc(m, d, "bf16")
+    ws, wp = workspace(fs.fs_layer_norm_workspace(desc))
+
+    def run(dy, r, dx, dg, db, wp):
+        fs.fs_layer_norm_backward(desc, dy, x, mean, rstd, None, r, dx, dg, db, wp)
+        return dx
+
+    dg, db = torch.empty((d,), device=DEV), torch.empty((d,), device=DEV)
+    want = run(dy, r, torch.empty_like(dy), dg, db, wp)
+    g1, b1 = torch.empty_like(dg), torch.empty_like(db)
+    assert torch.equal(run(dy, r, torch.empty_like(dy), None, None, None), want)
+    run(dy, r, torch.empty_like(dy), g1, None, wp)
+    run(dy, r, torch.empty_like(dy), None, b1, wp)
+    assert torch.equal(g1, dg) and torch.equal(b1, db)
+    y2, r2 = dy.clone(), r.clone()
+    assert torch.equal(run(y2, r, y2, None, None, None), want)
+    assert torch.equal(run(dy, r2, r2, None, None, None), want)
+    none = fs.norm_desc(0, d, "bf16")
+    fs.fs_layer_norm_backward(none, None, None, None, None, None, None, None, g1, b1, None)
+    torch.cuda.synchronize()
+    assert float(g1.abs().sum() + b1.abs().sum()) == 0.0
+
+
+# -------------------------------------------------------------- checkpoints
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,d,pad", [(1, 1, 0), (3, 31, 0), (5, 32, 1), (7, 33, 0), (300, 70, 8), (9, 2500, 3)])
+def test_checkpoint(m, d, pad, dtype):
+    g = gen(m + d)
+    x = mat(g, m, d, dtype, pad)
+    x.mul_(torch.exp(6 * torch.randn((m, d), generator=g, device=DEV)))
+    c, back = Codes(m, d), Out(m, d, dtype, pad)
+    fs.fs_checkpoint_fp8(CODE[dtype], m, d, x, *c.pair)
+    fs.fs_checkpoint_restore(CODE[dtype], m, d, *c.pair, back.view)
+    torch.cuda.synchronize()
+    assert all(np.array_equal(p, q) for p, q in zip(c.get(), O.checkpoint(f64(x))))
+    assert np.array_equal(back.get(), O.restore(*c.get()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_checkpoint_edges(dtype):
+    """Ties, the border of a scale, the smallest and largest values, zeros of
+    both signs, infinities and NaNs."""
+    big = float(torch.finfo(TORCH[dtype]).max)
+    rows = [[448.0, 17.0, 19.0, -0.0, 2.0 ** -9, 2.0 ** -10, 1.5 * 2.0 ** -9], [450.0, 17.0, 1.0], [0.0, -0.0],
+            [big, -big, 1.0], [2.0 ** -126, 2.0 ** -117, -2.0 ** -120], [1e-38, 2e-38], [float("inf"), 1.0],
+            [float("nan"), 5.0], [-float("inf")]]
+    x = torch.zeros((len(rows), 64), dtype=TORCH[dtype], device=DEV)
+    for i, r in enumerate(rows):
+        x[i, :len(r)] = torch.tensor(r, device=DEV).to(TORCH[dtype])
+        x[i, 63] = 3.0
+    c, back = Codes(len(rows), 64), torch.empty_like(x)
+    fs.fs_checkpoint_fp8(CODE[dtype], len(rows), 64, x, *c.pair)
+    fs.fs_checkpoint_restore(CODE[dtype], len(rows), 64, *c.pair, back)
+    torch.cuda.synchronize()
+    want = O.checkpoint(f64(x))
+    assert all(np.array_equal(p, q) for p, q in zip(c.get(), want))
+    assert np.array_equal(f64(back), O.restore(*want), equal_nan=True)
+
+
+# ------------------------------------------------------------ used together
+def sublayer_oracle(x, dout, p, act, center, rounded, coded):
+    """Forward and gradients of DenseSublayer with its roundings."""
+    gam, bet, w1, b1, w2, b2 = p
+    keep = (lambda t: O.restore(*O.checkpoint(t))) if coded else (lambda t: t)
+    h, mean, rstd = O.layer_norm(x, gam, bet, center)
+    h = rounded(h)
+    z, u = O.linear(h, w1, b1, None, act)
+    u = rounded(u)
+    _, out = O.linear(u, w2, b2, x)
+    z = rounded(z)
+    du, dw2, db2, _ = O.linear_backward(dout, keep(u), w2)
+    dh, dw1, db1, _ = O.linear_backward(rounded(du), keep(h), w1, keep(z), act)
+    dx, dg, db = O.layer_norm_backward(rounded(dh), keep(x), mean, rstd, gam, dout, center)
+    return out, dict(x=dx, gamma=dg, beta=db, w1=dw1, b1=db1, w2=dw2, b2=db2)
+
+
+def make_sublayer(n, d, f, dtype, act, center, save, seed=0):
+    g = gen(seed)
+    t = TORCH[dtype]
+    p = [1 + 0.2 * torch.randn((d,), generator=g, device=DEV), 0.2 * torch.randn((d,), generator=g, device=DEV),
+         (torch.randn((f, d), generator=g, device=DEV) * d ** -0.5).to(t), 0.2 * torch.randn((f,), generator=g, device=DEV),
+         (torch.randn((d, f), generator=g, device=DEV) * f ** -0.5).to(t), 0.2 * torch.randn((d,), generator=g, device=DEV)]
+    layer = fs.DenseSublayer(n, *p, act=act, center=center, save=save)
+    x, dout = (torch.randn((n, d), generator=g, device=DEV).to(t) for _ in range(2))
+    grads = dict(x=torch.empty_like(x), w1=torch.empty_like(p[2]), w2=torch.empty_like(p[4]),
+                 **{k: torch.empty((s,), device=DEV) for k, s in (("gamma", d), ("beta", d), ("b1", f), ("b2", d))})
+    return p, layer, x, dout, grads
+
+
+# With fp32 rows the sublayer's values and gradients differ from the oracle's
+# by sums of at most 600 terms: 600 * 2^-23 of sums of absolute values, which
+# are about sqrt(600) = 25 times the sums: 2e-3 of the rms at worst.  In bf16
+# a stored h, u, du, dh and dz each err by half a step, 2^-9 on average; of
+# five such in turn at most 5 * 2^-8 = 2e-2.  (relative norms)
+@pytest.mark.parametrize("dtype,tol", [("f32", 2e-3), ("bf16", 2e-2)])
+@pytest.mark.parametrize("save", ["rows", "codes"])
+@pytest.mark.parametrize("n,d,f,act,center", [(70, 96, 264, "silu", True), (33, 130, 70, "gelu", False),
+                                              (600, 128, 320, "relu", True)])
+def test_sublayer(n, d, f, act, center, save, dtype, tol):
+    p, layer, x, dout, grads = make_sublayer(n, d, f, dtype, act, center, save)
+    out = layer.forward(x, torch.empty_like(x))
+    layer.backward(dout, grads)
+    torch.cuda.synchronize()
+
+    def rounded(v):
+        return f64(torch.tensor(v).to(TORCH[dtype]))
+
+    want, wg = sublayer_oracle(f64(x), f64(dout), [f64(t) for t in p], act, center, rounded, save == "codes")
+
+    def rel(a, b):
+        return np.linalg.norm(f64(a) - b) / np.linalg.norm(b)
+
+    assert rel(out, want) <= tol
+    for k, v in grads.items():
+        # codes: a value at a code's border may fall to the other side (two in
+        # a thousand do in bf16, one step of 2^-3 each: 2^-3 sqrt(2e-3) = 6e-3)
+        assert rel(v, wg[k]) <= tol + (6e-3 if save == "codes" else 0), k
+
+
+def test_sublayer_serving_matches_training():
+    p, layer, x, dout, grads = make_sublayer(40, 128, 256, "bf16", "silu", True, "codes")
+    want = layer.forward(x, torch.empty_like(x))
+    serve = fs.DenseSublayer(40, *p, act="silu")
+    got = serve.forward(x, torch.empty_like(x))
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    with pytest.raises(ValueError):
+        serve.backward(dout, grads)
+
+
+@pytest.mark.parametrize("n", [1, 64, 300])
+def test_sublayer_in_a_graph_and_on_a_side_stream(n):
+    """Forward and backward captured once and replayed on new inputs, with
+    eager work between; and the same calls on another stream."""
+    p, layer, x, dout, grads = make_sublayer(n, 256, 520, "bf16", "gelu", True, "codes")
+    _, eager, _, _, egrads = make_sublayer(n, 256, 520, "bf16", "gelu", True, "codes")
+    out, eout = torch.empty_like(x), torch.empty_like(x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer.forward(x, out)
+        layer.backward(dout, grads)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward(x, out)
+        layer.backward(dout, grads)
+    g = gen(77)
+    for _ in range(4):
+        x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        dout.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        eager.forward(x, eout)
+        eager.backward(dout, egrads)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eout)
+        for k in grads:
+            assert torch.equal(grads[k], egrads[k]), k
+
+
+def test_sublayer_in_the_far_skip_window():
+    """The sublayer as the next layer of a block: BEGIN, the sublayer on the
+    partial input, FINISH into its output."""
+    from workloads import CONFIGS, make_workload
+    cfg = CONFIGS["tiny"]
+    wl = make_workload(cfg, DEV)
+    blk = fs.MoEBlock(cfg, wl.w_router, None, wl.w_gate_up, wl.w_down, device=DEV)
+    d = cfg.hidden
+    p, layer, _, _, _ = make_sublayer(cfg.n_tokens, d, 2 * d, "f32", "silu", False, None)
+    comm = torch.cuda.Stream()
+    partial, out = torch.empty_like(wl.x), torch.empty_like(wl.x)
+    blk.begin(wl.x, partial, comm=comm)
+    layer.forward(partial, out)
+    nxt = out.clone()
+    blk.finish(wl.x, out, comm=comm)
+    routed = torch.empty_like(wl.x)
+    L.fs_combine_unpack(blk.desc, blk.y_ret(), blk.t["slot_to_row"], blk.t["topk_w"], None, routed, None)
+    torch.cuda.synchronize()
+    gam, bet, w1, b1, w2, b2 = (f64(t) for t in p)
+    h, _, _ = O.layer_norm(f64(partial), gam, bet, False)
+    want = O.linear(O.linear(h, w1, b1, None, "silu")[1], w2, b2, f64(partial))[1]
+    assert np.linalg.norm(f64(nxt) - want) <= 2e-3 * np.linalg.norm(want)
+    # FINISH adds the routed output, one rounding
+    both = f64(nxt) + f64(routed)
+    near(f64(out), both, 4 * U * (np.abs(f64(nxt)) + np.abs(f64(routed))))
+    blk.close()
