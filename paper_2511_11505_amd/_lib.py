@@ -393,81 +393,83 @@ def fs_moe_block_forward(desc, phase, weights, residual_in, partial_out, residua
 # Matrices are 2-D tensors with unit column stride (row strides are passed on)
 # or int addresses of gapless rows; a checkpoint is its (codes, scales) pair.
 # Types, shapes and devices are checked here, since the C side sees addresses.
+# These entries serve single tokens, whose kernels take a few microseconds, so
+# the checks and lookups are the cheapest that torch has (8 us less per call
+# than current_stream(), current_device() and is_cuda).
 _ELEM = {}
+_gpu = None
+
+
+def _here(stream):
+    """(current device, stream handle); device -2 without a GPU."""
+    global _gpu
+    if _gpu is None:
+        import torch
+        _ELEM.update({FS_F32: torch.float32, FS_BF16: torch.bfloat16, "u8": torch.uint8})
+        _gpu = ((torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+                if torch.cuda.is_available() else (lambda: -2, lambda device: 0))
+        if torch.cuda.is_available():
+            torch.cuda.init()
+    dev = _gpu[0]()
+    return dev, _gpu[1](dev) if stream is None else stream_handle(stream)
 
 
 def _bad(name, what):
     raise FsError(FS_ERR_INVALID, f"{name} must be {what}")
 
 
-def _elem_types():
-    if not _ELEM:
-        import torch
-        _ELEM.update({FS_F32: torch.float32, FS_BF16: torch.bfloat16, "f32": torch.float32,
-                      "u8": torch.uint8})
-    return _ELEM
-
-
-def _here(t, name):
-    import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        _bad(name, "on the current GPU")
-
-
-def _mat(t, name, dtype, rows, cols):
+def _mat(t, name, dtype, rows, cols, dev):
     """(address, row stride) of a matrix argument."""
     if t is None or isinstance(t, int):
         return t, cols
-    if t.dtype != _elem_types().get(dtype) or tuple(t.shape) != (rows, cols):
+    if t.dtype is not _ELEM.get(dtype) or t.shape != (rows, cols):
         _bad(name, f"[{rows}, {cols}] of the descriptor's type, not {list(t.shape)} of {t.dtype}")
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         _bad(name, "of unit column stride")
-    _here(t, name)
-    return t.data_ptr(), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
+    if t.get_device() != dev:
+        _bad(name, "on the current GPU")
+    return t.data_ptr(), ld if rows > 1 or ld > cols else cols
 
 
-def _vec(t, name, size):
-    """Address of an fp32 vector argument."""
+def _flat(t, name, dtype, shape, dev):
+    """Address of a gapless argument (vectors, codes, scales)."""
     if t is None or isinstance(t, int):
         return t
-    if t.dtype != _elem_types()["f32"] or tuple(t.shape) != (size,) or not t.is_contiguous():
-        _bad(name, f"[{size}] contiguous fp32, not {list(t.shape)} of {t.dtype}")
-    _here(t, name)
+    if t.dtype is not _ELEM.get(dtype) or t.shape != shape or not t.is_contiguous():
+        _bad(name, f"{list(shape)} contiguous {_ELEM.get(dtype)}, not {list(t.shape)} of {t.dtype}")
+    if t.get_device() != dev:
+        _bad(name, "on the current GPU")
     return t.data_ptr()
 
 
-def _codes(pair, name, rows, cols):
+def _codes(pair, name, rows, cols, dev):
     """Addresses of a checkpoint's codes and scales."""
-    out = []
-    for t, what, shape in zip(pair, ("codes", "scales"), ((rows, cols), (rows, (cols + 31) // 32))):
-        if t is not None and not isinstance(t, int):
-            if t.dtype != _elem_types()["u8"] or tuple(t.shape) != shape or not t.is_contiguous():
-                _bad(f"{name} {what}", f"{list(shape)} contiguous uint8, not {list(t.shape)} of {t.dtype}")
-            _here(t, name)
-            t = t.data_ptr()
-        out.append(t)
-    return out
+    codes, scales = pair
+    return (_flat(codes, f"{name} codes", "u8", (rows, cols), dev),
+            _flat(scales, f"{name} scales", "u8", (rows, (cols + 31) // 32), dev))
 
 
-def _saved(s, name, dtype, rows, cols):
+def _saved(s, name, dtype, rows, cols, dev):
     """fs_saved of a tensor, a (codes, scales) pair, an fs_saved, or None."""
     if s is None or isinstance(s, fs_saved):
         return s
     if isinstance(s, (tuple, list)):
-        return fs_saved(None, 0, *_codes(s, name, rows, cols))
-    return fs_saved(*_mat(s, name, dtype, rows, cols), None, None)
+        return fs_saved(None, 0, *_codes(s, name, rows, cols, dev))
+    return fs_saved(*_mat(s, name, dtype, rows, cols, dev), None, None)
 
 
 def fs_checkpoint_fp8(dtype, rows, cols, src, codes, scales, stream=None):
-    _check(load().fs_checkpoint_fp8(dtype, rows, cols, *_mat(src, "src", dtype, rows, cols),
-                                    *_codes((codes, scales), "checkpoint", rows, cols),
-                                    stream_handle(stream)))
+    dev, s = _here(stream)
+    _check(load().fs_checkpoint_fp8(dtype, rows, cols, *_mat(src, "src", dtype, rows, cols, dev),
+                                    *_codes((codes, scales), "checkpoint", rows, cols, dev), s))
 
 
 def fs_checkpoint_restore(dtype, rows, cols, codes, scales, dst, stream=None):
+    dev, s = _here(stream)
     _check(load().fs_checkpoint_restore(dtype, rows, cols,
-                                        *_codes((codes, scales), "checkpoint", rows, cols),
-                                        *_mat(dst, "dst", dtype, rows, cols), stream_handle(stream)))
+                                        *_codes((codes, scales), "checkpoint", rows, cols, dev),
+                                        *_mat(dst, "dst", dtype, rows, cols, dev), s))
 
 
 def fs_linear_workspace(desc, op):
@@ -477,22 +479,29 @@ def fs_linear_workspace(desc, op):
 
 
 def fs_linear(desc, a, w, bias, residual, out, ws, save_z=None, save_out=None, stream=None):
-    wp, wb = _ws(ws)
+    dev, s = _here(stream)
     dt, m, n, k = desc.dtype, desc.m, desc.n, desc.k
-    _check(load().fs_linear(ctypes.byref(desc), *_mat(a, "a", dt, m, k), *_mat(w, "w", dt, n, k),
-                            _vec(bias, "bias", n), *_mat(residual, "residual", dt, m, n),
-                            *_mat(out, "out", dt, m, n), _saved(save_z, "save_z", dt, m, n),
-                            _saved(save_out, "save_out", dt, m, n), wp, wb, stream_handle(stream)))
+    wp, wb = _ws(ws)
+    ap, lda = _mat(a, "a", dt, m, k, dev)
+    bp, ldb = _mat(w, "w", dt, n, k, dev)
+    rp, ldr = _mat(residual, "residual", dt, m, n, dev)
+    op, ldo = _mat(out, "out", dt, m, n, dev)
+    _check(load().fs_linear(ctypes.byref(desc), ap, lda, bp, ldb, _flat(bias, "bias", FS_F32, (n,), dev),
+                            rp, ldr, op, ldo, _saved(save_z, "save_z", dt, m, n, dev),
+                            _saved(save_out, "save_out", dt, m, n, dev), wp, wb, s))
 
 
 def fs_linear_backward(desc, dout, a, w, z, da, dw, dbias, ws, stream=None):
-    wp, wb = _ws(ws)
+    dev, s = _here(stream)
     dt, m, n, k = desc.dtype, desc.m, desc.n, desc.k
-    _check(load().fs_linear_backward(ctypes.byref(desc), *_mat(dout, "dout", dt, m, n),
-                                     _saved(a, "a", dt, m, k), *_mat(w, "w", dt, n, k),
-                                     _saved(z, "z", dt, m, n), *_mat(da, "da", dt, m, k),
-                                     *_mat(dw, "dw", dt, n, k), _vec(dbias, "dbias", n), wp, wb,
-                                     stream_handle(stream)))
+    wp, wb = _ws(ws)
+    gp, ldg = _mat(dout, "dout", dt, m, n, dev)
+    bp, ldb = _mat(w, "w", dt, n, k, dev)
+    xp, ldx = _mat(da, "da", dt, m, k, dev)
+    yp, ldy = _mat(dw, "dw", dt, n, k, dev)
+    _check(load().fs_linear_backward(ctypes.byref(desc), gp, ldg, _saved(a, "a", dt, m, k, dev), bp, ldb,
+                                     _saved(z, "z", dt, m, n, dev), xp, ldx, yp, ldy,
+                                     _flat(dbias, "dbias", FS_F32, (n,), dev), wp, wb, s))
 
 
 def fs_layer_norm_workspace(desc):
@@ -503,24 +512,34 @@ def fs_layer_norm_workspace(desc):
 
 def fs_layer_norm(desc, x, add, gamma, beta, sum_out, y, mean, rstd, save_in=None, save_y=None,
                   stream=None):
+    dev, s = _here(stream)
     dt, r, c = desc.dtype, desc.rows, desc.cols
-    _check(load().fs_layer_norm(ctypes.byref(desc), *_mat(x, "x", dt, r, c), *_mat(add, "add", dt, r, c),
-                                _vec(gamma, "gamma", c), _vec(beta, "beta", c),
-                                *_mat(sum_out, "sum_out", dt, r, c), *_mat(y, "y", dt, r, c),
-                                _vec(mean, "mean", r), _vec(rstd, "rstd", r),
-                                _saved(save_in, "save_in", dt, r, c),
-                                _saved(save_y, "save_y", dt, r, c), stream_handle(stream)))
+    xp, ldx = _mat(x, "x", dt, r, c, dev)
+    ap, lda = _mat(add, "add", dt, r, c, dev)
+    sp, lds = _mat(sum_out, "sum_out", dt, r, c, dev)
+    yp, ldy = _mat(y, "y", dt, r, c, dev)
+    _check(load().fs_layer_norm(ctypes.byref(desc), xp, ldx, ap, lda,
+                                _flat(gamma, "gamma", FS_F32, (c,), dev),
+                                _flat(beta, "beta", FS_F32, (c,), dev), sp, lds, yp, ldy,
+                                _flat(mean, "mean", FS_F32, (r,), dev),
+                                _flat(rstd, "rstd", FS_F32, (r,), dev),
+                                _saved(save_in, "save_in", dt, r, c, dev),
+                                _saved(save_y, "save_y", dt, r, c, dev), s))
 
 
 def fs_layer_norm_backward(desc, dy, x, mean, rstd, gamma, dres, dx, dgamma, dbeta, ws, stream=None):
-    wp, wb = _ws(ws)
+    dev, s = _here(stream)
     dt, r, c = desc.dtype, desc.rows, desc.cols
-    _check(load().fs_layer_norm_backward(ctypes.byref(desc), *_mat(dy, "dy", dt, r, c),
-                                         _saved(x, "x", dt, r, c), _vec(mean, "mean", r),
-                                         _vec(rstd, "rstd", r), _vec(gamma, "gamma", c),
-                                         *_mat(dres, "dres", dt, r, c), *_mat(dx, "dx", dt, r, c),
-                                         _vec(dgamma, "dgamma", c), _vec(dbeta, "dbeta", c), wp, wb,
-                                         stream_handle(stream)))
+    wp, wb = _ws(ws)
+    gp, ldg = _mat(dy, "dy", dt, r, c, dev)
+    rp, ldr = _mat(dres, "dres", dt, r, c, dev)
+    xp, ldx = _mat(dx, "dx", dt, r, c, dev)
+    _check(load().fs_layer_norm_backward(ctypes.byref(desc), gp, ldg, _saved(x, "x", dt, r, c, dev),
+                                         _flat(mean, "mean", FS_F32, (r,), dev),
+                                         _flat(rstd, "rstd", FS_F32, (r,), dev),
+                                         _flat(gamma, "gamma", FS_F32, (c,), dev), rp, ldr, xp, ldx,
+                                         _flat(dgamma, "dgamma", FS_F32, (c,), dev),
+                                         _flat(dbeta, "dbeta", FS_F32, (c,), dev), wp, wb, s))
 
 
 def fs_profile_enable(on=True):

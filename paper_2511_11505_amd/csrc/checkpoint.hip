@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void checkpoint_kernel(T* __restrict__ x, int6
       if (live) a = load8<T>(x + r * ld + c, n);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = a.get(i);
-      ckpt_store8<1, 2>(codes, scales, r, c, cols, v, n, live);
+      ckpt_store8<LANES_NEXT>(codes, scales, r, c, cols, v, n, live);
     }
   }
 }

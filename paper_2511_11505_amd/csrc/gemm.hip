@@ -1709,6 +1709,8 @@ hipError_t launch_grouped_ffn_fo_fp8(int G, int ffn, int d, const uint8_t* x, co
   return hipGetLastError();
 }
 
+int compute_units() { return num_cus(); }
+
 hipError_t launch_dense_linear(int dtype, int m, int n, int kdim, const void* a, const void* w,
                                void* out, hipStream_t s) {
   if (m <= 0) return hipSuccess;

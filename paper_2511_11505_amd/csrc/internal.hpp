@@ -109,6 +109,7 @@ void launch_r192_gateup(const void* A, const int32_t* rows, const int32_t* goff,
 void launch_r192_down(const void* A, const int32_t* rows, const int32_t* goff, int G,
                       int64_t m_total, const void* B, int K, int NOUT, void* C, int ldc, int cus,
                       int hmax, hipStream_t s);
+int compute_units();   // of the device, 256 without one
 hipError_t launch_dense_linear(int dtype, int m, int n, int kdim, const void* a, const void* w,
                                void* out, hipStream_t s);
 // Expert weights in MFMA fragment order: n_mats row-major [rows, cols] bf16

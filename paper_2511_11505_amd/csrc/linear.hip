@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "linear.hpp"
+#include "linear_rules.hpp"
 
 namespace fs {
 namespace {
@@ -17,28 +18,6 @@ namespace {
 typedef __attribute__((address_space(3))) short lds_i16;
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-
-// 16 bytes of a row at element p, the first n (of 16 / sizeof(T)) elements;
-// the rest 0.
-template <typename T>
-__device__ __forceinline__ uint4 load16(const T* p, int n) {
-  constexpr int V = 16 / sizeof(T);
-  if (n >= V) {
-    const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p);
-    return make_uint4(v[0], v[1], v[2], v[3]);
-  }
-  uint32_t w[4] = {0, 0, 0, 0};
-  int z = 0;   // as in load8
-  asm volatile("" : "+v"(z));
-  p += z;
-#pragma unroll
-  for (int i = 0; i < V - 1; ++i)
-    if (i < n) {
-      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
-      else w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
-    }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 // One operand's 64 rows x 128 bytes of K in LDS, as it lies in memory: along,
 // 64 rows of 128 bytes; across, BK rows (of k) of 64 elements.  Padding
@@ -155,7 +134,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(Product p, Epilogue e, 
     if (part) {
       if (r < p.M && c < p.N) store8<float>(part + ((int64_t)blockIdx.y * p.M + r) * np + c, v, 8);
     } else {
-      epilogue8<T, 16, 32>(e, p.M, p.N, r, c, v);
+      epilogue8<T, LANES_APART>(e, p.M, p.N, r, c, v, epilogue_bias(e, p.N, c), epilogue_res<T>(e, p.M, p.N, r, c));
     }
   }
 }
@@ -176,7 +155,7 @@ __global__ __launch_bounds__(256) void linear_reduce_kernel(const float* __restr
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += x.get(i);
     }
-  epilogue8<T, 1, 2>(e, M, N, r, c, v);
+  epilogue8<T, LANES_NEXT>(e, M, N, r, c, v, epilogue_bias(e, N, c), epilogue_res<T>(e, M, N, r, c));
 }
 
 // dz = round(dout * act'(z)) (when dz is given: [m, ldz8], columns past n are
@@ -207,8 +186,9 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dou
       if (act != ACT_NONE) {
         float x[8];
         saved_load8<T>(z, ldz, codes, scales, r, c, n, nv, x);
+        act_slope8<T>(act, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = j < nv ? g[j] * act_slope<T>(act, x[j]) : 0.f;
+        for (int j = 0; j < 8; ++j) g[j] = j < nv ? g[j] * x[j] : 0.f;
       }
       if (dz) store8<T>(dz + r * ld8 + c, g, 8);
 #pragma unroll
@@ -230,47 +210,50 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dou
 
 int pad8(int n) { return (n + 7) / 8 * 8; }
 
-// K slices of the 64 x 64 tiles: enough workgroups for two per CU, at least
-// four K blocks each, and partial sums of at most 64 MB.
-int any_slices(int dtype, int M, int N, int K) {
-  if (M == 0 || N == 0) return 1;
-  const int64_t tiles = cdiv64(M, 64) * cdiv64(N, 64);
-  const int bk = dtype == 0 ? 32 : 64;
-  int64_t s = std::min<int64_t>({cdiv64(512, tiles), cdiv64(K, 4 * bk), 32});
-  while (s > 1 && s * M * pad8(N) * 4 > ((int64_t)64 << 20)) --s;
-  if (s <= 1) return 1;
-  const int64_t kper = cdiv64(cdiv64(K, s), bk) * bk;
-  return (int)cdiv64(K, kper);
-}
-
-size_t product_ws_bytes(int dtype, int M, int N, int K) {
-  const int s = any_slices(dtype, M, N, K);
-  return s > 1 ? (size_t)s * M * pad8(N) * 4 : 0;
-}
-
 template <typename T>
-void run_any(const Product& p, const Epilogue& e, int slices, float* part, hipStream_t s) {
-  const int bk = 128 / sizeof(T);
-  const int kper = (int)(cdiv64(cdiv64(p.K, slices), bk) * bk), np = pad8(p.N);
-  const dim3 grid((unsigned)(cdiv64(p.N, 64) * cdiv64(p.M, 64)), (unsigned)slices);
-  float* dst = slices > 1 ? part : nullptr;
+void run_any(const Product& p, const Epilogue& e, const ProductPlan& plan, float* part, int np,
+             hipStream_t s) {
+  const dim3 grid((unsigned)(cdiv64(p.N, 64) * cdiv64(p.M, 64)), (unsigned)plan.slices);
   if (p.a_along && p.b_along)
-    launch_k(linear_any_kernel<T, true, true>, grid, 256, 0, s, p, e, kper, dst, np);
+    launch_k(linear_any_kernel<T, true, true>, grid, 256, 0, s, p, e, plan.per, part, np);
   else if (p.a_along)
-    launch_k(linear_any_kernel<T, true, false>, grid, 256, 0, s, p, e, kper, dst, np);
+    launch_k(linear_any_kernel<T, true, false>, grid, 256, 0, s, p, e, plan.per, part, np);
   else
-    launch_k(linear_any_kernel<T, false, false>, grid, 256, 0, s, p, e, kper, dst, np);
-  if (slices > 1) {
-    const int64_t chunks = (int64_t)p.M * ((p.N + 31) / 32 * 4);
-    launch_k(linear_reduce_kernel<T>, (unsigned)cdiv64(chunks, 256), 256, 0, s, (const float*)part,
-             slices, p.M, p.N, np, e);
-  }
+    launch_k(linear_any_kernel<T, false, false>, grid, 256, 0, s, p, e, plan.per, part, np);
+}
+
+size_t product_ws_bytes(int dtype, bool a_along, int M, int N, int K) {
+  return product_ws(dtype == 1, a_along, M, N, K, compute_units());
 }
 
 hipError_t run_product(int dtype, const Product& p, const Epilogue& e, void* ws, hipStream_t s) {
-  const int slices = any_slices(dtype, p.M, p.N, p.K);
-  if (dtype == 0) run_any<float>(p, e, slices, (float*)ws, s);
-  else run_any<bf16_t>(p, e, slices, (float*)ws, s);
+  const int cus = compute_units(), np = pad8(p.N);
+  const bool ok = tile_operand((uintptr_t)p.A, p.lda, p.a_padded ? 0 : p.a_along ? p.K : p.M) &&
+                  tile_operand((uintptr_t)p.B, p.ldb, p.b_along ? p.K : p.N);
+  // (the few-token kernel has no checkpoints: a block's columns lie in many waves)
+  if (p.a_along && p.b_along && p.M <= kFewTokens && !e.z_codes && !e.out_codes) {
+    launch_few(dtype, p, e, cus, s);
+    return hipGetLastError();
+  }
+  const ProductPlan plan = product_plan(dtype == 1, ok, p.a_along, p.M, p.N, p.K, cus);
+  float* part = plan.slices > 1 ? (float*)ws : nullptr;
+  if (plan.height) {
+    const TileGrid g{(int)cdiv64(p.M, plan.height), (int)cdiv64(p.N, 256), plan.slices, plan.per, part, np};
+    (p.a_along ? p.b_along ? launch_tile_forward : launch_tile_da : launch_tile_dw)(
+        p, e, g, plan.height / 32, cus, s);
+  } else if (dtype == 0) {
+    run_any<float>(p, e, plan, part, np, s);
+  } else {
+    run_any<bf16_t>(p, e, plan, part, np, s);
+  }
+  if (part) {
+    const int64_t chunks = (int64_t)p.M * ((p.N + 31) / 32 * 4);
+    const unsigned grid = (unsigned)cdiv64(chunks, 256);
+    if (dtype == 0)
+      launch_k(linear_reduce_kernel<float>, grid, 256, 0, s, (const float*)part, plan.slices, p.M, p.N, np, e);
+    else
+      launch_k(linear_reduce_kernel<bf16_t>, grid, 256, 0, s, (const float*)part, plan.slices, p.M, p.N, np, e);
+  }
   return hipGetLastError();
 }
 
@@ -286,13 +269,13 @@ struct BackSpace {
     part = dz + (act == ACT_NONE ? 0 : up256((size_t)m * pad8(n) * es));
     a = part + up256((size_t)cdiv64(m, 64) * n * 4);
     prod = a + up256((size_t)m * pad8(k) * es);
-    bytes = prod + up256(std::max(product_ws_bytes(dtype, m, k, n), product_ws_bytes(dtype, n, k, m)));
+    bytes = prod + up256(std::max(product_ws_bytes(dtype, true, m, k, n), product_ws_bytes(dtype, false, n, k, m)));
   }
 };
 
 }  // namespace
 
-size_t linear_ws_bytes(int dtype, int m, int n, int k) { return up256(product_ws_bytes(dtype, m, n, k)); }
+size_t linear_ws_bytes(int dtype, int m, int n, int k) { return up256(product_ws_bytes(dtype, true, m, n, k)); }
 
 size_t linear_backward_ws_bytes(int dtype, int act, int m, int n, int k) {
   return BackSpace(dtype, act, m, n, k).bytes;
@@ -300,7 +283,7 @@ size_t linear_backward_ws_bytes(int dtype, int act, int m, int n, int k) {
 
 hipError_t launch_linear(int dtype, int m, int n, int k, const void* a, int64_t lda, const void* w,
                          int64_t ldw, const LinearOut& o, void* ws, hipStream_t s) {
-  const Product p{a, lda, true, w, ldw, true, m, n, k};
+  const Product p{a, lda, true, false, w, ldw, true, m, n, k};
   const Epilogue e{o.bias, o.res, o.ldr, o.out, o.ldo, o.z, o.ldz, o.z_codes, o.z_scales,
                    o.out_codes, o.out_scales, o.act};
   return run_product(dtype, p, e, ws, s);
@@ -311,6 +294,7 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
   char* base = static_cast<char*>(ws);
   const void* dz = b.dout;
   int64_t lddz = b.ldo;
+  bool padded = false;
   float* part = b.dbias ? (float*)(base + sp.part) : nullptr;
   const bool need_dz = b.act != ACT_NONE && (b.da || b.dw);
   if (b.m == 0) {
@@ -331,7 +315,7 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
                (const bf16_t*)b.z, b.ldz, b.z_codes, b.z_scales, (bf16_t*)dst, ld8, part);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    if (need_dz) dz = dst, lddz = ld8;
+    if (need_dz) dz = dst, lddz = ld8, padded = true;
     if (part) {
       err = launch_colsum(part, (int)cdiv64(b.m, 64), b.n, b.dbias, nullptr, s);
       if (err != hipSuccess) return err;
@@ -342,7 +326,7 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
     e.out = b.da;
     e.ldo = b.ldda;
     const hipError_t err =
-        run_product(dtype, Product{dz, lddz, true, b.w, b.ldw, false, b.m, b.k, b.n}, e, base + sp.prod, s);
+        run_product(dtype, Product{dz, lddz, true, padded, b.w, b.ldw, false, b.m, b.k, b.n}, e, base + sp.prod, s);
     if (err != hipSuccess) return err;
   }
   if (b.dw) {
@@ -357,7 +341,7 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
     }
     e.out = b.dw;
     e.ldo = b.lddw;
-    return run_product(dtype, Product{dz, lddz, false, a, lda, false, b.n, b.k, b.m}, e, base + sp.prod, s);
+    return run_product(dtype, Product{dz, lddz, false, padded, a, lda, false, b.n, b.k, b.m}, e, base + sp.prod, s);
   }
   return hipSuccess;
 }

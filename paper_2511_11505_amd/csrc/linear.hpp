@@ -9,11 +9,12 @@ namespace fs {
 
 // out[i, j] = sum over k of A(i, k) B(j, k), i < M, j < N.  An operand is
 // "along" when k runs along its rows (element (i, k) at i * ld + k), else
-// "across" (at k * ld + i).
+// "across" (at k * ld + i).  a_padded: A's rows go on to a multiple of 8
+// elements, with zeros.
 struct Product {
   const void* A;
   int64_t lda;
-  bool a_along;
+  bool a_along, a_padded;
   const void* B;
   int64_t ldb;
   bool b_along;
@@ -34,6 +35,26 @@ struct Epilogue {
   int act;
 };
 
+// The large tiles' grid (linear_tile.hpp).
+struct TileGrid {
+  int tiles_m, tiles_n, slices;
+  int kb_per;      // K blocks per slice (the last may have fewer, but 4)
+  float* part;     // more than one slice: fp32 sums [slice][M][np]
+  int np;
+};
+// tm: tile height in units of 32 rows, 4, 6, 7 or 8 (dw: not 7); cus: compute
+// units to fill.
+void launch_tile_forward(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
+                         hipStream_t s);
+void launch_tile_da(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
+                    hipStream_t s);
+void launch_tile_dw(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
+                    hipStream_t s);
+
+// Forward products of up to kFewTokens rows (linear_few.hip).
+constexpr int kFewTokens = 8;
+void launch_few(int dtype, const Product& p, const Epilogue& e, int cus, hipStream_t s);
+
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
 namespace {
@@ -45,66 +66,120 @@ __device__ __forceinline__ float logistic(float z) {
   if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
   else return 1.0f / (1.0f + expf(-z));
 }
-// Phi(z), by erfc: 1 + erf(z / sqrt 2) would cancel for z far below 0
-__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(z * -0.70710678118654752f); }
-
+// Phi(z) and exp(-z^2 / 2).  By erfc, since 1 + erf(z / sqrt 2) would cancel
+// for z far below 0.  For bf16 results erfc(x) = t Q(t) exp(-x^2), t = 1 / (1 +
+// 0.4 x), with Q of degree 7 fitted here to exp(x^2) erfc(x) / t over 0 <= x
+// <= 10 for the least relative error, 4.3e-7 (reweighted least squares at
+// Chebyshev points); the library's erfcf took 58 us of a 4096 x 5632 backward
+// pass's act' against 23 us of memory.
 template <typename T>
-__device__ __forceinline__ float act_value(int act, float z) {
-  switch (act) {
-    case ACT_RELU: return z < 0.f ? 0.f : z;
-    case ACT_GELU: return z * normal_cdf(z);
-    case ACT_SILU: return z * logistic<T>(z);
-    default: return z;
+__device__ __forceinline__ float normal_cdf(float z, float& gauss) {
+  if constexpr (sizeof(T) == 2) {
+    gauss = __expf(-0.5f * z * z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.4f * 0.70710678118654752f, fabsf(z), 1.0f));
+    float q = 0.051215760409832f;
+    q = fmaf(q, t, -0.2920388877391815f);
+    q = fmaf(q, t, 0.49442407488822937f);
+    q = fmaf(q, t, -0.18401390314102173f);
+    q = fmaf(q, t, 0.2983193099498749f);
+    q = fmaf(q, t, 0.1769629865884781f);
+    q = fmaf(q, t, 0.22967028617858887f);
+    q = fmaf(q, t, 0.22545994818210602f);
+    q *= 0.5f * t * gauss;
+    return z > 0.f ? 1.0f - q : q;
+  } else {
+    gauss = expf(-0.5f * z * z);
+    return 0.5f * erfcf(z * -0.70710678118654752f);
+  }
+}
+
+// act and act' of 8 values; the choice is made once, outside the loops (inside,
+// every element takes the branches: 18 us more for each 224 x 256 tile).
+template <typename T>
+__device__ __forceinline__ void act8(int act, float (&v)[8]) {
+  float gauss;
+  if (act == ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+  } else if (act == ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= normal_cdf<T>(v[i], gauss);
+  } else if (act == ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= logistic<T>(v[i]);
   }
 }
 template <typename T>
-__device__ __forceinline__ float act_slope(int act, float z) {
-  switch (act) {
-    case ACT_RELU: return z > 0.f ? 1.f : 0.f;
-    case ACT_GELU: return normal_cdf(z) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
-    case ACT_SILU: {
-      const float g = logistic<T>(z);
-      return g * (1.f + z * (1.f - g));
+__device__ __forceinline__ void act_slope8(int act, float (&v)[8]) {
+  if (act == ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] > 0.f ? 1.f : 0.f;
+  } else if (act == ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float gauss;
+      const float cdf = normal_cdf<T>(v[i], gauss);
+      v[i] = fmaf(v[i] * 0.39894228040143268f, gauss, cdf);
     }
-    default: return 1.f;
+  } else if (act == ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float g = logistic<T>(v[i]);
+      v[i] = g * (1.f + v[i] * (1.f - g));
+    }
   }
+}
+
+// What the epilogue of 8 columns reads: the bias, and the residual of a row.
+// Loaded apart from epilogue8, so that a kernel with many of them can ask for
+// all early: a load behind a store waits for the store to finish.
+__device__ __forceinline__ Raw8<float> epilogue_bias(const Epilogue& e, int N, int c) {
+  Raw8<float> b = {};
+  if (e.bias && c < N) b = load8<float>(e.bias + c, min(8, N - c));
+  return b;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> epilogue_res(const Epilogue& e, int M, int N, int64_t r, int c) {
+  Raw8<T> a = {};
+  if (e.res && r < M && c < N) a = load8<T>((const T*)e.res + r * e.ldr + c, min(8, N - c));
+  return a;
 }
 
 // The epilogue of 8 columns, from c (c % 8 == 0), of row r.  Every lane of
-// the wave calls it together (the checkpoints' exchange between the lanes that
-// differ in bits X1 and X2); rows and columns past the end are not stored.
-template <typename T, int X1, int X2>
-__device__ __forceinline__ void epilogue8(const Epilogue& e, int M, int N, int64_t r, int c,
-                                          float (&v)[8]) {
+// the wave calls it together (the checkpoints' exchange between the lanes of a
+// block); rows and columns past the end are not stored.  The blocks' scale
+// bytes are returned (z's in bits 0 .. 7, out's in bits 8 .. 15), and written
+// unless the caller does.
+template <typename T, int LANES, bool SCALE = true>
+__device__ __forceinline__ uint32_t epilogue8(const Epilogue& e, int M, int N, int64_t r, int c,
+                                              float (&v)[8], const Raw8<float>& bias,
+                                              const Raw8<T>& res) {
   const int n = min(8, N - c);
   const bool live = r < M && n > 0;
-  if (e.bias && n > 0) {
-    const Raw8<float> b = load8<float>(e.bias + c, n);
+  uint32_t bytes = 0;
+  if (e.bias) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += b.get(i);
+    for (int i = 0; i < 8; ++i) v[i] += bias.get(i);
   }
   if (e.z && live) store8<T>((T*)e.z + r * e.ldz + c, v, n);
   if (e.z_codes) {
     float q[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[i] = i < n ? rounded<T>(v[i]) : 0.f;
-    ckpt_store8<X1, X2>(e.z_codes, e.z_scales, r, c, N, q, n, live);
+    bytes = ckpt_store8<LANES, SCALE>(e.z_codes, e.z_scales, r, c, N, q, n, live);
   }
-  if (e.act != ACT_NONE) {
+  act8<T>(e.act, v);
+  if (e.res) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = act_value<T>(e.act, v[i]);
-  }
-  if (e.res && live) {
-    const Raw8<T> a = load8<T>((const T*)e.res + r * e.ldr + c, n);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += a.get(i);
+    for (int i = 0; i < 8; ++i) v[i] += res.get(i);
   }
   if (live) store8<T>((T*)e.out + r * e.ldo + c, v, n);
   if (e.out_codes) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < n ? rounded<T>(v[i]) : 0.f;
-    ckpt_store8<X1, X2>(e.out_codes, e.out_scales, r, c, N, v, n, live);
+    bytes |= ckpt_store8<LANES, SCALE>(e.out_codes, e.out_scales, r, c, N, v, n, live) << 8;
   }
+  return bytes;
 }
 
 // Two 16 x 16 accumulators of neighbouring column fragments (the weights are

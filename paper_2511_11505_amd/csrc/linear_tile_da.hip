@@ -1,0 +1,14 @@
+// Input gradients on the large tiles: dz along K, the weight across it.
+#include "linear_tile.hpp"
+
+namespace fs {
+void launch_tile_da(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
+                    hipStream_t s) {
+  switch (tm) {
+    case 4: run_tile<true, false, 4, false>(p, e, g, cus, s); break;
+    case 6: run_tile<true, false, 6, false>(p, e, g, cus, s); break;
+    case 7: run_tile<true, false, 7, false>(p, e, g, cus, s); break;
+    default: run_tile<true, false, 8, false>(p, e, g, cus, s);
+  }
+}
+}  // namespace fs

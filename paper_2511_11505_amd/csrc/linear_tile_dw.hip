@@ -1,0 +1,13 @@
+// Weight gradients on the large tiles: both operands across K (the tokens).
+#include "linear_tile.hpp"
+
+namespace fs {
+void launch_tile_dw(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
+                    hipStream_t s) {
+  switch (tm) {
+    case 4: run_tile<false, false, 4, false>(p, e, g, cus, s); break;
+    case 6: run_tile<false, false, 6, false>(p, e, g, cus, s); break;
+    default: run_tile<false, false, 8, false>(p, e, g, cus, s);
+  }
+}
+}  // namespace fs

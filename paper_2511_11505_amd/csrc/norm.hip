@@ -79,7 +79,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_kernel(NormArgs a) {
   for (int j = 0; j < NC; ++j) {
     const int c = (j * TPR + tid) * 8, n = min(8, a.cols - c);
     if (a.sum && n > 0) store8<T>((T*)a.sum + r * a.ldsum + c, v[j], n);
-    if (a.in_codes) ckpt_store8<1, 2>(a.in_codes, a.in_scales, r, c, a.cols, v[j], n, true);
+    if (a.in_codes) ckpt_store8<LANES_NEXT>(a.in_codes, a.in_scales, r, c, a.cols, v[j], n, true);
     float y[8] = {};
     if (n > 0) {
       Raw8<float> g = {}, b = {};
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_kernel(NormArgs a) {
       }
       store8<T>((T*)a.y + r * a.ldy + c, y, n);
     }
-    if (a.y_codes) ckpt_store8<1, 2>(a.y_codes, a.y_scales, r, c, a.cols, y, n, true);
+    if (a.y_codes) ckpt_store8<LANES_NEXT>(a.y_codes, a.y_scales, r, c, a.cols, y, n, true);
   }
 }
 

@@ -65,6 +65,28 @@ __device__ __forceinline__ Raw8<T> load8(const T* p, int n) {
   return r;
 }
 
+// 16 bytes of a row at element p, the first n (of 16 / sizeof(T)) elements;
+// the rest 0.
+template <typename T>
+__device__ __forceinline__ uint4 load16(const T* p, int n) {
+  constexpr int V = 16 / sizeof(T);
+  if (n >= V) {
+    const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p);
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  }
+  uint32_t w[4] = {0, 0, 0, 0};
+  int z = 0;   // as in load8
+  asm volatile("" : "+v"(z));
+  p += z;
+#pragma unroll
+  for (int i = 0; i < V - 1; ++i)
+    if (i < n) {
+      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
+      else w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float (&v)[8], int n) {
   if (n >= 8) {
@@ -99,8 +121,7 @@ __device__ __forceinline__ uint32_t amax8(const float (&v)[8]) {
 }
 // Codes of 8 values under scale byte b.
 __device__ __forceinline__ uint2 ckpt_codes(const float (&v)[8], int b) {
-  if (b == 255) return make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
-  const float inv = __uint_as_float((uint32_t)(254 - b) << 23);
+  const float inv = __uint_as_float((uint32_t)(254 - min(b, 254)) << 23);
   float q[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) q[i] = v[i] * inv;
@@ -113,7 +134,8 @@ __device__ __forceinline__ uint2 ckpt_codes(const float (&v)[8], int b) {
   w0 = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w0, true);
   w1 = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], w1, false);
   w1 = __builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], w1, true);
-  return make_uint2((uint32_t)w0, (uint32_t)w1);
+  const bool nan = b == 255;
+  return make_uint2(nan ? 0x7F7F7F7Fu : (uint32_t)w0, nan ? 0x7F7F7F7Fu : (uint32_t)w1);
 }
 __device__ __forceinline__ void store_codes(uint8_t* p, uint2 c, int n) {
   if (n >= 8) {
@@ -148,21 +170,37 @@ __device__ __forceinline__ void ckpt_values(uint2 c, int b, float (&v)[8]) {
   v[4] = a2[0] * s, v[5] = a2[1] * s, v[6] = a3[0] * s, v[7] = a3[1] * s;
 }
 
+// Largest of m over the four lanes that hold a block: neighbours (lane bits 0
+// and 1), or the lanes of the four 16-lane groups (bits 4 and 5; the swap of a
+// register with itself leaves both groups' values in its two results).
+enum { LANES_NEXT = 0, LANES_APART = 1 };
+template <int LANES>
+__device__ __forceinline__ uint32_t block_max(uint32_t m) {
+  if constexpr (LANES == LANES_NEXT) {
+    m = max(m, (uint32_t)dpp_i<kDppXor1>((int)m));
+    return max(m, (uint32_t)dpp_i<kDppXor2>((int)m));
+  } else {
+    const auto a = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    m = max(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return max(b[0], b[1]);
+  }
+}
+
 // Write 8 values (already rounded to the stored type; those past n are 0) of
-// row r from column c, c % 8 == 0, into a checkpoint of `cols` columns.  The
-// four lanes that hold a block's 32 columns differ in the lane bits X1 and
-// X2; every lane of the wave calls this, `live` where its row exists.
-template <int X1, int X2>
-__device__ __forceinline__ void ckpt_store8(uint8_t* codes, uint8_t* scales, int64_t r, int c,
-                                            int cols, const float (&v)[8], int n, bool live) {
-  uint32_t m = amax8(v);
-  m = max(m, (uint32_t)__shfl_xor((int)m, X1));
-  m = max(m, (uint32_t)__shfl_xor((int)m, X2));
-  const int b = ckpt_byte(m);
-  if (!live || n <= 0) return;
-  store_codes(codes + r * cols + c, ckpt_codes(v, b), n);
-  if (c % kCkptBlock == 0)
-    scales[r * ((cols + kCkptBlock - 1) / kCkptBlock) + c / kCkptBlock] = (uint8_t)b;
+// row r from column c, c % 8 == 0, into a checkpoint of `cols` columns; the
+// block's scale byte is returned, and written unless the caller does.  Every
+// lane of the wave calls this, `live` where its row exists.
+template <int LANES, bool SCALE = true>
+__device__ __forceinline__ int ckpt_store8(uint8_t* codes, uint8_t* scales, int64_t r, int c, int cols,
+                                           const float (&v)[8], int n, bool live) {
+  const int b = ckpt_byte(block_max<LANES>(amax8(v)));
+  if (live && n > 0) {
+    store_codes(codes + r * cols + c, ckpt_codes(v, b), n);
+    if (SCALE && c % kCkptBlock == 0)
+      scales[r * ((cols + kCkptBlock - 1) / kCkptBlock) + c / kCkptBlock] = (uint8_t)b;
+  }
+  return b;
 }
 
 // 8 values of a saved activation, row r, columns c .. c + n - 1.

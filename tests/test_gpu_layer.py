@@ -123,6 +123,22 @@ def test_linear(m, n, k, dtype):
     check_linear(m, n, k, dtype, "none", False, False, 0)
 
 
+# sizes that fill the large tiles: whole tiles, ragged rows and columns, K that
+# ends inside a block, the least K, one and several tiles per workgroup
+LARGE = [(4096, 2048, 256, 0), (3000, 2600, 328, 8), (6100, 1992, 200, 0), (2047, 4104, 520, 0),
+         (9000, 2900, 264, 0)]
+
+
+@pytest.mark.parametrize("m,n,k,pad", LARGE)
+def test_linear_large(m, n, k, pad):
+    check_linear(m, n, k, "bf16", "none", False, False, pad, save=False)
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_linear_large_epilogue(act):
+    check_linear(2500, 2824, 264, "bf16", act, True, True, 8)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
 @pytest.mark.parametrize("m,n,k,pad", [(33, 70, 45, 0), (33, 70, 45, 3), (96, 128, 192, 8), (2, 40, 2048, 0)])
@@ -210,6 +226,14 @@ def check_backward(m, n, k, dtype, act, pad, coded, seed=0, lead=0):
 @pytest.mark.parametrize("m,n,k", SIZES)
 def test_linear_backward(m, n, k, dtype):
     check_backward(m, n, k, dtype, "none", 0, False)
+
+
+@pytest.mark.parametrize("m,n,k,act,pad,coded", [
+    (4096, 1024, 2048, "none", 0, False), (3000, 2600, 2504, "silu", 8, True),
+    (2047, 1999, 4104, "gelu", 0, False), (300, 4104, 3000, "relu", 0, True), (5000, 200, 6104, "none", 0, True),
+    (6100, 3001, 1992, "silu", 0, True)])
+def test_linear_backward_large(m, n, k, act, pad, coded):
+    check_backward(m, n, k, "bf16", act, pad, coded)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
