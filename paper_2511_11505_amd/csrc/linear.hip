@@ -112,17 +112,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(Product p, Epilogue e, 
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          if constexpr (sizeof(T) == 2) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, fb[j]), __builtin_bit_cast(bf16x8, fa[i]), acc[i][j], 0, 0, 0);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                  __uint_as_float((&fb[j].x)[k]), __uint_as_float((&fa[i].x)[k]), acc[i][j], 0, 0, 0);
-          }
-        }
+        for (int j = 0; j < 2; ++j) acc[i][j] = mma16<T>(fb[j], fa[i], acc[i][j]);
     }
   }
 #pragma unroll
@@ -222,8 +212,8 @@ void run_any(const Product& p, const Epilogue& e, const ProductPlan& plan, float
     launch_k(linear_any_kernel<T, false, false>, grid, 256, 0, s, p, e, plan.per, part, np);
 }
 
-size_t product_ws_bytes(int dtype, bool a_along, int M, int N, int K) {
-  return product_ws(dtype == 1, a_along, M, N, K, compute_units());
+size_t product_ws_bytes(int dtype, bool a_along, bool b_along, int M, int N, int K) {
+  return product_ws(dtype == 1, a_along, b_along, M, N, K, compute_units());
 }
 
 hipError_t run_product(int dtype, const Product& p, const Epilogue& e, void* ws, hipStream_t s) {
@@ -235,12 +225,16 @@ hipError_t run_product(int dtype, const Product& p, const Epilogue& e, void* ws,
     launch_few(dtype, p, e, cus, s);
     return hipGetLastError();
   }
-  const ProductPlan plan = product_plan(dtype == 1, ok, p.a_along, p.M, p.N, p.K, cus);
+  const ProductPlan plan = product_plan(dtype == 1, ok, p.a_along, p.b_along, p.M, p.N, p.K, cus);
+  if (plan.mid && p.a_along && p.b_along) {
+    launch_mid(dtype, p, e, plan.mid, s);
+    return hipGetLastError();
+  }
   float* part = plan.slices > 1 ? (float*)ws : nullptr;
   if (plan.height) {
-    const TileGrid g{(int)cdiv64(p.M, plan.height), (int)cdiv64(p.N, 256), plan.slices, plan.per, part, np};
-    (p.a_along ? p.b_along ? launch_tile_forward : launch_tile_da : launch_tile_dw)(
-        p, e, g, plan.height / 32, cus, s);
+    const TileGrid g{(int)cdiv64(p.M, plan.height), (int)cdiv64(p.N, plan.width), plan.slices, plan.per, part, np};
+    TileLaunch* run = p.a_along ? p.b_along ? launch_tile_forward : launch_tile_da : launch_tile_dw;
+    run(p, e, g, plan.height / 32, cus, s);
   } else if (dtype == 0) {
     run_any<float>(p, e, plan, part, np, s);
   } else {
@@ -269,13 +263,13 @@ struct BackSpace {
     part = dz + (act == ACT_NONE ? 0 : up256((size_t)m * pad8(n) * es));
     a = part + up256((size_t)cdiv64(m, 64) * n * 4);
     prod = a + up256((size_t)m * pad8(k) * es);
-    bytes = prod + up256(std::max(product_ws_bytes(dtype, true, m, k, n), product_ws_bytes(dtype, false, n, k, m)));
+    bytes = prod + up256(std::max(product_ws_bytes(dtype, true, false, m, k, n), product_ws_bytes(dtype, false, false, n, k, m)));
   }
 };
 
 }  // namespace
 
-size_t linear_ws_bytes(int dtype, int m, int n, int k) { return up256(product_ws_bytes(dtype, true, m, n, k)); }
+size_t linear_ws_bytes(int dtype, int m, int n, int k) { return up256(product_ws_bytes(dtype, true, true, m, n, k)); }
 
 size_t linear_backward_ws_bytes(int dtype, int act, int m, int n, int k) {
   return BackSpace(dtype, act, m, n, k).bytes;

@@ -42,18 +42,19 @@ struct TileGrid {
   float* part;     // more than one slice: fp32 sums [slice][M][np]
   int np;
 };
-// tm: tile height in units of 32 rows, 4, 6, 7 or 8 (dw: not 7); cus: compute
-// units to fill.
-void launch_tile_forward(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
-                         hipStream_t s);
-void launch_tile_da(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
-                    hipStream_t s);
-void launch_tile_dw(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
-                    hipStream_t s);
+// tm: tile height in units of 32 rows, 2 (of 128 columns), 4, 6, 7 or 8 (of 256;
+// dw: not 7); cus: compute units to fill.
+typedef void TileLaunch(const Product& p, const Epilogue& e, const TileGrid& g, int tm, int cus,
+                        hipStream_t s);
+TileLaunch launch_tile_forward, launch_tile_da, launch_tile_dw;
 
 // Forward products of up to kFewTokens rows (linear_few.hip).
 constexpr int kFewTokens = 8;
 void launch_few(int dtype, const Product& p, const Epilogue& e, int cus, hipStream_t s);
+
+// Forward products on tiles whose waves split K (linear_mid.hip); shape: a
+// MidShape of linear_rules.hpp.
+void launch_mid(int dtype, const Product& p, const Epilogue& e, int shape, hipStream_t s);
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
@@ -180,6 +181,21 @@ __device__ __forceinline__ uint32_t epilogue8(const Epilogue& e, int M, int N, i
     bytes |= ckpt_store8<LANES, SCALE>(e.out_codes, e.out_scales, r, c, N, v, n, live) << 8;
   }
   return bytes;
+}
+
+// One step of K on 16 x 16 outputs: 16 bytes per lane and operand, that is 32 of K
+// for bf16, 16 for fp32.
+template <typename T>
+__device__ __forceinline__ floatx4 mma16(const uint4& b, const uint4& a, floatx4 c) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b),
+                                                   __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+  } else {
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.x), __uint_as_float(a.x), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.y), __uint_as_float(a.y), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.z), __uint_as_float(a.z), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.w), __uint_as_float(a.w), c, 0, 0, 0);
+  }
 }
 
 // Two 16 x 16 accumulators of neighbouring column fragments (the weights are

@@ -11,70 +11,116 @@ namespace {
 
 inline int64_t cdiv_(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How a product runs: height 0: the 64 x 64 tiles; else the large tiles of
-// `height` rows x 256.  K is cut into `slices` of `per` K blocks of 64 (large
-// tiles) or elements (64 x 64).
+// Tiles of the kernel whose waves split K (forward only): tokens x outputs,
+// waves.
+enum MidShape { MID_NONE, MID_16 /* 16 x 32, 8 */, MID_32 /* 32 x 32, 8 */, MID_64 /* 64 x 32, 8 */, MID_SHAPES };
+
+// How a product runs: height > 0: tiles of `height` x `width` (linear_tile.hpp);
+// else mid != MID_NONE: the kernel whose waves split K; else the 64 x 64 tiles.
+// K is cut into `slices` of `per` K blocks of 64 (linear_tile.hpp; each at least
+// 4, which its copies run ahead) or elements (64 x 64).
 struct ProductPlan {
-  int height, slices, per;
+  int height, width, slices, per, mid;
 };
 
-// What the large tiles ask of an operand: 16-byte chunks that lie whole in
+// What linear_tile.hpp asks of an operand: 16-byte chunks that lie whole in
 // their row (along: K % 8 == 0; across: its width % 8 == 0), from an aligned
 // base and stride, a tile's rows within 32-bit offsets.
 inline bool tile_operand(uintptr_t base, int64_t ld, int64_t row_elems) {
   return base % 16 == 0 && ld % 8 == 0 && row_elems % 8 == 0 && ld <= (1 << 22);
 }
 
-// Relative time of the large tiles of h rows: rounds over the CUs, half of a
-// part-filled one counted (its workgroups run faster, the chip being bound by
-// power), each its rows and a fixed part worth about 53.  Ranks the measured
-// times of every height (us at 128, 160, 192, 224, 256 rows): 8192 x 8192 outputs,
-// K 5120, 528, 518, 500, 484, 463; 8192 x 5120, K 8192, 564, 557, 510, 466, 506;
-// 4096 x 2048, K 5632, 73, 76, 82, 91, 104; 4096 x 5632, K 2048, 110, 134, 110,
-// 121, 139.
-inline int64_t tile_cost(int64_t M, int64_t N, int cus, int h) {
-  const int64_t tiles = cdiv_(M, h) * cdiv_(N, 256);
-  return (cdiv_(tiles, cus) * cus + tiles) * (h + 53);
+// Partial sums of a cut K: at most 64 MB.
+inline bool slices_fit(int64_t s, int64_t M, int64_t N) {
+  return s == 1 || s * M * (cdiv_(N, 8) * 8) * 4 <= ((int64_t)64 << 20);
+}
+// Time in us of adding s slices: a second launch, and the sums written and read.
+inline double slices_us(int64_t s, int64_t M, int64_t N) {
+  return s == 1 ? 0.0 : 4.5 + (double)s * M * N * 8 / 8e6;
 }
 
-// The heights that the products have: 128, 192, 224 (not where A lies across K:
-// whole panels of 64 rows) and 256 rows (not where K ends inside a block: the
-// copies' pointers leave no registers for it).
-inline int tile_height(int64_t M, int64_t N, int64_t K, int cus, bool a_along) {
-  int best = 192;
-  for (const int h : {256, 224, 128})
-    if ((a_along || h % 64 == 0) && (h < 256 || K % 64 == 0) &&
-        tile_cost(M, N, cus, h) < tile_cost(M, N, cus, best))
-      best = h;
-  return best;
+// The kernels' times in us, fitted to measurements on one MI355X; they only
+// have to rank.
+//
+// Large tiles of h x 256: rounds over the CUs, half of a part-filled one after
+// the first counted (its workgroups run faster, the chip being bound by power),
+// 0.0047 us per K block and row, and a fixed part worth 53 rows.  Measured (us
+// at 128, 192, 224, 256 rows): 8192 x 8192 outputs, K 5120, 528, 500, 484, 463;
+// 8192 x 5120, K 8192, 564, 510, 466, 506; 4096 x 2048, K 5632, 73, 82, 91, 104;
+// 4096 x 5632, K 2048, 110, 110, 121, 139; 2048 x 2048, K 2048, 32 at 128.
+inline double large_us(int64_t M, int64_t N, int64_t K, int cus, int h) {
+  const int64_t tiles = cdiv_(M, h) * cdiv_(N, 256), rounds = cdiv_(tiles, cus);
+  const double r = rounds == 1 ? 1.0 : 0.5 * (rounds + (double)tiles / cus);
+  return 4.0 + cdiv_(K, 64) * r * (h + 53) * 0.0047;
+}
+// 64 x 128 tiles: a K block 0.43 us while there is a workgroup per CU, 0.70 with
+// two.  Measured (us, by slices): 512 x 2048, K 2048, 17.4 (1), 17.9 (2), 20.3
+// (4); 128 x 4096, K 4096, 28 (1), 20.5 (2), 17.1 (4), 19.2 (8); 2048 x 2048, K
+// 2048, 24.7 (1), 37.8 (2); 64 x 7168, K 2048, 17.1 (1), 14.7 (2), 14.0 (4).  (128 x
+// 128 tiles were never better by more than 1 us.)
+inline double small_us(int64_t M, int64_t N, int64_t per, int64_t s, int cus) {
+  const int64_t wgs = cdiv_(M, 64) * cdiv_(N, 128) * s;
+  return 4.0 + per * (wgs <= cus ? 0.43 : 0.70 * cdiv_(wgs, 2 * cus)) + slices_us(s, M, N);
+}
+// Waves splitting K: a CU gets 35 KB/us from the L2, 2.5 times less from rows
+// that 16 bytes do not align, and multiplies fp32 at half an MFMA's rate.
+// Measured: 64 x 512, K 512, 4.3 us at 16 x 32, 4.8, 6.0 at 64 x 32; 64 x 7168, K
+// 2048, 25, 18.6, 15.0; 200 x 1000, K 2000, 11.7, 9.2, 12.2; 777 x 1001, K 1409
+// (unaligned) 90, 65, 55, and 22, 19 from K 1408.
+inline double mid_us(int64_t M, int64_t N, int64_t K, int es, bool aligned, int cus, int rows) {
+  const double wgs = (double)cdiv_(M, rows) * cdiv_(N, 32) / cus;
+  return 3.5 + std::max(wgs, 1.0) * (rows + 32) * K * es * (aligned ? 1.0 : 2.5) / 35e3;
+}
+// 64 x 64 tiles: a K block of 128 bytes 0.70 us (fp32 0.92), or 0.28 (0.70) per
+// workgroup of the CU.  Measured: 2048 x 2048, K 2048, 39 us; 777 x 1001, K 1409,
+// 22.2 (1 slice), 19.9 (2); fp32 512 x 1408, K 2048, 63 (1), 52 (2), 41 (4).
+inline double any_us(int64_t M, int64_t N, int64_t blocks, int64_t s, bool bf16, int cus) {
+  const double wgs = (double)cdiv_(M, 64) * cdiv_(N, 64) * s / cus;
+  return 4.0 + blocks * std::max(bf16 ? 0.70 : 0.92, (bf16 ? 0.28 : 0.70) * wgs) + slices_us(s, M, N);
 }
 
-inline ProductPlan product_plan(bool bf16, bool tiles_ok, bool a_along, int64_t M, int64_t N, int64_t K,
-                                int cus) {
-  if (M <= 0 || N <= 0) return {0, 1, 1 << 30};
-  const int64_t np = cdiv_(N, 8) * 8;
-  auto fits = [&](int64_t s) { return s * M * np * 4 <= ((int64_t)64 << 20); };   // partial sums
-  if (bf16 && tiles_ok && K > 192) {
-    const int h = tile_height(M, N, K, cus, a_along);
-    const int64_t tiles = cdiv_(M, h) * cdiv_(N, 256), blocks = cdiv_(K, 64);
-    if (tiles * 2 >= cus) return {h, 1, (int)blocks};
+// The plan of least time.  tiles_ok: the operands suit linear_tile.hpp.
+inline ProductPlan product_plan(bool bf16, bool tiles_ok, bool a_along, bool b_along, int64_t M,
+                                int64_t N, int64_t K, int cus) {
+  ProductPlan best{0, 0, 1, 1 << 30, MID_NONE};
+  if (M <= 0 || N <= 0) return best;
+  double us = 1e30;
+  auto take = [&](double t, ProductPlan p) {
+    if (t < us) us = t, best = p;
+  };
+  const int64_t blocks = cdiv_(K, 64);
+  if (bf16 && tiles_ok && blocks >= 4) {
+    // heights: 224 not where A lies across K (whole panels of 64 rows), 256 not
+    // where K ends inside a block (the copies' pointers leave no registers)
+    for (const int h : {128, 192, 224, 256})
+      if ((a_along || h % 64 == 0) && (h < 256 || K % 64 == 0))
+        take(large_us(M, N, K, cus, h), {h, 256, 1, (int)blocks, MID_NONE});
+    for (int64_t s = 1; s <= 16 && slices_fit(s, M, N); s *= 2) {
+      const int64_t per = cdiv_(blocks, s), n = cdiv_(blocks, per);
+      if (blocks - per * (n - 1) < 4) continue;
+      take(small_us(M, N, per, n, cus), {64, 128, (int)n, (int)per, MID_NONE});
+    }
   }
-  // 64 x 64 tiles: enough workgroups for two per CU, at least four K blocks
-  // each
-  const int64_t tiles = cdiv_(M, 64) * cdiv_(N, 64), bk = bf16 ? 64 : 32;
-  int64_t s = std::min<int64_t>({cdiv_(2 * cus, tiles), cdiv_(K, 4 * bk), 32});
-  while (s > 1 && !fits(s)) --s;
-  s = std::max<int64_t>(s, 1);
-  const int64_t per = std::max<int64_t>(cdiv_(cdiv_(K, s), bk) * bk, bk);
-  return {0, (int)std::max<int64_t>(1, cdiv_(K, per)), (int)per};
+  if (a_along && b_along) {
+    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 16), {0, 0, 1, 0, MID_16});
+    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 32), {0, 0, 1, 0, MID_32});
+    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 64), {0, 0, 1, 0, MID_64});
+  }
+  const int64_t bk = bf16 ? 64 : 32;
+  for (int64_t s = 1; s <= 32 && slices_fit(s, M, N); s *= 2) {
+    const int64_t per = std::max<int64_t>(cdiv_(cdiv_(K, s), bk) * bk, bk);
+    const int64_t n = std::max<int64_t>(1, cdiv_(K, per));
+    take(any_us(M, N, per / bk, n, bf16, cus), {0, 0, (int)n, (int)per, MID_NONE});
+  }
+  return best;
 }
 
 // Bytes of partial sums of the plan, whichever kernel the operands' alignment
 // leaves.
-inline size_t product_ws(bool bf16, bool a_along, int64_t M, int64_t N, int64_t K, int cus) {
+inline size_t product_ws(bool bf16, bool a_along, bool b_along, int64_t M, int64_t N, int64_t K, int cus) {
   size_t b = 0;
   for (const bool ok : {false, true}) {
-    const ProductPlan p = product_plan(bf16, ok, a_along, M, N, K, cus);
+    const ProductPlan p = product_plan(bf16, ok, a_along, b_along, M, N, K, cus);
     if (p.slices > 1) b = std::max(b, (size_t)p.slices * M * (cdiv_(N, 8) * 8) * 4);
   }
   return b;

@@ -11,6 +11,7 @@
 //             copies so that the reads cover every bank once: along, chunk c of
 //             row r sits at c ^ ((r / 2) % 8); across, the 32 bytes of columns
 //             16 c .. of row k sit at c ^ s(k), s = bits 1 and 3 of k.
+//             Products with few tiles take 64 x 128, two workgroups per CU, and K cut into slices whose sums a second kernel adds.
 //   Ring      Two 64-wide LDS slots for A, three for B (160 KB at 256
 //             rows); one barrier per block.  The copies run on from tile to tile.
 //   Tail      K % 64 != 0: chunks past K are copied from 16 zero bytes.
@@ -169,11 +170,12 @@ struct Reader {
   }
 };
 
-// out tile = A rows (tokens, 32 TM) x B rows (256).  FULL: the forward's
-// epilogue; else the sums are stored as they are.
-template <bool LA, bool LB, int TM, bool TAIL, bool FULL>
-__global__ __launch_bounds__(256, 1) void linear_tile_kernel(Product p, Epilogue e, TileGrid tg) {
-  constexpr int BM = 32 * TM, BN = 256, TN = 8;
+// out tile = 32 TM rows of A x 32 TN rows of B.  FULL: the forward's epilogue;
+// else the sums are stored as they are.
+template <bool LA, bool LB, int TM, int TN, bool TAIL, bool FULL>
+__global__ __launch_bounds__(256, TN == 8 ? 1 : 2) void linear_tile_kernel(Product p, Epilogue e,
+                                                                           TileGrid tg) {
+  constexpr int BM = 32 * TM, BN = 32 * TN;
   constexpr int ASLOT = BM * 128, BSLOT = BN * 128;
   constexpr int MPS = TM * TN, NR = TM + TN;
   static_assert(LA || TM % 2 == 0, "whole panels");
@@ -194,7 +196,7 @@ __global__ __launch_bounds__(256, 1) void linear_tile_kernel(Product p, Epilogue
   Reader<LA, 32> rdA;
   Reader<LB, 16> rdB;
   rdA.init(ring_lds, wm * 16);
-  rdB.init(ring_lds + 2 * ASLOT, wn * 128);
+  rdB.init(ring_lds + 2 * ASLOT, wn * 16 * TN);
 
   // items: XCD x takes the range [x per_xcd, (x + 1) per_xcd)
   const int total = tg.tiles_m * tg.tiles_n * tg.slices;
@@ -333,7 +335,7 @@ __global__ __launch_bounds__(256, 1) void linear_tile_kernel(Product p, Epilogue
     half(F[1], F[0], I1{}, I0{});
     half(F[0], F[1], I0{}, I1{});
     half(F[1], F[0], I1{}, I1{});
-    const int c0 = it.n0 + wn * 128 + col8(lane);
+    const int c0 = it.n0 + wn * 16 * TN + col8(lane);
     const int r0 = it.m0 + wm * 16 + (lane & 15);
     if constexpr (FULL) {
       // A loop over the fragment rows, each fetched from its accumulators by a
@@ -383,14 +385,15 @@ __global__ __launch_bounds__(256, 1) void linear_tile_kernel(Product p, Epilogue
         // z's, the second out's
         uint8_t* scales = lane < 16 ? e.z_scales : lane < 32 ? e.out_scales : nullptr;
         if (scales && r < p.M) {
+          constexpr int NB = TN / 2;
           const uint32_t bytes = lane < 16 ? zb : ob;
-          const int nb = (p.N + kCkptBlock - 1) / kCkptBlock, b0 = (it.n0 + wn * 128) / kCkptBlock;
+          const int nb = (p.N + kCkptBlock - 1) / kCkptBlock, b0 = (it.n0 + wn * 16 * TN) / kCkptBlock;
           uint8_t* q = scales + r * nb + b0;
-          if (b0 + 4 <= nb) {
-            memcpy(q, &bytes, 4);
+          if (b0 + NB <= nb) {
+            memcpy(q, &bytes, NB);
           } else {
 #pragma unroll
-            for (int j = 0; j < 3; ++j)
+            for (int j = 0; j < NB - 1; ++j)
               if (b0 + j < nb) q[j] = (uint8_t)(bytes >> (8 * j));
           }
         }
@@ -419,18 +422,18 @@ __global__ __launch_bounds__(256, 1) void linear_tile_kernel(Product p, Epilogue
   wait_vmcnt<0>();   // no copy outlives the workgroup's LDS
 }
 
-template <bool LA, bool LB, int TM, bool FULL>
+template <bool LA, bool LB, int TM, int TN, bool FULL>
 void run_tile(const Product& p, const Epilogue& e, const TileGrid& tg, int cus, hipStream_t s) {
   const int64_t items = (int64_t)tg.tiles_m * tg.tiles_n * tg.slices;
-  const int64_t want = cdiv64(items, kXcd), have = cus / kXcd;
+  const int64_t want = cdiv64(items, kXcd), have = (TN == 8 ? 1 : 2) * cus / kXcd;
   const unsigned grid = (unsigned)((want < have ? want : have) * kXcd);
-  if constexpr (TM < 8) {   // (tile_height: no 256 rows with a tail)
+  if constexpr (TM < 8) {   // (product_plan: no 256 rows with a tail)
     if (p.K % 64) {
-      launch_k(linear_tile_kernel<LA, LB, TM, true, FULL>, grid, 256, 0, s, p, e, tg);
+      launch_k(linear_tile_kernel<LA, LB, TM, TN, true, FULL>, grid, 256, 0, s, p, e, tg);
       return;
     }
   }
-  launch_k(linear_tile_kernel<LA, LB, TM, false, FULL>, grid, 256, 0, s, p, e, tg);
+  launch_k(linear_tile_kernel<LA, LB, TM, TN, false, FULL>, grid, 256, 0, s, p, e, tg);
 }
 
 }  // namespace

@@ -125,7 +125,8 @@ def test_linear(m, n, k, dtype):
 
 # sizes that fill the large tiles: whole tiles, ragged rows and columns, K that
 # ends inside a block, the least K, one and several tiles per workgroup
-LARGE = [(4096, 2048, 256, 0), (3000, 2600, 328, 8), (6100, 1992, 200, 0), (2047, 4104, 520, 0),
+# (and the 64 x 128 tiles: ragged edges, K in slices)
+LARGE = [(1000, 1992, 520, 0), (520, 2056, 2056, 8), (70, 4104, 4104, 0), (513, 1000, 1992, 0), (4096, 2048, 256, 0), (3000, 2600, 328, 8), (6100, 1992, 200, 0), (2047, 4104, 520, 0),
          (9000, 2900, 264, 0)]
 
 
@@ -230,6 +231,7 @@ def test_linear_backward(m, n, k, dtype):
 
 @pytest.mark.parametrize("m,n,k,act,pad,coded", [
     (4096, 1024, 2048, "none", 0, False), (3000, 2600, 2504, "silu", 8, True),
+    (600, 2056, 2504, "silu", 0, False), (130, 1999, 4104, "relu", 0, True), (2500, 264, 520, "none", 8, False),
     (2047, 1999, 4104, "gelu", 0, False), (300, 4104, 3000, "relu", 0, True), (5000, 200, 6104, "none", 0, True),
     (6100, 3001, 1992, "silu", 0, True)])
 def test_linear_backward_large(m, n, k, act, pad, coded):
