@@ -148,6 +148,27 @@ __global__ __launch_bounds__(256) void linear_reduce_kernel(const float* __restr
   epilogue8<T, LANES_NEXT>(e, M, N, r, c, v, epilogue_bias(e, N, c), epilogue_res<T>(e, M, N, r, c));
 }
 
+// Copies of up to two bf16 matrices with rows of whole 16-byte chunks, zeros
+// behind the last element.  A thread copies a chunk.
+struct PackArgs {
+  const bf16_t* src[2];
+  int64_t ld[2];
+  bf16_t* dst[2];
+  int rows[2], cols[2];
+};
+__global__ __launch_bounds__(256) void pack_rows_kernel(PackArgs a) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int ch = (a.cols[i] + 7) / 8;
+    const int64_t total = (int64_t)a.rows[i] * ch;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
+      const int64_t r = q / ch;
+      const int c = (int)(q - r * ch) * 8;
+      st16(a.dst[i] + r * ch * 8 + c, load16<bf16_t>(a.src[i] + r * a.ld[i] + c, a.cols[i] - c));
+    }
+  }
+}
+
 // dz = round(dout * act'(z)) (when dz is given: [m, ldz8], columns past n are
 // 0) and the column sums of 64 rows of it before the rounding (when part is
 // given: [m / 64 rounded up][n]).  32 threads of 8 columns by 8 rows.
@@ -216,14 +237,33 @@ size_t product_ws_bytes(int dtype, bool a_along, bool b_along, int M, int N, int
   return product_ws(dtype == 1, a_along, b_along, M, N, K, compute_units());
 }
 
-hipError_t run_product(int dtype, const Product& p, const Epilogue& e, void* ws, hipStream_t s) {
+hipError_t run_product(int dtype, Product p, const Epilogue& e, void* ws, hipStream_t s) {
   const int cus = compute_units(), np = pad8(p.N);
-  const bool ok = tile_operand((uintptr_t)p.A, p.lda, p.a_padded ? 0 : p.a_along ? p.K : p.M) &&
-                  tile_operand((uintptr_t)p.B, p.ldb, p.b_along ? p.K : p.N);
   // (the few-token kernel has no checkpoints: a block's columns lie in many waves)
   if (p.a_along && p.b_along && p.M <= kFewTokens && !e.z_codes && !e.out_codes) {
     launch_few(dtype, p, e, cus, s);
     return hipGetLastError();
+  }
+  const bool ok_a = tile_operand((uintptr_t)p.A, p.lda, p.a_padded ? 0 : p.a_along ? p.K : p.M);
+  const bool ok_b = tile_operand((uintptr_t)p.B, p.ldb, p.b_padded ? 0 : p.b_along ? p.K : p.N);
+  bool ok = ok_a && ok_b;
+  if (!ok && (ok_a || p.a_pack) && (ok_b || p.b_pack)) {
+    PackArgs q{};
+    if (!ok_a) {
+      const int rows = p.a_along ? p.M : p.K, cols = p.a_along ? p.K : p.M;
+      q.src[0] = (const bf16_t*)p.A, q.ld[0] = p.lda, q.dst[0] = (bf16_t*)p.a_pack;
+      q.rows[0] = rows, q.cols[0] = cols;
+      p.A = p.a_pack, p.lda = pad8(cols), p.a_padded = true;
+    }
+    if (!ok_b) {
+      const int rows = p.b_along ? p.N : p.K, cols = p.b_along ? p.K : p.N;
+      q.src[1] = (const bf16_t*)p.B, q.ld[1] = p.ldb, q.dst[1] = (bf16_t*)p.b_pack;
+      q.rows[1] = rows, q.cols[1] = cols;
+      p.B = p.b_pack, p.ldb = pad8(cols), p.b_padded = true;
+    }
+    const int64_t most = std::max((int64_t)q.rows[0] * pad8(q.cols[0]), (int64_t)q.rows[1] * pad8(q.cols[1])) / 8;
+    launch_k(pack_rows_kernel, (unsigned)std::min<int64_t>(cdiv64(most, 256), 16 * cus), 256, 0, s, q);
+    ok = p.lda <= (1 << 22) && p.ldb <= (1 << 22);
   }
   const ProductPlan plan = product_plan(dtype == 1, ok, p.a_along, p.b_along, p.M, p.N, p.K, cus);
   if (plan.mid && p.a_along && p.b_along) {
@@ -253,23 +293,46 @@ hipError_t run_product(int dtype, const Product& p, const Epilogue& e, void* ws,
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
-// Workspace of the backward pass: dz, the bias gradient's partial sums, a
-// restored from its checkpoint, the products' K slices.
+size_t rows_bytes(int dtype, int64_t rows, int cols) {
+  return up256((size_t)rows * pad8(cols) * (dtype == 0 ? 4 : 2));
+}
+
+// Workspace of the forward pass: copies of a and w, the product's K slices.
+struct ForwardSpace {
+  bool packs;
+  size_t w, prod, bytes;
+  ForwardSpace(int dtype, int m, int n, int k) {
+    packs = m > kFewTokens && product_packs(dtype == 1, true, true, m, n, k, compute_units());
+    w = packs ? rows_bytes(dtype, m, k) : 0;
+    prod = w + (packs ? rows_bytes(dtype, n, k) : 0);
+    bytes = prod + up256(product_ws_bytes(dtype, true, true, m, n, k));
+  }
+};
+
+// Workspace of the backward pass: dz, or dout with whole chunks; the bias
+// gradient's partial sums; a restored from its checkpoint, or with whole
+// chunks; w with whole chunks; the products' K slices.
 struct BackSpace {
-  size_t dz, part, a, prod, bytes;
+  bool packs_da, packs_dw, keeps_dz;
+  size_t dz, part, a, w, prod, bytes;
   BackSpace(int dtype, int act, int m, int n, int k) {
-    const size_t es = dtype == 0 ? 4 : 2;
+    const int cus = compute_units();
+    packs_da = product_packs(dtype == 1, true, false, m, k, n, cus);
+    packs_dw = product_packs(dtype == 1, false, false, n, k, m, cus);
+    keeps_dz = act != ACT_NONE || (n % 8 != 0 && (packs_da || packs_dw));
     dz = 0;
-    part = dz + (act == ACT_NONE ? 0 : up256((size_t)m * pad8(n) * es));
+    part = dz + (keeps_dz ? rows_bytes(dtype, m, n) : 0);
     a = part + up256((size_t)cdiv64(m, 64) * n * 4);
-    prod = a + up256((size_t)m * pad8(k) * es);
-    bytes = prod + up256(std::max(product_ws_bytes(dtype, true, false, m, k, n), product_ws_bytes(dtype, false, false, n, k, m)));
+    w = a + rows_bytes(dtype, m, k);
+    prod = w + (packs_da && k % 8 != 0 ? rows_bytes(dtype, n, k) : 0);
+    bytes = prod + up256(std::max(product_ws_bytes(dtype, true, false, m, k, n),
+                                  product_ws_bytes(dtype, false, false, n, k, m)));
   }
 };
 
 }  // namespace
 
-size_t linear_ws_bytes(int dtype, int m, int n, int k) { return up256(product_ws_bytes(dtype, true, true, m, n, k)); }
+size_t linear_ws_bytes(int dtype, int m, int n, int k) { return ForwardSpace(dtype, m, n, k).bytes; }
 
 size_t linear_backward_ws_bytes(int dtype, int act, int m, int n, int k) {
   return BackSpace(dtype, act, m, n, k).bytes;
@@ -277,10 +340,13 @@ size_t linear_backward_ws_bytes(int dtype, int act, int m, int n, int k) {
 
 hipError_t launch_linear(int dtype, int m, int n, int k, const void* a, int64_t lda, const void* w,
                          int64_t ldw, const LinearOut& o, void* ws, hipStream_t s) {
-  const Product p{a, lda, true, false, w, ldw, true, m, n, k};
+  const ForwardSpace sp(dtype, m, n, k);
+  char* base = static_cast<char*>(ws);
+  const Product p{a, lda, true, false, w, ldw, true, false, m, n, k,
+                  sp.packs ? base : nullptr, sp.packs ? base + sp.w : nullptr};
   const Epilogue e{o.bias, o.res, o.ldr, o.out, o.ldo, o.z, o.ldz, o.z_codes, o.z_scales,
                    o.out_codes, o.out_scales, o.act};
-  return run_product(dtype, p, e, ws, s);
+  return run_product(dtype, p, e, base + sp.prod, s);
 }
 
 hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipStream_t s) {
@@ -290,7 +356,9 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
   int64_t lddz = b.ldo;
   bool padded = false;
   float* part = b.dbias ? (float*)(base + sp.part) : nullptr;
-  const bool need_dz = b.act != ACT_NONE && (b.da || b.dw);
+  const bool need_dz = sp.keeps_dz && (b.da || b.dw);
+  // (64 rows make one part, the gradient itself)
+  const bool one_part = b.m <= 64;
   if (b.m == 0) {
     // no rows: the weight's gradients are 0
     if (b.dbias) {
@@ -303,14 +371,14 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
     const int64_t ld8 = pad8(b.n);
     if (dtype == 0)
       launch_k(act_grad_kernel<float>, grid, 256, 0, s, (const float*)b.dout, b.ldo, b.m, b.n, b.act,
-               (const float*)b.z, b.ldz, b.z_codes, b.z_scales, (float*)dst, ld8, part);
+               (const float*)b.z, b.ldz, b.z_codes, b.z_scales, (float*)dst, ld8, one_part ? b.dbias : part);
     else
       launch_k(act_grad_kernel<bf16_t>, grid, 256, 0, s, (const bf16_t*)b.dout, b.ldo, b.m, b.n, b.act,
-               (const bf16_t*)b.z, b.ldz, b.z_codes, b.z_scales, (bf16_t*)dst, ld8, part);
+               (const bf16_t*)b.z, b.ldz, b.z_codes, b.z_scales, (bf16_t*)dst, ld8, one_part ? b.dbias : part);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     if (need_dz) dz = dst, lddz = ld8, padded = true;
-    if (part) {
+    if (part && !one_part) {
       err = launch_colsum(part, (int)cdiv64(b.m, 64), b.n, b.dbias, nullptr, s);
       if (err != hipSuccess) return err;
     }
@@ -319,14 +387,16 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
   if (b.da && b.m > 0) {
     e.out = b.da;
     e.ldo = b.ldda;
-    const hipError_t err =
-        run_product(dtype, Product{dz, lddz, true, padded, b.w, b.ldw, false, b.m, b.k, b.n}, e, base + sp.prod, s);
+    const Product p{dz, lddz, true, padded, b.w, b.ldw, false, false, b.m, b.k, b.n, nullptr,
+                    sp.packs_da && b.k % 8 != 0 ? base + sp.w : nullptr};
+    const hipError_t err = run_product(dtype, p, e, base + sp.prod, s);
     if (err != hipSuccess) return err;
   }
   if (b.dw) {
     const void* a = b.a;
     int64_t lda = b.lda;
-    if (b.a_codes && b.m > 0) {
+    const bool restored = b.a_codes && b.m > 0;
+    if (restored) {
       a = base + sp.a;
       lda = pad8(b.k);
       const hipError_t err =
@@ -335,7 +405,11 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
     }
     e.out = b.dw;
     e.ldo = b.lddw;
-    return run_product(dtype, Product{dz, lddz, false, padded, a, lda, false, b.n, b.k, b.m}, e, base + sp.prod, s);
+    // (the columns behind a's last are not zeros here, but only reach columns
+    // of dw that are not stored)
+    const Product p{dz, lddz, false, padded, a, lda, false, restored, b.n, b.k, b.m, nullptr,
+                    sp.packs_dw && b.k % 8 != 0 && !restored ? base + sp.a : nullptr};
+    return run_product(dtype, p, e, base + sp.prod, s);
   }
   return hipSuccess;
 }

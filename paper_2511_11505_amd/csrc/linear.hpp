@@ -9,16 +9,17 @@ namespace fs {
 
 // out[i, j] = sum over k of A(i, k) B(j, k), i < M, j < N.  An operand is
 // "along" when k runs along its rows (element (i, k) at i * ld + k), else
-// "across" (at k * ld + i).  a_padded: A's rows go on to a multiple of 8
-// elements, with zeros.
+// "across" (at k * ld + i).  *_padded: the rows go on to a multiple of 8
+// elements, with zeros.  *_pack: room for such a copy, or null.
 struct Product {
   const void* A;
   int64_t lda;
   bool a_along, a_padded;
   const void* B;
   int64_t ldb;
-  bool b_along;
+  bool b_along, b_padded;
   int M, N, K;
+  void *a_pack, *b_pack;
 };
 
 // z = product + bias;  out = act(z) + residual, rounded once.  z and out may

@@ -21,6 +21,7 @@ enum MidShape { MID_NONE, MID_16 /* 16 x 32, 8 */, MID_32 /* 32 x 32, 8 */, MID_
 // 4, which its copies run ahead) or elements (64 x 64).
 struct ProductPlan {
   int height, width, slices, per, mid;
+  double us;   // estimated time
 };
 
 // What linear_tile.hpp asks of an operand: 16-byte chunks that lie whole in
@@ -82,11 +83,11 @@ inline double any_us(int64_t M, int64_t N, int64_t blocks, int64_t s, bool bf16,
 // The plan of least time.  tiles_ok: the operands suit linear_tile.hpp.
 inline ProductPlan product_plan(bool bf16, bool tiles_ok, bool a_along, bool b_along, int64_t M,
                                 int64_t N, int64_t K, int cus) {
-  ProductPlan best{0, 0, 1, 1 << 30, MID_NONE};
+  ProductPlan best{0, 0, 1, 1 << 30, MID_NONE, 1e30};
   if (M <= 0 || N <= 0) return best;
-  double us = 1e30;
   auto take = [&](double t, ProductPlan p) {
-    if (t < us) us = t, best = p;
+    p.us = t;
+    if (t < best.us) best = p;
   };
   const int64_t blocks = cdiv_(K, 64);
   if (bf16 && tiles_ok && blocks >= 4) {
@@ -94,25 +95,41 @@ inline ProductPlan product_plan(bool bf16, bool tiles_ok, bool a_along, bool b_a
     // where K ends inside a block (the copies' pointers leave no registers)
     for (const int h : {128, 192, 224, 256})
       if ((a_along || h % 64 == 0) && (h < 256 || K % 64 == 0))
-        take(large_us(M, N, K, cus, h), {h, 256, 1, (int)blocks, MID_NONE});
+        take(large_us(M, N, K, cus, h), {h, 256, 1, (int)blocks, MID_NONE, 0});
     for (int64_t s = 1; s <= 16 && slices_fit(s, M, N); s *= 2) {
       const int64_t per = cdiv_(blocks, s), n = cdiv_(blocks, per);
       if (blocks - per * (n - 1) < 4) continue;
-      take(small_us(M, N, per, n, cus), {64, 128, (int)n, (int)per, MID_NONE});
+      take(small_us(M, N, per, n, cus), {64, 128, (int)n, (int)per, MID_NONE, 0});
     }
   }
   if (a_along && b_along) {
-    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 16), {0, 0, 1, 0, MID_16});
-    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 32), {0, 0, 1, 0, MID_32});
-    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 64), {0, 0, 1, 0, MID_64});
+    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 16), {0, 0, 1, 0, MID_16, 0});
+    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 32), {0, 0, 1, 0, MID_32, 0});
+    take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 64), {0, 0, 1, 0, MID_64, 0});
   }
   const int64_t bk = bf16 ? 64 : 32;
   for (int64_t s = 1; s <= 32 && slices_fit(s, M, N); s *= 2) {
     const int64_t per = std::max<int64_t>(cdiv_(cdiv_(K, s), bk) * bk, bk);
     const int64_t n = std::max<int64_t>(1, cdiv_(K, per));
-    take(any_us(M, N, per / bk, n, bf16, cus), {0, 0, (int)n, (int)per, MID_NONE});
+    take(any_us(M, N, per / bk, n, bf16, cus), {0, 0, (int)n, (int)per, MID_NONE, 0});
   }
   return best;
+}
+
+// Whether operands that linear_tile.hpp cannot read for their widths (K % 8 !=
+// 0 along, M or N % 8 != 0 across) are first copied to rows of whole 16-byte
+// chunks (zeros behind the last element): when the tiles' time and the copies',
+// a launch and a pass over memory, are less than the other kernels'.  By the
+// sizes alone, so that the workspace is known.  (777 x 1001, K 1409: 19 us
+// without, 8192 x 8191, K 5119: 1.36 ms.)
+inline bool product_packs(bool bf16, bool a_along, bool b_along, int64_t M, int64_t N, int64_t K, int cus) {
+  if (!bf16 || M <= 0 || N <= 0) return false;
+  const bool a = (a_along ? K : M) % 8 != 0, b = (b_along ? K : N) % 8 != 0;
+  if (!a && !b) return false;
+  const ProductPlan tiles = product_plan(true, true, a_along, b_along, M, N, K, cus);
+  const double copied = (a ? (double)M * K : 0.0) + (b ? (double)N * K : 0.0);
+  return tiles.height &&
+         tiles.us + 3.5 + copied * 4 / 3e6 < product_plan(true, false, a_along, b_along, M, N, K, cus).us;
 }
 
 // Bytes of partial sums of the plan, whichever kernel the operands' alignment

@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256, TN == 8 ? 1 : 2) void linear_tile_kernel(Produ
   auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const bf16_t *A = (const bf16_t*)p.A, *B = (const bf16_t*)p.B;
   const int nblocks = (p.K + 63) / 64;
-  const int ma = LA ? p.M : (p.M + 7) & ~7;
+  const int ma = LA ? p.M : (p.M + 7) & ~7, nb = LB ? p.N : (p.N + 7) & ~7;
 
   const unsigned ring_lds = lds_addr(ring);
   const unsigned ldsA = ring_lds + wave * 1024, ldsB = ring_lds + 2 * ASLOT + wave * 1024;
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(256, TN == 8 ? 1 : 2) void linear_tile_kernel(Produ
   SrcA sa;
   SrcB sb;
   sa.set(A, p.lda, it.m0, ma, it.kb, p.K);
-  sb.set(B, p.ldb, it.n0, p.N, it.kb, p.K);
+  sb.set(B, p.ldb, it.n0, nb, it.kb, p.K);
   // LDS offsets of the slots of the current block, the next (and, B, the one
   // after)
   unsigned oa0 = 0, oa1 = ASLOT, ob0 = 0, ob1 = BSLOT, ob2 = 2 * BSLOT;
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(256, TN == 8 ? 1 : 2) void linear_tile_kernel(Produ
     }
     // the last three blocks send out the next item's B copies, the last two
     // its A copies
-    sb.set(B, p.ldb, nx.n0, p.N, nx.kb, p.K);
+    sb.set(B, p.ldb, nx.n0, nb, nx.kb, p.K);
     half(F[0], F[1], I0{}, I0{});
     half(F[1], F[0], I1{}, I0{});
     sa.set(A, p.lda, nx.m0, ma, nx.kb, p.K);
@@ -387,14 +387,14 @@ __global__ __launch_bounds__(256, TN == 8 ? 1 : 2) void linear_tile_kernel(Produ
         if (scales && r < p.M) {
           constexpr int NB = TN / 2;
           const uint32_t bytes = lane < 16 ? zb : ob;
-          const int nb = (p.N + kCkptBlock - 1) / kCkptBlock, b0 = (it.n0 + wn * 16 * TN) / kCkptBlock;
-          uint8_t* q = scales + r * nb + b0;
-          if (b0 + NB <= nb) {
+          const int blks = (p.N + kCkptBlock - 1) / kCkptBlock, b0 = (it.n0 + wn * 16 * TN) / kCkptBlock;
+          uint8_t* q = scales + r * blks + b0;
+          if (b0 + NB <= blks) {
             memcpy(q, &bytes, NB);
           } else {
 #pragma unroll
             for (int j = 0; j < NB - 1; ++j)
-              if (b0 + j < nb) q[j] = (uint8_t)(bytes >> (8 * j));
+              if (b0 + j < blks) q[j] = (uint8_t)(bytes >> (8 * j));
           }
         }
       }

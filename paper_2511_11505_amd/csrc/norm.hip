@@ -8,10 +8,17 @@
 //   dx = dres + rstd * (u - mean(u) - h * mean(u * h))   (uncentred: no mean(u))
 //   dgamma = sum over rows of dy * h;  dbeta = sum over rows of dy
 //
-// Both are bound by memory.  A row stays in the registers of its TPR threads
-// (NC chunks of 8 columns each) from the load to the store, so every input is
-// read once; the variance is a second sum over the registers, of squares of
-// differences, which loses no digits to a large mean.
+// Both are bound by memory.  A row stays in registers from the load to the
+// store, so every input is read once; the variance is a second sum over the
+// registers, of squares of differences, which loses no digits to a large mean.
+// A row of up to 1024 columns belongs to a wave (sums without a barrier, four
+// rows to a workgroup), a longer one to a workgroup of as many threads as it
+// has 8-column chunks, or half or a quarter of that (NC chunks per thread): with
+// 256 threads and three chunks each, 8192 x 5120 took 91 us (now FORWARD_US) and
+// the backward pass 92 us (now BACKWARD_US), 64 x 7168 7.5 us (now DECODE_US).
+
+#include <algorithm>
+#include <type_traits>
 
 #include "internal.hpp"
 #include "saved.hpp"
@@ -19,65 +26,77 @@
 namespace fs {
 namespace {
 
-// Sum over the TPR threads of a row; `red` holds one float per wave, and two
-// calls that follow each other use different ones.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* red) {
-  v = wave_sum(v);
-  if constexpr (TPR > 64) {
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
+// Sums of N values over the threads of a row; `red` holds N floats per wave,
+// and two calls that follow each other use different ones.
+template <bool WAVE, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*red)[N]) {
 #pragma unroll
-    for (int w = 0; w < TPR / 64; ++w) v += red[w];
+  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+  if constexpr (!WAVE) {
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) red[threadIdx.x >> 6][i] = v[i];
+    __syncthreads();
+    // lane w of 16 takes wave w's; a fixed tree over 16 lanes
+    const int w = threadIdx.x & 15, nw = blockDim.x >> 6;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float x = w < nw ? red[w][i] : 0.f;
+      x += dpp_f<kDppXor1>(x);
+      x += dpp_f<kDppXor2>(x);
+      x += dpp_f<kDppHalfMirror>(x);
+      x += dpp_f<kDppMirror>(x);
+      v[i] = x;
+    }
   }
-  return v;
 }
 
-constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
-
-template <typename T, int TPR, int NC>
-__global__ __launch_bounds__(threads_of(TPR)) void norm_kernel(NormArgs a) {
-  constexpr int RPB = threads_of(TPR) / TPR;
-  __shared__ float red[2][TPR / 64];
-  const int tid = threadIdx.x % TPR;
-  const int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-  if (r >= a.rows) return;   // a whole wave; with more waves per row, none
+template <typename T, bool WAVE, int NC>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a) {
+  __shared__ float red[2][16][1];
+  const int tpr = WAVE ? 64 : blockDim.x, tid = WAVE ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t r = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  if (r >= a.rows) return;   // a whole wave of its own row
   const T* x = (const T*)a.x + r * a.ldx;
   const T* add = (const T*)a.add + r * a.ldadd;
   float v[NC][8];
-  float s = 0.f;
+  float s[1] = {0.f};
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
-    const int c = (j * TPR + tid) * 8, n = min(8, a.cols - c);
+    const int c = (j * tpr + tid) * 8, n = min(8, a.cols - c);
     Raw8<T> q = {}, p = {};
     if (n > 0) q = load8<T>(x + c, n);
     if (a.add && n > 0) p = load8<T>(add + c, n);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[j][i] = a.add ? rounded<T>(q.get(i) + p.get(i)) : q.get(i);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += v[j][i];   // 0 past the row's end
+    for (int i = 0; i < 8; ++i) s[0] += v[j][i];   // 0 past the row's end
   }
   const float inv_d = 1.0f / (float)a.cols;
-  const float mean = a.center ? row_sum<TPR>(s, red[0]) * inv_d : 0.f;
-  float q = 0.f;
+  float mean = 0.f;
+  if (a.center) {
+    row_sums<WAVE>(s, red[0]);
+    mean = s[0] * inv_d;
+  }
+  float q[1] = {0.f};
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
-    const int n = a.cols - (j * TPR + tid) * 8;
+    const int n = a.cols - (j * tpr + tid) * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float t = v[j][i] - mean;
-      q += i < n ? t * t : 0.f;
+      q[0] += i < n ? t * t : 0.f;
     }
   }
-  const float rstd = 1.0f / sqrtf(row_sum<TPR>(q, red[1]) * inv_d + a.eps);
+  row_sums<WAVE>(q, red[1]);
+  const float rstd = 1.0f / sqrtf(q[0] * inv_d + a.eps);
   if (tid == 0) {
     if (a.mean) a.mean[r] = mean;
     if (a.rstd) a.rstd[r] = rstd;
   }
 #pragma unroll
   for (int j = 0; j < NC; ++j) {
-    const int c = (j * TPR + tid) * 8, n = min(8, a.cols - c);
+    const int c = (j * tpr + tid) * 8, n = min(8, a.cols - c);
     if (a.sum && n > 0) store8<T>((T*)a.sum + r * a.ldsum + c, v[j], n);
     if (a.in_codes) ckpt_store8<LANES_NEXT>(a.in_codes, a.in_scales, r, c, a.cols, v[j], n, true);
     float y[8] = {};
@@ -98,96 +117,121 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_kernel(NormArgs a) {
   }
 }
 
-// One group of TPR threads takes rows g, g + groups, ..; each thread keeps its
-// columns' part of dgamma and dbeta in registers and writes it once at the
-// end, part[0][group][cols] and part[1][group][cols], which colsum_kernel adds
-// in group order.
-template <typename T, int TPR, int NC, bool CODES>
-__global__ __launch_bounds__(threads_of(TPR)) void norm_backward_kernel(NormBackArgs a) {
-  constexpr int RPB = threads_of(TPR) / TPR, NW = TPR / 64;
-  __shared__ float red[2][2][NW];
-  const int tid = threadIdx.x % TPR, wave = (threadIdx.x % TPR) >> 6;
-  const int64_t group = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-  const int64_t groups = (int64_t)gridDim.x * RPB;
+// One group (a wave, or a workgroup) takes rows g, g + groups, ..; each thread
+// keeps its columns' part of dgamma and dbeta in registers and writes it once at
+// the end, part[0][group][cols] and part[1][group][cols], which colsum_kernel
+// adds in a fixed order.  The next row is in flight during a row's sums; h and u
+// are computed twice rather than kept.
+template <typename T, bool WAVE, int NC, bool CODES>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_backward_kernel(NormBackArgs a) {
+  __shared__ float red[2][16][2];
+  const int tpr = WAVE ? 64 : blockDim.x, tid = WAVE ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t group = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int64_t groups = (int64_t)gridDim.x * (WAVE ? 4 : 1);
   const int nb = (a.cols + kCkptBlock - 1) / kCkptBlock;
   const float inv_d = 1.0f / (float)a.cols;
+  // More than a chunk per thread of a workgroup's row leaves no registers for a
+  // row ahead and gamma, four not even for the row: the second pass loads it
+  // again.
+  constexpr bool AHEAD = WAVE || NC == 1, HOLD = WAVE || NC < 4;
   float dg[NC][8] = {}, db[NC][8] = {};
-  Raw8<T> xr[NC], yr[NC], rr[NC];
-  uint2 xc[NC];
-  int xb[NC];
-  float nmean = 0.f, nrstd = 0.f;
-  auto load = [&](int64_t r) {
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const int c = (j * TPR + tid) * 8, n = min(8, a.cols - c);
-      xr[j] = {}, yr[j] = {}, rr[j] = {};
-      xc[j] = make_uint2(0, 0);
-      xb[j] = 127;
-      if (n <= 0) continue;
+  struct Chunk {
+    Raw8<T> x, dy, res;
+    uint2 codes;
+    int byte;
+  };
+  auto chunk = [&](int j, int64_t r) __attribute__((always_inline)) {
+    const int c = (j * tpr + tid) * 8, n = min(8, a.cols - c);
+    Chunk w = {};
+    w.byte = 127;
+    if (n > 0) {
       if constexpr (CODES) {
-        xc[j] = load_codes(a.x_codes + r * a.cols + c, n);
-        xb[j] = a.x_scales[r * nb + c / kCkptBlock];
+        w.codes = load_codes(a.x_codes + r * a.cols + c, n);
+        w.byte = a.x_scales[r * nb + c / kCkptBlock];
       } else {
-        xr[j] = load8<T>((const T*)a.x + r * a.ldx + c, n);
+        w.x = load8<T>((const T*)a.x + r * a.ldx + c, n);
       }
-      yr[j] = load8<T>((const T*)a.dy + r * a.lddy + c, n);
-      if (a.dres) rr[j] = load8<T>((const T*)a.dres + r * a.lddres + c, n);
+      w.dy = load8<T>((const T*)a.dy + r * a.lddy + c, n);
+      if (a.dres) w.res = load8<T>((const T*)a.dres + r * a.lddres + c, n);
+    }
+    return w;
+  };
+  auto load_gamma = [&](int j) __attribute__((always_inline)) {
+    const int c = (j * tpr + tid) * 8, n = min(8, a.cols - c);
+    Raw8<float> g;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g.w[i] = 0x3F800000u;
+    if (a.gamma && n > 0) g = load8<float>(a.gamma + c, n);
+    return g;
+  };
+  // h of a chunk, 0 past the row's end
+  auto values = [&](const Chunk& w, int j, float mean, float rstd, float (&h)[8]) __attribute__((always_inline)) {
+    const int n = a.cols - (j * tpr + tid) * 8;
+    if constexpr (CODES) {
+      ckpt_values(w.codes, w.byte, h);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = w.x.get(i);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = i < n ? (h[i] - mean) * rstd : 0.f;
+  };
+  Raw8<float> gamma[AHEAD ? NC : 1];
+  Chunk row[HOLD ? NC : 1], next[AHEAD ? NC : 1];
+  float nmean = 0.f, nrstd = 0.f;
+  auto load_next = [&](int64_t r) __attribute__((always_inline)) {
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int j = 0; j < NC; ++j) next[j] = chunk(j, r);
     }
     nmean = a.mean ? a.mean[r] : 0.f;
     nrstd = a.rstd[r];
   };
-  if (group < a.rows) load(group);
+  if constexpr (AHEAD) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) gamma[j] = load_gamma(j);
+  }
+  if (group < a.rows) load_next(group);
   int par = 0;
   for (int64_t r = group; r < a.rows; r += groups, par ^= 1) {
     const float mean = nmean, rstd = nrstd;
-    float h[NC][8], u[NC][8];
-    Raw8<T> res[NC];
-    float s1 = 0.f, s2 = 0.f;
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int j = 0; j < NC; ++j) row[j] = next[j];
+    }
+    if (r + groups < a.rows) load_next(r + groups);
+    float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      const int c = (j * TPR + tid) * 8, n = min(8, a.cols - c);
-      float x[8];
-      if constexpr (CODES) {
-        ckpt_values(xc[j], xb[j], x);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = xr[j].get(i);
-      }
-      Raw8<float> g = {};
-      if (a.gamma && n > 0) g = load8<float>(a.gamma + c, n);
+      Chunk& w = row[HOLD ? j : 0];
+      if constexpr (!AHEAD) w = chunk(j, r);
+      const Raw8<float> g = AHEAD ? gamma[AHEAD ? j : 0] : load_gamma(j);
+      float h[8];
+      values(w, j, mean, rstd, h);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bool in = i < n;
-        const float dy = yr[j].get(i);   // 0 past the row's end
-        h[j][i] = in ? (x[i] - mean) * rstd : 0.f;
-        u[j][i] = a.gamma ? dy * g.get(i) : dy;
-        dg[j][i] = fmaf(dy, h[j][i], dg[j][i]);
+        const float dy = w.dy.get(i), u = dy * g.get(i);   // 0 past the row's end
+        dg[j][i] = fmaf(dy, h[i], dg[j][i]);
         db[j][i] += dy;
-        s1 += u[j][i];
-        s2 = fmaf(u[j][i], h[j][i], s2);
+        s[0] += u;
+        s[1] = fmaf(u, h[i], s[1]);
       }
-      res[j] = rr[j];
     }
-    if (r + groups < a.rows) load(r + groups);   // in flight during this row's sums
-    s1 = wave_sum(s1);
-    s2 = wave_sum(s2);
-    if constexpr (TPR > 64) {
-      if ((threadIdx.x & 63) == 0) red[par][0][wave] = s1, red[par][1][wave] = s2;
-      __syncthreads();
-      s1 = s2 = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) s1 += red[par][0][w], s2 += red[par][1][w];
-    }
-    const float m1 = a.center ? s1 * inv_d : 0.f, m2 = s2 * inv_d;
+    row_sums<WAVE>(s, red[par]);
+    const float m1 = a.center ? s[0] * inv_d : 0.f, m2 = s[1] * inv_d;
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      const int c = (j * TPR + tid) * 8, n = min(8, a.cols - c);
+      const int c = (j * tpr + tid) * 8, n = min(8, a.cols - c);
       if (n <= 0) continue;
-      float o[8];
+      Chunk& w = row[HOLD ? j : 0];
+      if constexpr (!HOLD) w = chunk(j, r);
+      const Raw8<float> g = AHEAD ? gamma[AHEAD ? j : 0] : load_gamma(j);
+      float h[8], o[8];
+      values(w, j, mean, rstd, h);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        o[i] = rstd * (u[j][i] - m1 - h[j][i] * m2);
-        if (a.dres) o[i] += res[j].get(i);
+        o[i] = rstd * (w.dy.get(i) * g.get(i) - m1 - h[i] * m2);
+        if (a.dres) o[i] += w.res.get(i);
       }
       store8<T>((T*)a.dx + r * a.lddx + c, o, n);
     }
@@ -195,7 +239,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_backward_kernel(NormBack
   if (a.part) {
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-      const int c = (j * TPR + tid) * 8, n = min(8, a.cols - c);
+      const int c = (j * tpr + tid) * 8, n = min(8, a.cols - c);
       if (n <= 0) continue;
       float* p = a.part + group * a.cols + c;
       store8<float>(p, dg[j], n);
@@ -227,49 +271,44 @@ __global__ __launch_bounds__(1024) void colsum_kernel(const float* __restrict__ 
   }
 }
 
-// Threads per row and chunks per thread.  A wave per row up to 2048 columns
-// (four rows to a workgroup, sums without a barrier), then the workgroup that
-// holds the row in at most 4 chunks per thread.
+// Calls f(wave per row?, chunks per thread) with the threads of a workgroup.
 template <typename F>
 void with_shape(int cols, F&& f) {
   using std::integral_constant;
-#define FS_NORM_SHAPE(TPR, NC) \
-  if (cols <= TPR * NC * 8) return f(integral_constant<int, TPR>{}, integral_constant<int, NC>{})
-  FS_NORM_SHAPE(64, 1);
-  FS_NORM_SHAPE(64, 2);
-  FS_NORM_SHAPE(64, 4);
-  FS_NORM_SHAPE(256, 2);
-  FS_NORM_SHAPE(256, 3);
-  FS_NORM_SHAPE(256, 4);
-  FS_NORM_SHAPE(1024, 2);
-  FS_NORM_SHAPE(1024, 4);
-#undef FS_NORM_SHAPE
+  using Yes = std::true_type;
+  using No = std::false_type;
+  const int chunks = (cols + 7) / 8;
+  auto threads = [&](int nc) { return (chunks + 64 * nc - 1) / (64 * nc) * 64; };
+  if (chunks <= 64) f(Yes{}, integral_constant<int, 1>{}, 256);
+  else if (chunks <= 128) f(Yes{}, integral_constant<int, 2>{}, 256);
+  else if (chunks <= 1024) f(No{}, integral_constant<int, 1>{}, threads(1));
+  else if (chunks <= 2048) f(No{}, integral_constant<int, 2>{}, threads(2));
+  else f(No{}, integral_constant<int, 4>{}, threads(4));
 }
 
-constexpr int kNormGroups = 512;   // workgroups of the backward pass
-
-// Groups (rows of partial sums) of the backward pass.
-int64_t norm_groups(int64_t rows, int cols, int tpr) {
-  (void)cols;
-  const int rpb = threads_of(tpr) / tpr;
-  const int64_t wg = cdiv64(rows, rpb);
-  return (wg < kNormGroups ? wg : kNormGroups) * rpb;
+// Workgroups of the backward pass: about 16 waves per CU.  (More of them write
+// more partial sums: 8 bytes per column each.)
+int64_t norm_groups(int64_t rows, bool wave, int threads) {
+  const int64_t wgs = wave ? cdiv64(rows, 4) : rows;
+  const int64_t most = (int64_t)compute_units() * std::max(1, 16 * 64 / threads);
+  return wgs < most ? wgs : most;
 }
 
 }  // namespace
 
 size_t norm_ws_bytes(int64_t rows, int cols) {
   int64_t g = 0;
-  with_shape(cols, [&](auto tpr, auto) { g = norm_groups(rows, cols, tpr); });
+  with_shape(cols, [&](auto wave, auto, int threads) { g = norm_groups(rows, wave, threads) * (wave ? 4 : 1); });
   return (size_t)g * cols * 2 * sizeof(float);
 }
 
 hipError_t launch_norm(int dtype, const NormArgs& a, hipStream_t s) {
-  with_shape(a.cols, [&](auto tpr, auto nc) {
-    constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
-    const unsigned grid = (unsigned)cdiv64(a.rows, threads_of(TPR) / TPR);
-    if (dtype == 0) launch_k(norm_kernel<float, TPR, NC>, grid, threads_of(TPR), 0, s, a);
-    else launch_k(norm_kernel<bf16_t, TPR, NC>, grid, threads_of(TPR), 0, s, a);
+  with_shape(a.cols, [&](auto wave, auto nc, int threads) {
+    constexpr bool W = decltype(wave)::value;
+    constexpr int NC = decltype(nc)::value;
+    const unsigned grid = (unsigned)cdiv64(a.rows, W ? 4 : 1);
+    if (dtype == 0) launch_k(norm_kernel<float, W, NC>, grid, threads, 0, s, a);
+    else launch_k(norm_kernel<bf16_t, W, NC>, grid, threads, 0, s, a);
   });
   return hipGetLastError();
 }
@@ -277,16 +316,18 @@ hipError_t launch_norm(int dtype, const NormArgs& a, hipStream_t s) {
 hipError_t launch_norm_backward(int dtype, const NormBackArgs& a, float* dgamma, float* dbeta,
                                 hipStream_t s) {
   int64_t groups = 0;
-  with_shape(a.cols, [&](auto tpr, auto nc) {
-    constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
-    groups = norm_groups(a.rows, a.cols, TPR);
-    const unsigned grid = (unsigned)(groups / (threads_of(TPR) / TPR)), nt = threads_of(TPR);
+  with_shape(a.cols, [&](auto wave, auto nc, int threads) {
+    constexpr bool W = decltype(wave)::value;
+    constexpr int NC = decltype(nc)::value;
+    const int64_t wgs = norm_groups(a.rows, W, threads);
+    groups = wgs * (W ? 4 : 1);
+    const unsigned grid = (unsigned)wgs;
     if (dtype == 0) {
-      if (a.x_codes) launch_k(norm_backward_kernel<float, TPR, NC, true>, grid, nt, 0, s, a);
-      else launch_k(norm_backward_kernel<float, TPR, NC, false>, grid, nt, 0, s, a);
+      if (a.x_codes) launch_k(norm_backward_kernel<float, W, NC, true>, grid, threads, 0, s, a);
+      else launch_k(norm_backward_kernel<float, W, NC, false>, grid, threads, 0, s, a);
     } else {
-      if (a.x_codes) launch_k(norm_backward_kernel<bf16_t, TPR, NC, true>, grid, nt, 0, s, a);
-      else launch_k(norm_backward_kernel<bf16_t, TPR, NC, false>, grid, nt, 0, s, a);
+      if (a.x_codes) launch_k(norm_backward_kernel<bf16_t, W, NC, true>, grid, threads, 0, s, a);
+      else launch_k(norm_backward_kernel<bf16_t, W, NC, false>, grid, threads, 0, s, a);
     }
   });
   hipError_t e = hipGetLastError();

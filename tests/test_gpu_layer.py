@@ -126,7 +126,8 @@ def test_linear(m, n, k, dtype):
 # sizes that fill the large tiles: whole tiles, ragged rows and columns, K that
 # ends inside a block, the least K, one and several tiles per workgroup
 # (and the 64 x 128 tiles: ragged edges, K in slices)
-LARGE = [(1000, 1992, 520, 0), (520, 2056, 2056, 8), (70, 4104, 4104, 0), (513, 1000, 1992, 0), (4096, 2048, 256, 0), (3000, 2600, 328, 8), (6100, 1992, 200, 0), (2047, 4104, 520, 0),
+# (and operands that have to be copied first)
+LARGE = [(900, 1501, 1409, 0), (3001, 2003, 777, 0), (2050, 2050, 301, 1), (1000, 1992, 520, 0), (520, 2056, 2056, 8), (70, 4104, 4104, 0), (513, 1000, 1992, 0), (4096, 2048, 256, 0), (3000, 2600, 328, 8), (6100, 1992, 200, 0), (2047, 4104, 520, 0),
          (9000, 2900, 264, 0)]
 
 
@@ -231,7 +232,8 @@ def test_linear_backward(m, n, k, dtype):
 
 @pytest.mark.parametrize("m,n,k,act,pad,coded", [
     (4096, 1024, 2048, "none", 0, False), (3000, 2600, 2504, "silu", 8, True),
-    (600, 2056, 2504, "silu", 0, False), (130, 1999, 4104, "relu", 0, True), (2500, 264, 520, "none", 8, False),
+    (1501, 1409, 2003, "none", 0, False), (1501, 1408, 2003, "silu", 0, False), (2003, 1409, 1504, "none", 0, False),
+    (3000, 1001, 2002, "gelu", 1, True), (600, 2056, 2504, "silu", 0, False), (130, 1999, 4104, "relu", 0, True), (2500, 264, 520, "none", 8, False),
     (2047, 1999, 4104, "gelu", 0, False), (300, 4104, 3000, "relu", 0, True), (5000, 200, 6104, "none", 0, True),
     (6100, 3001, 1992, "silu", 0, True)])
 def test_linear_backward_large(m, n, k, act, pad, coded):
@@ -283,7 +285,7 @@ def test_linear_backward_without_tokens():
 
 # --------------------------------------------------------------- layer norm
 NORM_SIZES = [(1, 1), (3, 7), (5, 64), (2, 515), (9, 1000), (4, 2048), (7, 2056), (3, 5120), (6, 7169),
-              (2, 12345), (1, 32768)]
+              (2, 12345), (3, 20001), (1, 32768)]
 
 
 def depth(d):
@@ -418,7 +420,7 @@ def check_norm_backward(m, d, dtype, center, coded, dres, affine, pad):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("coded", [False, True])
-@pytest.mark.parametrize("m,d", NORM_SIZES + [(700, 40), (1100, 300), (600, 2100)])
+@pytest.mark.parametrize("m,d", NORM_SIZES + [(700, 40), (1100, 300), (600, 2100), (5000, 24), (700, 9000)])
 def test_norm_backward(m, d, coded, dtype):
     check_norm_backward(m, d, dtype, True, coded, True, True, 0)
 
