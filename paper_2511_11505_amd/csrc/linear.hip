@@ -8,6 +8,7 @@
 // forward along/along, da along/across, dw across/across.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "linear.hpp"
 #include "linear_rules.hpp"
@@ -28,16 +29,39 @@ struct Panel {
   static constexpr int ROWS = ALONG ? 64 : BK, PIECES = ALONG ? 8 : 64 / V;
   static constexpr int STRIDE = (ALONG ? 128 : 64 * (int)sizeof(T)) + 16;   // bytes
   static constexpr int BYTES = ROWS * STRIDE;
-  // the two 16-byte pieces of this thread for the K block at kb
-  static __device__ __forceinline__ void fetch(const T* p, int64_t ld, int row0, int rows, int kb,
-                                               int kend, uint4 (&st)[2]) {
+  // This thread's two 16-byte pieces: where the next whole K block has them,
+  // and how many of their elements exist.  (Rows past the end, along, are
+  // copies of the last: their outputs are not stored.)
+  const T* p[2];
+  int n[2];
+  int64_t step;
+  __device__ __forceinline__ void init(const T* base, int64_t ld, int row0, int rows, int k0) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int q = (int)threadIdx.x + 256 * i, r = q / PIECES, e = (q % PIECES) * V;
-      const int row = ALONG ? row0 + r : kb + r;      // memory row
-      const int col = ALONG ? kb + e : row0 + e;
-      const int n = row < (ALONG ? rows : kend) ? (ALONG ? kend : rows) - col : 0;
-      st[i] = n > 0 ? load16<T>(p + (int64_t)row * ld + col, n) : make_uint4(0, 0, 0, 0);
+      if constexpr (ALONG) {
+        p[i] = base + (int64_t)min(row0 + r, rows - 1) * ld + k0 + e;
+        n[i] = V;
+      } else {
+        p[i] = base + (int64_t)(k0 + r) * ld + row0 + e;
+        n[i] = rows - row0 - e;
+      }
+    }
+    step = ALONG ? BK : BK * ld;
+  }
+  // the K block with `left` elements of K
+  __device__ __forceinline__ void fetch(int left, uint4 (&st)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int have = n[i];
+      if (left < BK) {   // (uniform; the last block)
+        const int q = (int)threadIdx.x + 256 * i;
+        if (ALONG) have = left - (q % PIECES) * V;
+        else if (q / PIECES >= left) have = 0;
+      }
+      if (ALONG && left >= BK) st[i] = load16<T>(p[i], V);
+      else st[i] = have > 0 ? load16<T>(p[i], have) : make_uint4(0, 0, 0, 0);
+      p[i] += step;
     }
   }
   static __device__ __forceinline__ void put(unsigned char* lds, const uint4 (&st)[2]) {
@@ -89,31 +113,41 @@ __global__ __launch_bounds__(256) void linear_any_kernel(Product p, Epilogue e, 
   const int k0 = blockIdx.y * kper, kend = min(p.K, k0 + kper);
   const T *A = (const T*)p.A, *B = (const T*)p.B;
   floatx4 acc[2][2] = {};
-  uint4 ra[2], rb[2];
-  PA::fetch(A, p.lda, m0, p.M, k0, kend, ra);
-  PB::fetch(B, p.ldb, n0, p.N, k0, kend, rb);
-  int buf = 0;
-  for (int kb = k0; kb < kend; kb += BK, buf ^= 1) {
-    PA::put(sa[buf], ra);
-    PB::put(sb[buf], rb);
-    __syncthreads();
-    if (kb + BK < kend) {
-      PA::fetch(A, p.lda, m0, p.M, kb + BK, kend, ra);
-      PB::fetch(B, p.ldb, n0, p.N, kb + BK, kend, rb);
+  // blocks go through registers two ahead: the loads of block i + 2 are sent
+  // out when block i is in LDS (with one ahead, a block of one workgroup per CU
+  // took a load's whole latency)
+  uint4 ra[2][2], rb[2][2];
+  PA pa;
+  PB pb;
+  pa.init(A, p.lda, m0, p.M, k0);
+  pb.init(B, p.ldb, n0, p.N, k0);
+  auto fetch = [&](int i, int kb) __attribute__((always_inline)) {
+    if (kb < kend) {
+      pa.fetch(kend - kb, ra[i]);
+      pb.fetch(kend - kb, rb[i]);
     }
+  };
+  auto block = [&](int i, int kb) __attribute__((always_inline)) {
+    PA::put(sa[i], ra[i]);
+    PB::put(sb[i], rb[i]);
+    __syncthreads();
+    fetch(i, kb + 2 * BK);
 #pragma unroll
     for (int step = 0; step < 2; ++step) {
       uint4 fa[2], fb[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fa[i] = PA::frag(sa[buf], wm + 16 * i, step);
-        fb[i] = PB::frag(sb[buf], wn + 16 * i, step);
+      for (int j = 0; j < 2; ++j) {
+        fa[j] = PA::frag(sa[i], wm + 16 * j, step);
+        fb[j] = PB::frag(sb[i], wn + 16 * j, step);
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = mma16<T>(fb[j], fa[i], acc[i][j]);
+      mma_step<T>(fa, fb, acc);
     }
+  };
+  fetch(0, k0);
+  fetch(1, k0 + BK);
+  for (int kb = k0; kb < kend; kb += 2 * BK) {
+    block(0, kb);
+    if (kb + BK < kend) block(1, kb + BK);
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -170,9 +204,9 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(PackArgs a) {
 }
 
 // dz = round(dout * act'(z)) (when dz is given: [m, ldz8], columns past n are
-// 0) and the column sums of 64 rows of it before the rounding (when part is
-// given: [m / 64 rounded up][n]).  32 threads of 8 columns by 8 rows.
-template <typename T>
+// 0) and the column sums of 8 R rows of it before the rounding (when part is
+// given: [m / (8 R) rounded up][n]).  32 threads of 8 columns by 8 rows.
+template <typename T, int R>
 __global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dout, int64_t ldo, int m,
                                                        int n, int act, const T* __restrict__ z,
                                                        int64_t ldz, const uint8_t* __restrict__ codes,
@@ -187,8 +221,8 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dou
   float sum[8] = {};
   if (nv > 0) {
 #pragma unroll 4
-    for (int i = 0; i < 8; ++i) {
-      const int64_t r = rb * 64 + 8 * i + ty;
+    for (int i = 0; i < R; ++i) {
+      const int64_t r = rb * 8 * R + 8 * i + ty;
       if (r >= m) break;
       const Raw8<T> d = load8<T>(dout + r * ldo + c, nv);
       float g[8];
@@ -217,6 +251,15 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const T* __restrict__ dou
     for (int i = 0; i < 8; ++i) s += sm[i][threadIdx.x];
     part[(size_t)rb * n + col] = s;
   }
+}
+
+// Rows of a workgroup of act_grad_kernel: 64, fewer while that leaves less than
+// two workgroups per CU (512 x 1408 fp32: 48 workgroups took 10.8 us, 384
+// 6.1 us).
+int act_grad_rows(int m, int n) {
+  int rows = 64;
+  while (rows > 8 && cdiv64(m, rows) * cdiv64(n, 256) < 2 * compute_units()) rows /= 2;
+  return rows;
 }
 
 int pad8(int n) { return (n + 7) / 8 * 8; }
@@ -322,7 +365,7 @@ struct BackSpace {
     keeps_dz = act != ACT_NONE || (n % 8 != 0 && (packs_da || packs_dw));
     dz = 0;
     part = dz + (keeps_dz ? rows_bytes(dtype, m, n) : 0);
-    a = part + up256((size_t)cdiv64(m, 64) * n * 4);
+    a = part + up256((size_t)cdiv64(m, act_grad_rows(m, n)) * n * 4);
     w = a + rows_bytes(dtype, m, k);
     prod = w + (packs_da && k % 8 != 0 ? rows_bytes(dtype, n, k) : 0);
     bytes = prod + up256(std::max(product_ws_bytes(dtype, true, false, m, k, n),
@@ -357,8 +400,9 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
   bool padded = false;
   float* part = b.dbias ? (float*)(base + sp.part) : nullptr;
   const bool need_dz = sp.keeps_dz && (b.da || b.dw);
-  // (64 rows make one part, the gradient itself)
-  const bool one_part = b.m <= 64;
+  // (with one part it is the gradient itself)
+  const int rows = act_grad_rows(b.m, b.n);
+  const bool one_part = b.m <= rows;
   if (b.m == 0) {
     // no rows: the weight's gradients are 0
     if (b.dbias) {
@@ -366,20 +410,28 @@ hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipS
       if (err != hipSuccess) return err;
     }
   } else if (need_dz || part) {
-    const unsigned grid = (unsigned)(cdiv64(b.n, 256) * cdiv64(b.m, 64));
+    const unsigned grid = (unsigned)(cdiv64(b.n, 256) * cdiv64(b.m, rows));
     void* dst = need_dz ? base + sp.dz : nullptr;
     const int64_t ld8 = pad8(b.n);
-    if (dtype == 0)
-      launch_k(act_grad_kernel<float>, grid, 256, 0, s, (const float*)b.dout, b.ldo, b.m, b.n, b.act,
-               (const float*)b.z, b.ldz, b.z_codes, b.z_scales, (float*)dst, ld8, one_part ? b.dbias : part);
-    else
-      launch_k(act_grad_kernel<bf16_t>, grid, 256, 0, s, (const bf16_t*)b.dout, b.ldo, b.m, b.n, b.act,
-               (const bf16_t*)b.z, b.ldz, b.z_codes, b.z_scales, (bf16_t*)dst, ld8, one_part ? b.dbias : part);
+    float* sums = one_part ? b.dbias : part;
+    auto run = [&](auto r) {
+      constexpr int R = decltype(r)::value;
+      if (dtype == 0)
+        launch_k(act_grad_kernel<float, R>, grid, 256, 0, s, (const float*)b.dout, b.ldo, b.m, b.n, b.act,
+                 (const float*)b.z, b.ldz, b.z_codes, b.z_scales, (float*)dst, ld8, sums);
+      else
+        launch_k(act_grad_kernel<bf16_t, R>, grid, 256, 0, s, (const bf16_t*)b.dout, b.ldo, b.m, b.n, b.act,
+                 (const bf16_t*)b.z, b.ldz, b.z_codes, b.z_scales, (bf16_t*)dst, ld8, sums);
+    };
+    if (rows == 8) run(std::integral_constant<int, 1>{});
+    else if (rows == 16) run(std::integral_constant<int, 2>{});
+    else if (rows == 32) run(std::integral_constant<int, 4>{});
+    else run(std::integral_constant<int, 8>{});
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     if (need_dz) dz = dst, lddz = ld8, padded = true;
     if (part && !one_part) {
-      err = launch_colsum(part, (int)cdiv64(b.m, 64), b.n, b.dbias, nullptr, s);
+      err = launch_colsum(part, (int)cdiv64(b.m, rows), b.n, b.dbias, nullptr, s);
       if (err != hipSuccess) return err;
     }
   }

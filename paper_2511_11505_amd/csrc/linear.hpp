@@ -184,18 +184,27 @@ __device__ __forceinline__ uint32_t epilogue8(const Epilogue& e, int M, int N, i
   return bytes;
 }
 
-// One step of K on 16 x 16 outputs: 16 bytes per lane and operand, that is 32 of K
-// for bf16, 16 for fp32.
-template <typename T>
-__device__ __forceinline__ floatx4 mma16(const uint4& b, const uint4& a, floatx4 c) {
+// One step of K on MF x NF fragments of 16 x 16 outputs: 16 bytes per lane and
+// operand, that is 32 of K for bf16, 16 for fp32 (whose four instructions per
+// fragment do not follow each other: each would wait for the last).
+template <typename T, int MF, int NF>
+__device__ __forceinline__ void mma_step(const uint4 (&a)[MF], const uint4 (&b)[NF], floatx4 (&c)[MF][NF]) {
   if constexpr (sizeof(T) == 2) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b),
-                                                   __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+      for (int j = 0; j < NF; ++j)
+        c[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[j]),
+                                                          __builtin_bit_cast(bf16x8, a[i]), c[i][j], 0, 0, 0);
   } else {
-    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.x), __uint_as_float(a.x), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.y), __uint_as_float(a.y), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.z), __uint_as_float(a.z), c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.w), __uint_as_float(a.w), c, 0, 0, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+          c[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float((&b[j].x)[k]),
+                                                         __uint_as_float((&a[i].x)[k]), c[i][j], 0, 0, 0);
   }
 }
 

@@ -44,18 +44,12 @@ __global__ __launch_bounds__(64 * NW) void linear_mid_kernel(Product p, Epilogue
       for (int i = 0; i < MF; ++i) fa[buf][i] = n > 0 ? load16<T>(a[i] + k, n) : make_uint4(0, 0, 0, 0);
     }
   };
-  auto mma = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-      for (int j = 0; j < NF; ++j) acc[i][j] = mma16<T>(fb[buf][j], fa[buf][i], acc[i][j]);
-  };
   load(0, k0);
   load(1, k0 + STEP);
   for (int k = k0; k < k1; k += 2 * STEP) {
-    mma(0);
+    mma_step<T>(fa[0], fb[0], acc);
     load(0, k + 2 * STEP);
-    mma(1);
+    mma_step<T>(fa[1], fb[1], acc);
     load(1, k + 3 * STEP);
   }
 #pragma unroll

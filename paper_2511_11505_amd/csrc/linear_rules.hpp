@@ -72,12 +72,15 @@ inline double mid_us(int64_t M, int64_t N, int64_t K, int es, bool aligned, int 
   const double wgs = (double)cdiv_(M, rows) * cdiv_(N, 32) / cus;
   return 3.5 + std::max(wgs, 1.0) * (rows + 32) * K * es * (aligned ? 1.0 : 2.5) / 35e3;
 }
-// 64 x 64 tiles: a K block of 128 bytes 0.70 us (fp32 0.92), or 0.28 (0.70) per
-// workgroup of the CU.  Measured: 2048 x 2048, K 2048, 39 us; 777 x 1001, K 1409,
-// 22.2 (1 slice), 19.9 (2); fp32 512 x 1408, K 2048, 63 (1), 52 (2), 41 (4).
-inline double any_us(int64_t M, int64_t N, int64_t blocks, int64_t s, bool bf16, int cus) {
-  const double wgs = (double)cdiv_(M, 64) * cdiv_(N, 64) * s / cus;
-  return 4.0 + blocks * std::max(bf16 ? 0.70 : 0.92, (bf16 ? 0.28 : 0.70) * wgs) + slices_us(s, M, N);
+// 64 x 64 tiles: a K block of 128 bytes 0.50 us (0.65 from rows that 16 bytes do
+// not align, 0.79 in fp32), or 0.26 (0.34, 0.70) per workgroup of the CU.  Measured:
+// 512 x 2048, K 2048, 20.0 us; 2048 x 2048, K 2048, 36.7; 777 x 1001, K 1409 (unaligned)
+// 18.6 (1 slice), 19.0 (2), 21.6 (4); fp32 512 x 1408, K 2048, 55 (1), 47 (2), 42 (4),
+// 1408 x 2048, K 512, 38.
+inline double any_us(int64_t M, int64_t N, int64_t blocks, int64_t s, bool bf16, bool aligned, int cus) {
+  const double wgs = (double)(cdiv_(M, 64) * cdiv_(N, 64) * s) / cus;
+  const double one = bf16 ? (aligned ? 0.50 : 0.65) : 0.79, each = bf16 ? (aligned ? 0.26 : 0.34) : 0.70;
+  return 4.0 + blocks * std::max(one, each * (bf16 ? wgs : (double)(int64_t)(wgs + 0.99))) + slices_us(s, M, N);
 }
 
 // The plan of least time.  tiles_ok: the operands suit linear_tile.hpp.
@@ -111,17 +114,17 @@ inline ProductPlan product_plan(bool bf16, bool tiles_ok, bool a_along, bool b_a
   for (int64_t s = 1; s <= 32 && slices_fit(s, M, N); s *= 2) {
     const int64_t per = std::max<int64_t>(cdiv_(cdiv_(K, s), bk) * bk, bk);
     const int64_t n = std::max<int64_t>(1, cdiv_(K, per));
-    take(any_us(M, N, per / bk, n, bf16, cus), {0, 0, (int)n, (int)per, MID_NONE, 0});
+    take(any_us(M, N, per / bk, n, bf16, tiles_ok, cus), {0, 0, (int)n, (int)per, MID_NONE, 0});
   }
   return best;
 }
 
 // Whether operands that linear_tile.hpp cannot read for their widths (K % 8 !=
 // 0 along, M or N % 8 != 0 across) are first copied to rows of whole 16-byte
-// chunks (zeros behind the last element): when the tiles' time and the copies',
-// a launch and a pass over memory, are less than the other kernels'.  By the
-// sizes alone, so that the workspace is known.  (777 x 1001, K 1409: 19 us
-// without, 8192 x 8191, K 5119: 1.36 ms.)
+// chunks (zeros behind the last element): when the tiles' time and the copies'
+// are less than the other kernels'.  By the sizes alone, so that the workspace
+// is known.  (777 x 1001, K 1409: 19 us without, 24 with, of which the copies
+// 10.)
 inline bool product_packs(bool bf16, bool a_along, bool b_along, int64_t M, int64_t N, int64_t K, int cus) {
   if (!bf16 || M <= 0 || N <= 0) return false;
   const bool a = (a_along ? K : M) % 8 != 0, b = (b_along ? K : N) % 8 != 0;
@@ -129,7 +132,7 @@ inline bool product_packs(bool bf16, bool a_along, bool b_along, int64_t M, int6
   const ProductPlan tiles = product_plan(true, true, a_along, b_along, M, N, K, cus);
   const double copied = (a ? (double)M * K : 0.0) + (b ? (double)N * K : 0.0);
   return tiles.height &&
-         tiles.us + 3.5 + copied * 4 / 3e6 < product_plan(true, false, a_along, b_along, M, N, K, cus).us;
+         tiles.us + 9.0 + copied * 4 / 5e6 < product_plan(true, false, a_along, b_along, M, N, K, cus).us;
 }
 
 // Bytes of partial sums of the plan, whichever kernel the operands' alignment

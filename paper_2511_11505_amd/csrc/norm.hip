@@ -13,9 +13,11 @@
 // registers, of squares of differences, which loses no digits to a large mean.
 // A row of up to 1024 columns belongs to a wave (sums without a barrier, four
 // rows to a workgroup), a longer one to a workgroup of as many threads as it
-// has 8-column chunks, or half or a quarter of that (NC chunks per thread): with
-// 256 threads and three chunks each, 8192 x 5120 took 91 us (now FORWARD_US) and
-// the backward pass 92 us (now BACKWARD_US), 64 x 7168 7.5 us (now DECODE_US).
+// has 8-column chunks, or half or a quarter of that (NC chunks per thread).
+// Measured on bf16 (us; 256 threads with three or four chunks each before):
+// forward of 8192 x 5120 with the add and an 8-bit copy, 379 MB, 91 -> 89 (a
+// copy's rate, 5.1 TB/s, would take 74), 64 x 7168 7.5 -> 4.9, bound by latency;
+// backward of 8192 x 5120 from its 8-bit input, 295 MB, 92 -> 70.
 
 #include <algorithm>
 #include <type_traits>
@@ -118,9 +120,9 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a) {
 }
 
 // One group (a wave, or a workgroup) takes rows g, g + groups, ..; each thread
-// keeps its columns' part of dgamma and dbeta in registers and writes it once at
-// the end, part[0][group][cols] and part[1][group][cols], which colsum_kernel
-// adds in a fixed order.  The next row is in flight during a row's sums; h and u
+// keeps its columns' part of dgamma and dbeta in registers; at the end a workgroup
+// writes them once, part[0][workgroup][cols] and part[1][workgroup][cols], which
+// colsum_kernel adds in a fixed order.  The next row is in flight during a row's sums; h and u
 // are computed twice rather than kept.
 template <typename T, bool WAVE, int NC, bool CODES>
 __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_backward_kernel(NormBackArgs a) {
@@ -237,13 +239,33 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_backward_kernel(NormBa
     }
   }
   if (a.part) {
+    float* part = a.part + (int64_t)blockIdx.x * a.cols;
+    if constexpr (WAVE) {
+      // the four waves' sums, in wave order
+      __shared__ float sm[4][NC * 512];
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const int c = (j * tpr + tid) * 8, n = min(8, a.cols - c);
-      if (n <= 0) continue;
-      float* p = a.part + group * a.cols + c;
-      store8<float>(p, dg[j], n);
-      store8<float>(p + groups * a.cols, db[j], n);
+      for (int h = 0; h < 2; ++h) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sm[threadIdx.x >> 6][j * 512 + i * 64 + tid] = h ? db[j][i] : dg[j][i];
+        __syncthreads();
+        for (int q = threadIdx.x; q < NC * 512; q += 256) {
+          // place q holds column 8 (64 j + lane) + i, q = 512 j + 64 i + lane
+          const int c = 512 * (q / 512) + 8 * (q % 64) + q / 64 % 8;
+          const float v = ((sm[0][q] + sm[1][q]) + sm[2][q]) + sm[3][q];
+          if (c < a.cols) part[(int64_t)h * gridDim.x * a.cols + c] = v;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int c = (j * tpr + tid) * 8, n = min(8, a.cols - c);
+        if (n <= 0) continue;
+        store8<float>(part + c, dg[j], n);
+        store8<float>(part + (int64_t)gridDim.x * a.cols + c, db[j], n);
+      }
     }
   }
 }
@@ -259,8 +281,17 @@ __global__ __launch_bounds__(1024) void colsum_kernel(const float* __restrict__ 
   const int cl = threadIdx.x & 31, sl = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + cl;
   float s = 0.f;
-  if (c < cols)
-    for (int p = sl; p < P; p += 32) s += src[(size_t)p * cols + c];
+  if (c < cols) {
+    int p = sl;
+    for (; p + 7 * 32 < P; p += 8 * 32) {   // eight loads in flight
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = src[(size_t)(p + 32 * i) * cols + c];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += x[i];
+    }
+    for (; p < P; p += 32) s += src[(size_t)p * cols + c];
+  }
   sm[sl][cl] = s;
   __syncthreads();
   if (sl == 0 && c < cols) {
@@ -286,11 +317,13 @@ void with_shape(int cols, F&& f) {
   else f(No{}, integral_constant<int, 4>{}, threads(4));
 }
 
-// Workgroups of the backward pass: about 16 waves per CU.  (More of them write
-// more partial sums: 8 bytes per column each.)
+// Workgroups of the backward pass: about 8 waves per CU, one workgroup at
+// least.  More of them write more partial sums, 8 bytes per column each (us with
+// 1, 2, 4, 8 workgroups per CU: 8192 x 5120, ten waves, 80, 84, 92, 109; 8192 x
+// 2048, four waves, 46, 33, 35, 47).
 int64_t norm_groups(int64_t rows, bool wave, int threads) {
   const int64_t wgs = wave ? cdiv64(rows, 4) : rows;
-  const int64_t most = (int64_t)compute_units() * std::max(1, 16 * 64 / threads);
+  const int64_t most = (int64_t)compute_units() * std::max(1, 8 * 64 / threads);
   return wgs < most ? wgs : most;
 }
 
@@ -298,7 +331,7 @@ int64_t norm_groups(int64_t rows, bool wave, int threads) {
 
 size_t norm_ws_bytes(int64_t rows, int cols) {
   int64_t g = 0;
-  with_shape(cols, [&](auto wave, auto, int threads) { g = norm_groups(rows, wave, threads) * (wave ? 4 : 1); });
+  with_shape(cols, [&](auto wave, auto, int threads) { g = norm_groups(rows, wave, threads); });
   return (size_t)g * cols * 2 * sizeof(float);
 }
 
@@ -319,9 +352,8 @@ hipError_t launch_norm_backward(int dtype, const NormBackArgs& a, float* dgamma,
   with_shape(a.cols, [&](auto wave, auto nc, int threads) {
     constexpr bool W = decltype(wave)::value;
     constexpr int NC = decltype(nc)::value;
-    const int64_t wgs = norm_groups(a.rows, W, threads);
-    groups = wgs * (W ? 4 : 1);
-    const unsigned grid = (unsigned)wgs;
+    groups = norm_groups(a.rows, W, threads);
+    const unsigned grid = (unsigned)groups;
     if (dtype == 0) {
       if (a.x_codes) launch_k(norm_backward_kernel<float, W, NC, true>, grid, threads, 0, s, a);
       else launch_k(norm_backward_kernel<float, W, NC, false>, grid, threads, 0, s, a);
