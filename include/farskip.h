@@ -642,7 +642,8 @@ typedef struct {
   int32_t abi_version; /* FS_ABI_VERSION */
   int32_t dtype;       /* fs_dtype of a, w, residual, out, z and their gradients */
   int32_t act;         /* fs_act */
-  int32_t m, n, k;     /* m tokens, n outputs, k inputs */
+  int32_t m, n, k;     /* m tokens, n outputs, k inputs: each <= 2^24, every
+                          product of fewer than 2^24 tiles of 64 x 64 */
 } fs_linear_desc;
 
 /* Bytes of workspace: op FS_OP_LINEAR for fs_linear, FS_OP_LINEAR_BACKWARD for

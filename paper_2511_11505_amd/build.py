@@ -26,7 +26,7 @@ COMMON = [
 PER_FILE = {"router.hip": ["-ffp-contract=off"]}
 SOURCES = ["api.cpp", "router.hip", "dispatch.hip", "gemm.hip", "gemm_r64.hip", "gemm_r192_gateup.hip", "gemm_r192_down.hip",
            "gemm_r192_fp8.hip", "elementwise.hip", "fp8.hip",
-           "standin.hip", "api_layer.cpp", "linear.hip", "linear_few.hip", "linear_mid.hip", "linear_tile_fwd.hip",
+           "standin.hip", "api_layer.cpp", "linear.hip", "linear_any.hip", "linear_few.hip", "linear_mid.hip", "linear_tile_fwd.hip",
            "linear_tile_da.hip", "linear_tile_dw.hip", "norm.hip", "checkpoint.hip"]
 
 

@@ -28,10 +28,12 @@ fs_status check_mat(const Mat& m) {
   return FS_OK;
 }
 
-// Whether an output shares bytes with an input, where both are gapless (of
-// views with gaps the bytes between rows may be another's).
+// Whether an output shares bytes with an input: the same base, or where both
+// are gapless (of views with gaps the bytes between rows may be another's).
 bool overlap(const Mat& a, const Mat& b) {
-  if (!a.p || !b.p || a.ld != a.cols || b.ld != b.cols) return false;
+  if (!a.p || !b.p) return false;
+  if (a.p == b.p) return true;
+  if (a.ld != a.cols || b.ld != b.cols) return false;
   const char *x = (const char*)a.p, *y = (const char*)b.p;
   return x < y + b.rows * b.cols * b.es && y < x + a.rows * a.cols * a.es;
 }
@@ -97,6 +99,8 @@ fs_status check_linear(const fs_linear_desc* d) {
   TRY(check_dtype(d->dtype));
   if (d->act < FS_ACT_NONE || d->act > FS_ACT_SILU) return fail(FS_ERR_INVALID, "act must be an fs_act");
   if (d->m < 0 || d->n <= 0 || d->k <= 0) return fail(FS_ERR_INVALID, "m >= 0, n > 0, k > 0 required");
+  if (d->m > (1 << 24) || d->n > (1 << 24) || d->k > (1 << 24))
+    return fail(FS_ERR_UNSUPPORTED, "m, n and k must be <= 2^24");
   if (!grid_ok(d->m, d->n) || !grid_ok(d->m, d->k) || !grid_ok(d->n, d->k))
     return fail(FS_ERR_UNSUPPORTED, "m, n, k: a product of more than 2^24 tiles of 64 x 64");
   return FS_OK;
@@ -170,6 +174,8 @@ fs_status fs_linear(const fs_linear_desc* d, const void* a, int64_t lda, const v
     if (!(out == residual && ldo == ldr)) TRY(no_overlap(O, R));
     TRY(no_overlap(Z, R));
     TRY(no_overlap(Z, O));
+    for (const Mat& x : {outs[2], outs[3]})
+      for (const Mat& y : {R, O, Z}) TRY(no_overlap(x, y));
     const size_t need = fs::linear_ws_bytes(dt(d->dtype), d->m, d->n, d->k);
     if (ws_bytes < need)
       return fail(FS_ERR_WORKSPACE, "workspace smaller than fs_linear_workspace(FS_OP_LINEAR)");
@@ -265,6 +271,8 @@ fs_status fs_layer_norm(const fs_norm_desc* d, const void* x, int64_t ldx, const
       for (const Mat& i : {X, ADD})
         if (!(o.p == i.p && o.ld == i.ld)) TRY(no_overlap(o, i));
     TRY(no_overlap(SUM, Y));
+    for (const Mat& o : {codes_of(save_in, "save_in", r, c), codes_of(save_y, "save_y", r, c)})
+      for (const Mat& i : {X, ADD, SUM, Y}) TRY(no_overlap(o, i));
     TRY(check_stream(stream));
     fs::NormArgs g{};
     g.rows = r, g.cols = d->cols, g.center = d->center, g.eps = d->eps;

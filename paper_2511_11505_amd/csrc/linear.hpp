@@ -49,6 +49,16 @@ typedef void TileLaunch(const Product& p, const Epilogue& e, const TileGrid& g, 
                         hipStream_t s);
 TileLaunch launch_tile_forward, launch_tile_da, launch_tile_dw;
 
+// 64 x 64 tiles for everything (linear_any.hip): K in `slices` of `per` elements,
+// the sums of more than one to part; both products of a small backward pass in
+// one launch; the sum of the slices with the epilogue.
+void launch_any(int dtype, const Product& p, const Epilogue& e, int slices, int per, float* part, int np,
+                hipStream_t s);
+void launch_any_pair(int dtype, const Product& da, const Epilogue& eda, const Product& dw, const Epilogue& edw,
+                     hipStream_t s);
+void launch_reduce(int dtype, const float* part, int slices, int M, int N, int np, const Epilogue& e,
+                   hipStream_t s);
+
 // Forward products of up to kFewTokens rows (linear_few.hip).
 constexpr int kFewTokens = 8;
 void launch_few(int dtype, const Product& p, const Epilogue& e, int cus, hipStream_t s);

@@ -105,7 +105,8 @@ inline ProductPlan product_plan(bool bf16, bool tiles_ok, bool a_along, bool b_a
       take(small_us(M, N, per, n, cus), {64, 128, (int)n, (int)per, MID_NONE, 0});
     }
   }
-  if (a_along && b_along) {
+  // (a grid holds fewer than 2^32 threads, 512 of a workgroup here)
+  if (a_along && b_along && cdiv_(M, 16) * cdiv_(N, 32) < (1 << 22)) {
     take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 16), {0, 0, 1, 0, MID_16, 0});
     take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 32), {0, 0, 1, 0, MID_32, 0});
     take(mid_us(M, N, K, bf16 ? 2 : 4, tiles_ok, cus, 64), {0, 0, 1, 0, MID_64, 0});

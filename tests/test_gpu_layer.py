@@ -497,6 +497,76 @@ def test_checkpoint_edges(dtype):
     assert np.array_equal(f64(back), O.restore(*want), equal_nan=True)
 
 
+# ------------------------------------------- offsets that pass 32 bits
+def test_offsets_past_32_bits():
+    """The last rows of matrices of more than 2^32 elements are what the same
+    rows give alone."""
+    m, d, tail = (1 << 19) + 70, 8200, 37
+    g = gen(8)
+    x = torch.zeros((m, d), dtype=torch.bfloat16, device=DEV)
+    x[-tail:] = torch.randn((tail, d), generator=g, device=DEV).bfloat16()
+    assert x.numel() > 1 << 32
+    # checkpoint and back
+    c, small = fs.checkpoint_buffers(m, d), fs.checkpoint_buffers(tail, d)
+    fs.fs_checkpoint_fp8(L.FS_BF16, m, d, x, *c)
+    fs.fs_checkpoint_fp8(L.FS_BF16, tail, d, x[-tail:], *small)
+    assert torch.equal(c[0][-tail:], small[0]) and torch.equal(c[1][-tail:], small[1])
+    y = torch.empty_like(x)
+    fs.fs_checkpoint_restore(L.FS_BF16, m, d, *c, y)
+    part = torch.empty((tail, d), dtype=torch.bfloat16, device=DEV)
+    fs.fs_checkpoint_restore(L.FS_BF16, tail, d, *small, part)
+    assert torch.equal(y[-tail:], part)
+    # norm and its backward pass
+    mean, rstd = torch.empty((m,), device=DEV), torch.empty((m,), device=DEV)
+    big, few = fs.norm_desc(m, d), fs.norm_desc(tail, d)
+    fs.fs_layer_norm(big, x, None, None, None, None, y, mean, rstd)
+    fs.fs_layer_norm(few, x[-tail:], None, None, None, None, part, None, None)
+    assert torch.equal(y[-tail:], part)
+    dg, dg2 = torch.empty((d,), device=DEV), torch.empty((d,), device=DEV)
+    xr = torch.empty_like(part)
+    fs.fs_checkpoint_restore(L.FS_BF16, tail, d, *small, xr)
+    terms = (part.double() * (xr.double() - mean[-tail:, None]) * rstd[-tail:, None]).abs().sum(0)
+    ws = torch.empty((fs.fs_layer_norm_workspace(big),), dtype=torch.uint8, device=DEV)
+    fs.fs_layer_norm_backward(big, y, c, mean, rstd, None, x, y, dg, None, ws)
+    fs.fs_layer_norm_backward(few, part, small, mean[-tail:], rstd[-tail:], None, x[-tail:], part, dg2, None, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(y[-tail:], part)
+    # the same 37 terms in two orders (the rows before add exact zeros): each
+    # order rounds at most 36 sums, and each term at most 3 times (a difference,
+    # two products), by half a step (U / 2) of at most the terms' absolute sum
+    assert ((dg - dg2).abs().double() <= 2 * (tail + 3) * U / 2 * terms).all()
+
+
+@pytest.mark.parametrize("k", [40, 264])
+def test_linear_offsets_past_32_bits(k):
+    """As above, with more output elements than 2^32: tokens that are zeros
+    but for the last rows."""
+    m, n, tail = (1 << 19) + 70, 8200, 37
+    g = gen(9)
+    a = torch.zeros((m, k), dtype=torch.bfloat16, device=DEV)
+    a[-tail:] = torch.randn((tail, k), generator=g, device=DEV).bfloat16()
+    w = torch.randn((n, k), generator=g, device=DEV).bfloat16()
+    desc = fs.linear_desc(m, n, k, "bf16", "relu")
+    out = torch.empty((m, n), dtype=torch.bfloat16, device=DEV)
+    z = fs.checkpoint_buffers(m, n)
+    ws = torch.empty((max(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR), 256),), dtype=torch.uint8, device=DEV)
+    fs.fs_linear(desc, a, w, None, None, out, ws, save_z=z)
+    Z = f64(a[-tail:]) @ f64(w).T
+    err = (k + 2) * U * (np.abs(f64(a[-tail:])) @ np.abs(f64(w)).T)
+    near(f64(out[-tail:]), np.maximum(Z, 0), err + HALF["bf16"] * (np.abs(Z) + err))
+    # the gradients of zero rows are zeros; of the last, the small call's
+    ws = torch.empty((fs.fs_linear_workspace(desc, L.FS_OP_LINEAR_BACKWARD),), dtype=torch.uint8, device=DEV)
+    da, dw = torch.empty_like(a), torch.empty_like(w)
+    fs.fs_linear_backward(desc, out, a, w, z, da, dw, None, ws)
+    torch.cuda.synchronize()
+    zt = O.restore(*(t[-tail:].cpu().numpy() for t in z))
+    G = f64(out[-tail:]) * (zt > 0)
+    wa, ww = G @ f64(w), G.T @ f64(a[-tail:])
+    near(f64(da[-tail:]), wa, (n + 2) * U * (np.abs(G) @ np.abs(f64(w))) + HALF["bf16"] * 1.01 * np.abs(wa))
+    near(f64(dw), ww, (tail + 40) * U * (np.abs(G).T @ np.abs(f64(a[-tail:]))) + HALF["bf16"] * 1.01 * np.abs(ww))
+    assert float(da[:-tail].abs().max()) == 0.0
+
+
 # ------------------------------------------------------------ used together
 def sublayer_oracle(x, dout, p, act, center, rounded, coded):
     """Forward and gradients of DenseSublayer with its roundings."""
@@ -596,6 +666,39 @@ def test_sublayer_in_a_graph_and_on_a_side_stream(n):
         assert torch.equal(out, eout)
         for k in grads:
             assert torch.equal(grads[k], egrads[k]), k
+
+
+def test_two_sublayers_at_once():
+    """Two sublayers' passes on two streams, captured into two graphs that are
+    replayed together, are what each gives alone."""
+    runs = []
+    for i, (n, d, f) in enumerate(((300, 256, 1032), (257, 520, 776))):
+        p, layer, x, dout, grads = make_sublayer(n, d, f, "bf16", "silu", True, "codes", seed=i)
+        out = torch.empty_like(x)
+
+        def step(layer=layer, x=x, out=out, dout=dout, grads=grads):
+            layer.forward(x, out)
+            layer.backward(dout, grads)
+
+        step()
+        torch.cuda.synchronize()
+        want = [out.clone(), *(grads[k].clone() for k in sorted(grads))]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        runs.append((graph, torch.cuda.Stream(), want, out, grads, step))
+    for way in ("graphs", "streams"):
+        for _ in range(4):
+            for graph, stream, want, out, grads, step in runs:
+                stream.wait_stream(torch.cuda.current_stream())
+                with torch.cuda.stream(stream):
+                    graph.replay() if way == "graphs" else step()
+            torch.cuda.synchronize()
+            for _, _, want, out, grads, _ in runs:
+                got = [out, *(grads[k] for k in sorted(grads))]
+                assert all(torch.equal(a, b) for a, b in zip(got, want)), way
+                for t in got:
+                    t.zero_()
 
 
 def test_sublayer_in_the_far_skip_window():

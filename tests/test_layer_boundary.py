@@ -34,7 +34,8 @@ def lin(m=8, n=16, k=24, act="none", **kw):
     (dict(abi_version=1), L.FS_ERR_INVALID), (dict(dtype=2), L.FS_ERR_INVALID),
     (dict(act=4), L.FS_ERR_INVALID), (dict(act=-1), L.FS_ERR_INVALID), (dict(m=-1), L.FS_ERR_INVALID),
     (dict(n=0), L.FS_ERR_INVALID), (dict(k=0), L.FS_ERR_INVALID),
-    (dict(m=2 ** 31 - 1, n=2 ** 31 - 1), L.FS_ERR_UNSUPPORTED)])
+    (dict(m=2 ** 24 + 1), L.FS_ERR_UNSUPPORTED), (dict(n=2 ** 31 - 1), L.FS_ERR_UNSUPPORTED),
+    (dict(m=2 ** 20, n=2 ** 20), L.FS_ERR_UNSUPPORTED)])
 def test_linear_descriptor(kw, status):
     d = lin(**kw)
     refuse(status, "", fs.fs_linear, d, A, B, None, None, C, BIG)
@@ -69,6 +70,18 @@ def test_linear_row_strides():
         st = lib.fs_linear(ctypes.byref(d), A, lda, B, ldw, None, D, ldr, C, ldo, *ok, None, 0, None)
         assert st == L.FS_ERR_INVALID, i
         assert b"row stride" in lib.fs_last_error_message()
+
+
+def test_in_place_needs_the_same_stride():
+    """An output on an input's base with another stride is refused."""
+    lib, d, n = L.load(), lin(), norm()
+    st = lib.fs_linear(ctypes.byref(d), A, 24, B, 24, None, C, 20, C, 16, None, None, None, 0, None)
+    assert st == L.FS_ERR_INVALID and b"overlap" in lib.fs_last_error_message()
+    st = lib.fs_layer_norm(ctypes.byref(n), A, 48, None, 0, None, None, None, 0, A, 40, None, None, None, None, None)
+    assert st == L.FS_ERR_INVALID and b"overlap" in lib.fs_last_error_message()
+    refuse(L.FS_ERR_INVALID, "overlap", fs.fs_linear, d, A, B, None, None, C, BIG, save_z=(C, D))
+    refuse(L.FS_ERR_INVALID, "overlap", fs.fs_layer_norm, n, A, None, None, None, None, B, None, None,
+           save_in=(A, C))
 
 
 def test_linear_empty():

@@ -19,7 +19,8 @@ def sizes(n, seed=1):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_plans_hold_what_the_kernels_need(kind, dtype):
-    for M, N, K in list(sizes(1500)) + [(1, 1, 1), (1, 1, 1 << 20), (1 << 20, 8, 8), (64, 64, 193), (64, 64, 192)]:
+    for M, N, K in list(sizes(1500)) + [(1, 1, 1), (1, 1, 1 << 20), (1 << 20, 8, 8), (64, 64, 193), (64, 64, 192),
+                                          (1 << 24, 2048, 8), (2048, 1 << 24, 8)]:
         for ok in (False, True):
             for cus in (R.CUS, 304, 8):
                 p = R.plan(kind, M, N, K, dtype, ok, cus)
@@ -36,6 +37,7 @@ def test_plans_hold_what_the_kernels_need(kind, dtype):
                     assert p.per >= 4 and 4 <= blocks - p.per * (p.slices - 1) <= p.per
                 elif p.mid:
                     assert kind == R.FORWARD and p.slices == 1 and p.mid in (1, 2, 3)
+                    assert -(-M // (8 << p.mid)) * -(-N // 32) * 512 < 2 ** 32
                 else:
                     bk = 64 if dtype == "bf16" else 32
                     assert p.per % bk == 0 and p.per * (p.slices - 1) < K <= p.per * p.slices
