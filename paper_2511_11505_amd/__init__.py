@@ -4,10 +4,14 @@ The hot path is libfarskip.so (C ABI in include/farskip.h): router and top-k,
 dispatch plan and pack, grouped SwiGLU experts on MFMA, Combine with the
 deferred FarSkip residual add, and the two-phase block driver; for the
 replicated-activation inference variant, the local rows, the gathered
-expert GEMMs, the partial Combine and the all-reduce stand-in.  This package
+expert GEMMs, the partial Combine and the all-reduce stand-in.  Beside it
+stand the operators of the dense sublayer in the far-skip window, with their
+backward passes: the linear with its epilogue, the norm with the deferred
+add, and 8-bit checkpoints of activations.  This package
 is its ctypes binding plus small owners of device buffers that order the
 calls: one block (block.py), stacked layers in the two-window schedule
-(stack.py) and stacked replicated-activation layers (replicated.py).
+(stack.py), stacked replicated-activation layers (replicated.py) and the
+dense sublayer (sublayer.py).
 """
 
 from . import _lib  # noqa: F401

@@ -11,7 +11,8 @@
 //             copies so that the reads cover every bank once: along, chunk c of
 //             row r sits at c ^ ((r / 2) % 8); across, the 32 bytes of columns
 //             16 c .. of row k sit at c ^ s(k), s = bits 1 and 3 of k.
-//             Products with few tiles take 64 x 128, two workgroups per CU, and K cut into slices whose sums a second kernel adds.
+//             Products with few tiles take 64 x 128, two workgroups per CU, and
+//             K cut into slices whose sums a second kernel adds.
 //   Ring      Two 64-wide LDS slots for A, three for B (160 KB at 256
 //             rows); one barrier per block.  The copies run on from tile to tile.
 //   Tail      K % 64 != 0: chunks past K are copied from 16 zero bytes.
