@@ -33,7 +33,7 @@ fs_status check_mat(const Mat& m) {
 bool overlap(const Mat& a, const Mat& b) {
   if (!a.p || !b.p) return false;
   if (a.p == b.p) return true;
-  if (a.ld != a.cols || b.ld != b.cols) return false;
+  if ((a.rows > 1 && a.ld != a.cols) || (b.rows > 1 && b.ld != b.cols)) return false;
   const char *x = (const char*)a.p, *y = (const char*)b.p;
   return x < y + b.rows * b.cols * b.es && y < x + a.rows * a.cols * a.es;
 }
@@ -41,6 +41,21 @@ fs_status no_overlap(const Mat& out, const Mat& in) {
   if (overlap(out, in)) return fail(FS_ERR_INVALID, std::string(out.name) + " and " + in.name + " overlap");
   return FS_OK;
 }
+
+// Outputs share bytes with no input and not with each other.
+template <size_t NO, size_t NI>
+fs_status check_apart(const Mat (&outs)[NO], const Mat (&ins)[NI]) {
+  for (size_t i = 0; i < NO; ++i) {
+    for (const Mat& in : ins)
+      if (overlap(outs[i], in)) return no_overlap(outs[i], in);
+    for (size_t j = i + 1; j < NO; ++j)
+      if (overlap(outs[i], outs[j])) return no_overlap(outs[i], outs[j]);
+  }
+  return FS_OK;
+}
+Mat vec_of(const float* p, const char* name, int64_t n) { return {name, p, 1, n, n, 4}; }
+// (bytes of a workspace that are not used: not there)
+Mat ws_of(const void* ws, size_t need) { return {"ws", need ? ws : nullptr, 1, (int64_t)need, (int64_t)need, 1}; }
 
 int64_t blocks_of(int64_t cols) { return (cols + 31) / 32; }
 
@@ -62,6 +77,9 @@ Mat rows_of(const fs_saved* s, const char* name, int64_t rows, int64_t cols, siz
 }
 Mat codes_of(const fs_saved* s, const char* name, int64_t rows, int64_t cols) {
   return {name, s ? s->codes : nullptr, rows, cols, cols, 1};
+}
+Mat scales_of(const fs_saved* s, const char* name, int64_t rows, int64_t cols) {
+  return {name, s && s->codes ? s->scales : nullptr, rows, blocks_of(cols), blocks_of(cols), 1};
 }
 
 #define TRY(expr)                 \
@@ -166,20 +184,19 @@ fs_status fs_linear(const fs_linear_desc* d, const void* a, int64_t lda, const v
     OPT4(bias, "bias");
     TRY(check_saved(save_z, "save_z", m, n, es, false, false));
     TRY(check_saved(save_out, "save_out", m, n, es, false, true));
-    const Mat Z = rows_of(save_z, "save_z", m, n, es);
-    const Mat outs[] = {O, Z, codes_of(save_z, "save_z", m, n), codes_of(save_out, "save_out", m, n)};
-    for (const Mat& x : outs)
-      for (const Mat& y : {A, W}) TRY(no_overlap(x, y));
-    // (out may be residual itself: each element is read before it is written)
-    if (!(out == residual && ldo == ldr)) TRY(no_overlap(O, R));
-    TRY(no_overlap(Z, R));
-    TRY(no_overlap(Z, O));
-    for (const Mat& x : {outs[2], outs[3]})
-      for (const Mat& y : {R, O, Z}) TRY(no_overlap(x, y));
     const size_t need = fs::linear_ws_bytes(dt(d->dtype), d->m, d->n, d->k);
     if (ws_bytes < need)
       return fail(FS_ERR_WORKSPACE, "workspace smaller than fs_linear_workspace(FS_OP_LINEAR)");
     if (need) NEED(ws, "ws");
+    const Mat Z = rows_of(save_z, "save_z", m, n, es);
+    const Mat outs[] = {O, Z, codes_of(save_z, "save_z", m, n), scales_of(save_z, "save_z", m, n),
+                        codes_of(save_out, "save_out", m, n), scales_of(save_out, "save_out", m, n),
+                        ws_of(ws, need)};
+    const Mat ins[] = {A, W, vec_of(bias, "bias", n)};
+    TRY(check_apart(outs, ins));
+    // (out may be residual itself: each element is read before it is written)
+    for (const Mat& x : outs)
+      if (!(x.p == O.p && out == residual && ldo == ldr)) TRY(no_overlap(x, R));
     TRY(check_stream(stream));
     fs::LinearOut o{bias, d->act, residual, ldr, out, ldo, nullptr, 0, nullptr, nullptr, nullptr, nullptr};
     if (save_z) o.z = save_z->rows, o.ldz = save_z->ld, o.z_codes = save_z->codes, o.z_scales = save_z->scales;
@@ -216,16 +233,14 @@ fs_status fs_linear_backward(const fs_linear_desc* d, const void* dout, int64_t 
     }
     if (dw) TRY(check_mat(DW));
     OPT4(dbias, "dbias");
-    if (m > 0)
-      for (const Mat& x : {DA, DW})
-        for (const Mat& y : {G, W, rows_of(a, "a", m, k, es), codes_of(a, "a", m, k),
-                             rows_of(z, "z", m, n, es), codes_of(z, "z", m, n)})
-          TRY(no_overlap(x, y));
-    TRY(no_overlap(DA, DW));
     const size_t need = fs::linear_backward_ws_bytes(dt(d->dtype), d->act, d->m, d->n, d->k);
     if (ws_bytes < need)
       return fail(FS_ERR_WORKSPACE, "workspace smaller than fs_linear_workspace(FS_OP_LINEAR_BACKWARD)");
     if (need) NEED(ws, "ws");
+    const Mat outs[] = {DA, DW, vec_of(dbias, "dbias", n), ws_of(ws, need)};
+    const Mat ins[] = {G, W, rows_of(a, "a", m, k, es), codes_of(a, "a", m, k), scales_of(a, "a", m, k),
+                       rows_of(z, "z", m, n, es), codes_of(z, "z", m, n), scales_of(z, "z", m, n)};
+    if (m > 0) TRY(check_apart(outs, ins));
     TRY(check_stream(stream));
     fs::LinearBack b{};
     b.act = d->act, b.m = d->m, b.n = d->n, b.k = d->k;
@@ -266,13 +281,15 @@ fs_status fs_layer_norm(const fs_norm_desc* d, const void* x, int64_t ldx, const
       OPT4(p, "gamma, beta, mean and rstd");
     TRY(check_saved(save_in, "save_in", r, c, es, false, true));
     TRY(check_saved(save_y, "save_y", r, c, es, false, true));
-    // (an output may be an input itself: a row is read before it is written)
-    for (const Mat& o : {SUM, Y})
+    const Mat outs[] = {SUM, Y, vec_of(mean, "mean", r), vec_of(rstd, "rstd", r),
+                        codes_of(save_in, "save_in", r, c), scales_of(save_in, "save_in", r, c),
+                        codes_of(save_y, "save_y", r, c), scales_of(save_y, "save_y", r, c)};
+    const Mat ins[] = {vec_of(gamma, "gamma", c), vec_of(beta, "beta", c)};
+    TRY(check_apart(outs, ins));
+    // (sum_out and y may be an input itself: a row is read before it is written)
+    for (const Mat& o : outs)
       for (const Mat& i : {X, ADD})
-        if (!(o.p == i.p && o.ld == i.ld)) TRY(no_overlap(o, i));
-    TRY(no_overlap(SUM, Y));
-    for (const Mat& o : {codes_of(save_in, "save_in", r, c), codes_of(save_y, "save_y", r, c)})
-      for (const Mat& i : {X, ADD, SUM, Y}) TRY(no_overlap(o, i));
+        if (!((o.p == sum_out || o.p == y) && o.p == i.p && o.ld == i.ld)) TRY(no_overlap(o, i));
     TRY(check_stream(stream));
     fs::NormArgs g{};
     g.rows = r, g.cols = d->cols, g.center = d->center, g.eps = d->eps;
@@ -306,17 +323,20 @@ fs_status fs_layer_norm_backward(const fs_norm_desc* d, const void* dy, int64_t 
       NEED4(rstd, "rstd");
       if (d->center) NEED4(mean, "mean");
       OPT4(gamma, "gamma");
-      // (dx may be dy or dres itself: a row is read before it is written)
-      for (const Mat& i : {DY, DR})
-        if (!(i.p == dx && i.ld == lddx)) TRY(no_overlap(DX, i));
-      TRY(no_overlap(DX, rows_of(x, "x", r, c, es)));
-      TRY(no_overlap(DX, codes_of(x, "x", r, c)));
     }
     const bool grads = dgamma || dbeta;
-    if (grads) {
-      const size_t need = fs::norm_ws_bytes(r, d->cols);
-      if (ws_bytes < need) return fail(FS_ERR_WORKSPACE, "workspace smaller than fs_layer_norm_workspace");
-      if (need) NEED(ws, "ws");
+    const size_t need = grads ? fs::norm_ws_bytes(r, d->cols) : 0;
+    if (ws_bytes < need) return fail(FS_ERR_WORKSPACE, "workspace smaller than fs_layer_norm_workspace");
+    if (need) NEED(ws, "ws");
+    if (r > 0) {
+      const Mat outs[] = {DX, vec_of(dgamma, "dgamma", c), vec_of(dbeta, "dbeta", c), ws_of(ws, need)};
+      const Mat ins[] = {rows_of(x, "x", r, c, es), codes_of(x, "x", r, c), scales_of(x, "x", r, c),
+                         vec_of(mean, "mean", r), vec_of(rstd, "rstd", r), vec_of(gamma, "gamma", c)};
+      TRY(check_apart(outs, ins));
+      // (dx may be dy or dres itself: a row is read before it is written)
+      for (const Mat& o : outs)
+        for (const Mat& i : {DY, DR})
+          if (!(o.p == dx && i.p == dx && i.ld == lddx)) TRY(no_overlap(o, i));
     }
     if (r == 0 && !grads) return FS_OK;
     TRY(check_stream(stream));

@@ -11,7 +11,8 @@ passes.  With ``save="codes"`` the activations that the backward pass reads (x,
 h, the pre-activation and u) are kept as 8-bit checkpoints, written by the
 passes that compute them; with "rows" as they are; with None (serving) not at
 all.  All arithmetic runs in the library's kernels; torch only allocates
-memory.
+memory.  A sublayer's passes share its buffers and its workspace, so they run
+one after another, on one stream or ordered by events.
 """
 
 import torch

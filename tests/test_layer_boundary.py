@@ -169,3 +169,31 @@ def test_binding_refuses_what_the_library_cannot_see():
         fs.DenseSublayer(4, None, None, torch.zeros(6, 4), None, torch.zeros(6, 4), None)
     with pytest.raises(ValueError):
         fs.DenseSublayer(4, None, None, torch.zeros(6, 4), None, torch.zeros(4, 6), None, save="fp8")
+
+
+def test_outputs_lie_apart():
+    """Vectors, scale bytes, checkpoints and the workspace, too, lie apart from
+    every input and from each other."""
+    lib, d, big, n = L.load(), lin(), lin(1, 16, 4096), norm()
+    fwd, bwd, ln, lnb = fs.fs_linear, fs.fs_linear_backward, fs.fs_layer_norm, fs.fs_layer_norm_backward
+    INV, text = L.FS_ERR_INVALID, "overlap"
+    refuse(INV, text, fwd, d, A, B, C, None, C, BIG)                                  # out, bias
+    refuse(INV, text, fwd, d, A, B, None, None, C, BIG, save_z=(D, C))                # out, scales
+    refuse(INV, text, fwd, d, A, B, None, None, C, BIG, save_z=(D, E), save_out=(D, E + 64))
+    refuse(INV, text, fwd, d, A, B, None, None, C, BIG, save_z=(D, E), save_out=(D + 4096, E))
+    refuse(INV, text, fwd, d, A, B, None, D, C, BIG, save_z=(D + 16, E))              # residual, codes
+    refuse(INV, text, fwd, big, A, B, None, None, C, (B + 64, 1 << 60))               # w, ws
+    refuse(INV, text, bwd, d, A, B, C, None, D, E, E + 4, BIG)                        # dw, dbias
+    refuse(INV, text, bwd, d, A, (B, E), C, None, D, E, None, BIG)                    # dw, a's scales
+    refuse(INV, text, bwd, lin(act="gelu"), A, B, C, D, E, None, None, (D, 1 << 60))  # z, ws
+    refuse(INV, text, ln, n, A, None, None, None, None, B, C, C + 4)                  # mean, rstd
+    refuse(INV, text, ln, n, A, None, B + 8, None, None, B, None, None)               # y, gamma
+    refuse(INV, text, ln, n, A, None, None, None, None, A, None, None, save_y=(A, B))
+    refuse(INV, text, lnb, n, A, B, C, D, None, None, E, E + 4, None, BIG)            # dx, dgamma
+    refuse(INV, text, lnb, n, A, B, C, D, None, None, C, None, None, BIG)             # dx, mean
+    refuse(INV, text, lnb, n, A, B, C, D, None, None, E, D, None, BIG)                # dgamma, rstd
+    refuse(INV, text, lnb, n, A, B, C, D, None, None, E, E + 4096, None, (A, 1 << 60))
+    # one row's stride says nothing about gaps
+    one = lin(1)
+    st = lib.fs_linear(ctypes.byref(one), A, 100, B, 24, None, None, 0, A + 40, 50, None, None, None, 0, None)
+    assert st == INV and b"overlap" in lib.fs_last_error_message()
