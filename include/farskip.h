@@ -621,7 +621,7 @@ typedef struct {
   void* rows;       /* [rows, cols] dtype with row stride ld, or NULL */
   int64_t ld;
   uint8_t* codes;   /* [rows, cols], or NULL */
-  uint8_t* scales;  /* [rows, ceil(cols / 32)] */
+  uint8_t* scales;  /* [rows, ceil(cols / 32)]; not read or written without codes */
 } fs_saved;
 
 /* Rows to a checkpoint, and back (dst gets the values it stands for).

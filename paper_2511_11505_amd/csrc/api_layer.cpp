@@ -199,7 +199,9 @@ fs_status fs_linear(const fs_linear_desc* d, const void* a, int64_t lda, const v
       if (!(x.p == O.p && out == residual && ldo == ldr)) TRY(no_overlap(x, R));
     TRY(check_stream(stream));
     fs::LinearOut o{bias, d->act, residual, ldr, out, ldo, nullptr, 0, nullptr, nullptr, nullptr, nullptr};
-    if (save_z) o.z = save_z->rows, o.ldz = save_z->ld, o.z_codes = save_z->codes, o.z_scales = save_z->scales;
+    if (save_z) o.z = save_z->rows, o.ldz = save_z->ld, o.z_codes = save_z->codes;
+    // (scales without codes are not part of the call: the checks above left them out)
+    if (o.z_codes) o.z_scales = save_z->scales;
     if (save_out) o.out_codes = save_out->codes, o.out_scales = save_out->scales;
     fs::prof_begin(FS_K_DENSE, S(stream));
     const hipError_t e =

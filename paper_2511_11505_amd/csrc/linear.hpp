@@ -23,7 +23,8 @@ struct Product {
 };
 
 // z = product + bias;  out = act(z) + residual, rounded once.  z and out may
-// also be kept as checkpoints of their rounded values.
+// also be kept as checkpoints of their rounded values (scales: null without
+// codes).
 struct Epilogue {
   const float* bias;
   const void* res;

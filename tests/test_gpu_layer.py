@@ -727,3 +727,27 @@ def test_sublayer_in_the_far_skip_window():
     both = f64(nxt) + f64(routed)
     near(f64(out), both, 4 * U * (np.abs(f64(nxt)) + np.abs(f64(routed))))
     blk.close()
+
+
+# --------------------------------------------- arguments that are left alone
+# (a size for each kernel that ends in the epilogue: few tokens, waves that
+# split K, 64 x 64 tiles, 64 x 128 tiles with and without slices, 128 x 256 tiles)
+@pytest.mark.parametrize("m,n,k", [(3, 96, 520), (64, 512, 512), (130, 72, 1000), (300, 1001, 1409), (128, 4096, 4096),
+                                   (520, 2056, 2056), (4096, 2048, 256)])
+def test_scales_without_codes_are_left_alone(m, n, k):
+    """z saved as rows, in a struct whose scales are set: they stay as they
+    were, and the call gives what it gives without them."""
+    g = gen(m + n)
+    a, w = mat(g, m, k, "bf16"), mat(g, n, k, "bf16", 0, k ** -0.5)
+    desc = fs.linear_desc(m, n, k, "bf16", "silu")
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR))
+    scales = torch.full((m, (n + 31) // 32), 0x5A, dtype=torch.uint8, device=DEV)
+    got = []
+    for extra in (None, scales.data_ptr()):
+        out, z = Out(m, n, "bf16"), Out(m, n, "bf16")
+        save_z = fs.fs_saved(z.view.data_ptr(), z.view.stride(0), None, extra)
+        fs.fs_linear(desc, a, w, None, None, out.view, wp, save_z=save_z)
+        torch.cuda.synchronize()
+        got.append((out.get(), z.get()))
+    assert bool((scales == 0x5A).all())
+    assert all(np.array_equal(p, q) for p, q in zip(*got))
