@@ -443,6 +443,18 @@ def _flat(t, name, dtype, shape, dev):
     return t.data_ptr()
 
 
+def _space(ws, dev):
+    """(address, bytes) of the workspace: a gapless tensor on the current GPU,
+    an (address, bytes) pair, or None."""
+    if ws is None or isinstance(ws, tuple):
+        return _ws(ws)
+    if not ws.is_contiguous():
+        _bad("ws", "contiguous")
+    if ws.get_device() != dev:
+        _bad("ws", "on the current GPU")
+    return _ws(ws)
+
+
 def _codes(pair, name, rows, cols, dev):
     """Addresses of a checkpoint's codes and scales."""
     codes, scales = pair
@@ -481,7 +493,7 @@ def fs_linear_workspace(desc, op):
 def fs_linear(desc, a, w, bias, residual, out, ws, save_z=None, save_out=None, stream=None):
     dev, s = _here(stream)
     dt, m, n, k = desc.dtype, desc.m, desc.n, desc.k
-    wp, wb = _ws(ws)
+    wp, wb = _space(ws, dev)
     ap, lda = _mat(a, "a", dt, m, k, dev)
     bp, ldb = _mat(w, "w", dt, n, k, dev)
     rp, ldr = _mat(residual, "residual", dt, m, n, dev)
@@ -494,7 +506,7 @@ def fs_linear(desc, a, w, bias, residual, out, ws, save_z=None, save_out=None, s
 def fs_linear_backward(desc, dout, a, w, z, da, dw, dbias, ws, stream=None):
     dev, s = _here(stream)
     dt, m, n, k = desc.dtype, desc.m, desc.n, desc.k
-    wp, wb = _ws(ws)
+    wp, wb = _space(ws, dev)
     gp, ldg = _mat(dout, "dout", dt, m, n, dev)
     bp, ldb = _mat(w, "w", dt, n, k, dev)
     xp, ldx = _mat(da, "da", dt, m, k, dev)
@@ -530,7 +542,7 @@ def fs_layer_norm(desc, x, add, gamma, beta, sum_out, y, mean, rstd, save_in=Non
 def fs_layer_norm_backward(desc, dy, x, mean, rstd, gamma, dres, dx, dgamma, dbeta, ws, stream=None):
     dev, s = _here(stream)
     dt, r, c = desc.dtype, desc.rows, desc.cols
-    wp, wb = _ws(ws)
+    wp, wb = _space(ws, dev)
     gp, ldg = _mat(dy, "dy", dt, r, c, dev)
     rp, ldr = _mat(dres, "dres", dt, r, c, dev)
     xp, ldx = _mat(dx, "dx", dt, r, c, dev)

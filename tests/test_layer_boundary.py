@@ -197,3 +197,13 @@ def test_outputs_lie_apart():
     one = lin(1)
     st = lib.fs_linear(ctypes.byref(one), A, 100, B, 24, None, None, 0, A + 40, 50, None, None, None, 0, None)
     assert st == INV and b"overlap" in lib.fs_last_error_message()
+
+
+def test_binding_refuses_a_workspace_elsewhere():
+    """A workspace on the host, or one whose bytes do not lie together."""
+    d, n = lin(1, 16, 4096), norm()
+    host, gaps = torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(1 << 20, dtype=torch.uint8)[::2]
+    for ws, text in ((host, "ws must be on the current GPU"), (gaps, "ws must be contiguous")):
+        refuse(L.FS_ERR_INVALID, text, fs.fs_linear, d, A, B, None, None, C, ws)
+        refuse(L.FS_ERR_INVALID, text, fs.fs_linear_backward, d, A, B, C, None, D, E, None, ws)
+        refuse(L.FS_ERR_INVALID, text, fs.fs_layer_norm_backward, n, A, B, C, D, None, None, E, E + 4096, None, ws)
