@@ -67,7 +67,7 @@ class DenseSublayer:
         self.mean, self.rstd = (torch.empty((tokens,), dtype=torch.float32, device=dev) for _ in range(2))
         self.x_ckpt, self.h_ckpt, self.u_ckpt = kept(d), kept(d), kept(f)
         self.z = kept(f) if save == "codes" else rows(f) if save == "rows" else None
-        self.x = None
+        self.x, self.ran = None, False
         need = max(L.fs_linear_workspace(self.up, L.FS_OP_LINEAR),
                    L.fs_linear_workspace(self.down, L.FS_OP_LINEAR))
         if save:
@@ -82,12 +82,13 @@ class DenseSublayer:
         backward pass reads x itself, which has to stay as it is until
         then."""
         gamma, beta, w1, b1, w2, b2 = self.params
-        self.x = x if self.save == "rows" else None
+        self.x, self.ran = x if self.save == "rows" else None, False
         L.fs_layer_norm(self.norm, x, None, gamma, beta, None, self.h, self.mean, self.rstd,
                         save_in=self.x_ckpt, save_y=self.h_ckpt, stream=stream)
         L.fs_linear(self.up, self.h, w1, b1, None, self.u, self.ws, save_z=self.z, save_out=self.u_ckpt,
                     stream=stream)
         L.fs_linear(self.down, self.u, w2, b2, x, out, self.ws, stream=stream)
+        self.ran = True
         return out
 
     def backward(self, dout, grads, stream=None):
@@ -96,11 +97,11 @@ class DenseSublayer:
         "beta", "b1", "b2" (fp32, absent or None to leave out)."""
         if not self.save:
             raise ValueError("nothing was saved for a backward pass (save=None)")
+        if not self.ran:
+            raise ValueError("backward before forward")
         gamma, beta, w1, b1, w2, b2 = self.params
         x, h, u = ((self.x_ckpt, self.h_ckpt, self.u_ckpt) if self.save == "codes"
                    else (self.x, self.h, self.u))
-        if x is None:
-            raise ValueError("backward before forward")
         L.fs_linear_backward(self.down, dout, u, w2, None, self.du, grads["w2"], grads.get("b2"), self.ws,
                              stream=stream)
         L.fs_linear_backward(self.up, self.du, h, w1, self.z, self.dh, grads["w1"], grads.get("b1"),

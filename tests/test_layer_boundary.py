@@ -207,3 +207,21 @@ def test_binding_refuses_a_workspace_elsewhere():
         refuse(L.FS_ERR_INVALID, text, fs.fs_linear, d, A, B, None, None, C, ws)
         refuse(L.FS_ERR_INVALID, text, fs.fs_linear_backward, d, A, B, C, None, D, E, None, ws)
         refuse(L.FS_ERR_INVALID, text, fs.fs_layer_norm_backward, n, A, B, C, D, None, None, E, E + 4096, None, ws)
+
+
+@pytest.mark.parametrize("save", ["rows", "codes"])
+def test_sublayer_backward_before_forward(save):
+    """Nothing is saved yet, nor after a forward pass that was refused."""
+    layer = sublayer(save)
+    x = torch.zeros((3, 4), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="before forward"):
+        layer.backward(x, {})
+    with pytest.raises(L.FsError):
+        layer.forward(x, torch.zeros((3, 5), dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="before forward"):
+        layer.backward(x, {})
+
+
+def sublayer(save, tokens=3, d=4, f=6):
+    w1, w2 = torch.zeros((f, d), dtype=torch.bfloat16), torch.zeros((d, f), dtype=torch.bfloat16)
+    return fs.DenseSublayer(tokens, None, None, w1, None, w2, None, save=save)
