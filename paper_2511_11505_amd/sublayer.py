@@ -78,9 +78,11 @@ class DenseSublayer:
         self.ws = torch.empty((max(need, 256),), dtype=torch.uint8, device=dev)
 
     def forward(self, x, out, stream=None):
-        """out = x + sublayer(x) (out may not be x).  With save="rows" the
-        backward pass reads x itself, which has to stay as it is until
-        then."""
+        """out = x + sublayer(x); out may be x itself, but not with
+        save="rows", where the backward pass reads x, which has to stay as it
+        is until then."""
+        if self.save == "rows" and self.norm.rows and L.ptr(out) == L.ptr(x):
+            raise ValueError("out may not be x with save='rows': the backward pass reads x")
         gamma, beta, w1, b1, w2, b2 = self.params
         self.x, self.ran = x if self.save == "rows" else None, False
         L.fs_layer_norm(self.norm, x, None, gamma, beta, None, self.h, self.mean, self.rstd,

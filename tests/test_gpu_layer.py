@@ -751,3 +751,19 @@ def test_scales_without_codes_are_left_alone(m, n, k):
         got.append((out.get(), z.get()))
     assert bool((scales == 0x5A).all())
     assert all(np.array_equal(p, q) for p, q in zip(*got))
+
+
+@pytest.mark.parametrize("save", [None, "codes"])
+@pytest.mark.parametrize("n,d,f", [(3, 128, 256), (300, 520, 1032)])
+def test_sublayer_in_place(n, d, f, save):
+    """out is x itself, where the backward pass does not read x: the bits of
+    the same pass into another tensor, forward and backward."""
+    _, layer, x, dout, grads = make_sublayer(n, d, f, "bf16", "silu", True, save)
+    want = layer.forward(x, torch.empty_like(x))
+    if save:
+        layer.backward(dout, grads)
+        wg = {k: v.clone() for k, v in grads.items()}
+    assert torch.equal(layer.forward(x, x), want)
+    if save:
+        layer.backward(dout, grads)
+        assert all(torch.equal(grads[k], wg[k]) for k in wg)

@@ -225,3 +225,9 @@ def test_sublayer_backward_before_forward(save):
 def sublayer(save, tokens=3, d=4, f=6):
     w1, w2 = torch.zeros((f, d), dtype=torch.bfloat16), torch.zeros((d, f), dtype=torch.bfloat16)
     return fs.DenseSublayer(tokens, None, None, w1, None, w2, None, save=save)
+
+
+def test_sublayer_in_place_would_lose_the_saved_rows():
+    x = torch.zeros((3, 4), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="may not be x"):
+        sublayer("rows").forward(x, x)
