@@ -9,8 +9,10 @@ Eq. 8b).  ``DenseSublayer`` is that computation in full:
 forward and backward, through fs_layer_norm, fs_linear and their backward
 passes.  With ``save="codes"`` the activations that the backward pass reads (x,
 h, the pre-activation and u) are kept as 8-bit checkpoints, written by the
-passes that compute them; with "rows" as they are; with None (serving) not at
-all.  All arithmetic runs in the library's kernels; torch only allocates
+passes that compute them, and the rows of h and u, read no more after the
+forward pass, become those of their gradients: in bf16 4.1 (d + f) bytes a
+token, against 4 d + 6 f and the caller's x with "rows", which keeps them as
+they are; with None (serving) nothing is kept.  All arithmetic runs in the library's kernels; torch only allocates
 memory.  A sublayer's passes share its buffers and its workspace, so they run
 one after another, on one stream or ordered by events.
 """
@@ -71,7 +73,8 @@ class DenseSublayer:
         need = max(L.fs_linear_workspace(self.up, L.FS_OP_LINEAR),
                    L.fs_linear_workspace(self.down, L.FS_OP_LINEAR))
         if save:
-            self.dh, self.du = rows(d), rows(f)
+            # (with rows saved, the backward pass still reads h and u)
+            self.dh, self.du = (self.h, self.u) if save == "codes" else (rows(d), rows(f))
             need = max(need, L.fs_layer_norm_workspace(self.norm),
                        L.fs_linear_workspace(self.up, L.FS_OP_LINEAR_BACKWARD),
                        L.fs_linear_workspace(self.down, L.FS_OP_LINEAR_BACKWARD))

@@ -231,3 +231,27 @@ def test_sublayer_in_place_would_lose_the_saved_rows():
     x = torch.zeros((3, 4), dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="may not be x"):
         sublayer("rows").forward(x, x)
+
+
+def held_bytes(layer):
+    """Bytes of the distinct tensors that a sublayer keeps beside its
+    parameters."""
+    held = {}
+    for v in vars(layer).values():
+        for t in v if isinstance(v, tuple) else (v,):
+            if isinstance(t, torch.Tensor) and not any(t is q for q in layer.params):
+                held[t.untyped_storage().data_ptr()] = t.untyped_storage().nbytes()
+    return sum(held.values())
+
+
+@pytest.mark.parametrize("d,f", [(64, 64), (256, 256), (256, 1024), (512, 128)])
+def test_sublayer_codes_hold_less_than_rows(d, f):
+    """A token's bytes beyond the workspace, as documented."""
+    n = 96
+    rows, codes = sublayer("rows", n, d, f), sublayer("codes", n, d, f)
+    stats = 2 * 4 * n   # mean, rstd
+    assert held_bytes(rows) - rows.ws.numel() - stats == n * (4 * d + 6 * f)
+    kept = n * (2 * (d + f) + 2 * (d + f) * 33 // 32)
+    assert held_bytes(codes) - codes.ws.numel() - stats == kept
+    # (rows mode reads the caller's x as well)
+    assert kept < n * (4 * d + 6 * f + 2 * d)
