@@ -13,6 +13,9 @@ import torch
 import paper_2511_11505_amd as fs
 from oracle import layer as O
 from paper_2511_11505_amd import _lib as L
+from tests import _bounds as B
+from tests import _linear_rules as R
+from tests._bounds import BACKWARD, FORWARD, SUBLAYER, rel
 from tests._util import f64
 
 pytestmark = [pytest.mark.gpu,
@@ -779,3 +782,52 @@ def test_sublayer_backward_twice(save):
     once = {k: v.clone() for k, v in grads.items()}
     layer.backward(dout, grads)
     assert all(torch.equal(grads[k], once[k]) for k in once)
+
+
+# ------------------------------------------------ fp32 results hold 32 bits
+# Bounds on the error's norm (tests/_bounds.py); an oracle with fewer bits
+# anywhere in these sizes is outside of them (tests/test_bounds.py).
+@pytest.mark.parametrize("m,n,k,parts,pad,route", FORWARD)
+def test_linear_holds_32_bits(m, n, k, parts, pad, route):
+    if route != "few":
+        assert R.route(R.FORWARD, m, n, k, "f32", k % 8 == 0 and pad == 0) == route
+    g = gen(m + n + k)
+    a, w = mat(g, m, k, "f32", pad), mat(g, n, k, "f32", pad)
+    desc = fs.linear_desc(m, n, k, "f32")
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR))
+    out = Out(m, n, "f32", pad)
+    fs.fs_linear(desc, a, w, None, None, out.view, wp)
+    torch.cuda.synchronize()
+    guard(ws, wp)
+    assert rel(out.get(), f64(a) @ f64(w).T) <= B.product(k, parts)
+
+
+@pytest.mark.parametrize("m,n,k,act,routes", BACKWARD)
+def test_linear_backward_holds_32_bits(m, n, k, act, routes):
+    for kind, size, width, route in ((R.INPUT, (m, k, n), k, routes[0]), (R.WEIGHT, (n, k, m), k, routes[1])):
+        assert R.route(kind, *size, "f32", n % 8 == 0 and width % 8 == 0) == route
+    g = gen(m + n + k)
+    a, z, dout, w = mat(g, m, k, "f32"), mat(g, m, n, "f32"), mat(g, m, n, "f32"), mat(g, n, k, "f32")
+    desc = fs.linear_desc(m, n, k, "f32", act)
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR_BACKWARD))
+    da, dw, db = Out(m, k, "f32"), Out(n, k, "f32"), torch.full((n,), float("nan"), device=DEV)
+    fs.fs_linear_backward(desc, dout, a, w, None if act == "none" else z, da.view, dw.view, db, wp)
+    torch.cuda.synchronize()
+    guard(ws, wp)
+    wa, ww, wb, _ = O.linear_backward(f64(dout), f64(a), f64(w), f64(z), act)
+    slope = 0 if act in ("none", "relu") else 2 * ACT
+    assert rel(da.get(), wa) <= B.product(n) + slope
+    assert rel(dw.get(), ww) <= B.product(m) + slope
+    assert rel(f64(db), wb) <= B.product(m) + slope
+
+
+@pytest.mark.parametrize("n,d,f,act", SUBLAYER)
+def test_sublayer_holds_32_bits(n, d, f, act):
+    p, layer, x, dout, grads = make_sublayer(n, d, f, "f32", act, True, "rows")
+    out = layer.forward(x, torch.empty_like(x))
+    layer.backward(dout, grads)
+    torch.cuda.synchronize()
+    want, wg = sublayer_oracle(f64(x), f64(dout), [f64(t) for t in p], act, True, lambda t: t, False)
+    assert rel(f64(out), want) <= B.sublayer_forward(d, f)
+    for k, v in grads.items():
+        assert rel(f64(v), wg[k]) <= B.sublayer_backward(n, d, f), k
