@@ -76,7 +76,9 @@ inline double mid_us(int64_t M, int64_t N, int64_t K, int es, bool aligned, int 
 // not align, 0.79 in fp32), or 0.26 (0.34, 0.70) per workgroup of the CU.  Measured:
 // 512 x 2048, K 2048, 20.0 us; 2048 x 2048, K 2048, 36.7; 777 x 1001, K 1409 (unaligned)
 // 18.6 (1 slice), 19.0 (2), 21.6 (4); fp32 512 x 1408, K 2048, 55 (1), 47 (2), 42 (4),
-// 1408 x 2048, K 512, 38.
+// 1408 x 2048, K 512, 38, 4096 x 4096, K 4096, 1317; rows that 16 bytes do not align,
+// by an odd stride (by a base one element off): 4096 x 4096, K 4096, 323 (458), 8192 x
+// 8192, K 5120, 1773 (2270).
 inline double any_us(int64_t M, int64_t N, int64_t blocks, int64_t s, bool bf16, bool aligned, int cus) {
   const double wgs = (double)(cdiv_(M, 64) * cdiv_(N, 64) * s) / cus;
   const double one = bf16 ? (aligned ? 0.50 : 0.65) : 0.79, each = bf16 ? (aligned ? 0.26 : 0.34) : 0.70;
@@ -124,8 +126,9 @@ inline ProductPlan product_plan(bool bf16, bool tiles_ok, bool a_along, bool b_a
 // 0 along, M or N % 8 != 0 across) are first copied to rows of whole 16-byte
 // chunks (zeros behind the last element): when the tiles' time and the copies'
 // are less than the other kernels'.  By the sizes alone, so that the workspace
-// is known.  (777 x 1001, K 1409: 19 us without, 24 with, of which the copies
-// 10.)
+// is known: an odd stride or base of divisible widths is not copied.  (777 x 1001, K
+// 1409: 19 us without, 24 with, of which the copies 10; 4096 x 4096, K 4097, 170 with,
+// where K 4096 with stride 4097 takes 323.)
 inline bool product_packs(bool bf16, bool a_along, bool b_along, int64_t M, int64_t N, int64_t K, int cus) {
   if (!bf16 || M <= 0 || N <= 0) return false;
   const bool a = (a_along ? K : M) % 8 != 0, b = (b_along ? K : N) % 8 != 0;

@@ -134,7 +134,8 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_backward_kernel(NormBa
   const float inv_d = 1.0f / (float)a.cols;
   // More than a chunk per thread of a workgroup's row leaves no registers for a
   // row ahead and gamma, four not even for the row: the second pass loads it
-  // again.
+  // again (2048 x 32768 in bf16, from rows: 331 us, where a copy's rate would take 79;
+  // 4096 x 12288, two chunks, 82 of 59).
   constexpr bool AHEAD = WAVE || NC == 1, HOLD = WAVE || NC < 4;
   float dg[NC][8] = {}, db[NC][8] = {};
   struct Chunk {

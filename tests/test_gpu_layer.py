@@ -831,3 +831,46 @@ def test_sublayer_holds_32_bits(n, d, f, act):
     assert rel(f64(out), want) <= B.sublayer_forward(d, f)
     for k, v in grads.items():
         assert rel(f64(v), wg[k]) <= B.sublayer_backward(n, d, f), k
+
+
+# -------------------------------------- a checkpoint and the rows it stands for
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,d", [(9, 77), (300, 1000), (5, 5120), (40, 9000), (3, 20001)])
+def test_norm_backward_of_restored_rows(m, d, dtype):
+    """Codes and the restored rows give the same bits."""
+    g = gen(m + d)
+    x, dy = mat(g, m, d, dtype), mat(g, m, d, dtype)
+    c, back = fs.checkpoint_buffers(m, d), torch.empty((m, d), dtype=TORCH[dtype], device=DEV)
+    fs.fs_checkpoint_fp8(CODE[dtype], m, d, x, *c)
+    fs.fs_checkpoint_restore(CODE[dtype], m, d, *c, back)
+    mean, rstd = x.float().mean(1), 1 / x.float().std(1)
+    desc = fs.norm_desc(m, d, dtype)
+    ws, wp = workspace(fs.fs_layer_norm_workspace(desc))
+    got = []
+    for saved in (c, back):
+        dx, dg, db = Out(m, d, dtype), torch.empty((d,), device=DEV), torch.empty((d,), device=DEV)
+        fs.fs_layer_norm_backward(desc, dy, saved, mean, rstd, None, None, dx.view, dg, db, wp)
+        got.append([dx.get(), f64(dg), f64(db)])
+    assert all(np.array_equal(p, q) for p, q in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(9, 64, 72), (130, 40, 2048), (300, 520, 1000), (3000, 1000, 2000)])
+def test_linear_backward_of_restored_rows(m, n, k, dtype):
+    """The same for the linear where widths are whole chunks."""
+    g = gen(m + n + k)
+    a, z, dout, w = mat(g, m, k, dtype), mat(g, m, n, dtype), mat(g, m, n, dtype), mat(g, n, k, dtype)
+    saved = []
+    for t, cols in ((a, k), (z, n)):
+        c, back = fs.checkpoint_buffers(m, cols), torch.empty((m, cols), dtype=TORCH[dtype], device=DEV)
+        fs.fs_checkpoint_fp8(CODE[dtype], m, cols, t, *c)
+        fs.fs_checkpoint_restore(CODE[dtype], m, cols, *c, back)
+        saved.append((c, back))
+    desc = fs.linear_desc(m, n, k, dtype, "gelu")
+    ws, wp = workspace(fs.fs_linear_workspace(desc, L.FS_OP_LINEAR_BACKWARD))
+    got = []
+    for i in (0, 1):
+        da, dw, db = Out(m, k, dtype), Out(n, k, dtype), torch.empty((n,), device=DEV)
+        fs.fs_linear_backward(desc, dout, saved[0][i], w, saved[1][i], da.view, dw.view, db, wp)
+        got.append([da.get(), dw.get(), f64(db)])
+    assert all(np.array_equal(p, q) for p, q in zip(*got))
