@@ -452,7 +452,7 @@ def _space(ws, dev):
         _bad("ws", "contiguous")
     if ws.get_device() != dev:
         _bad("ws", "on the current GPU")
-    return _ws(ws)
+    return ws.data_ptr(), ws.nbytes
 
 
 def _codes(pair, name, rows, cols, dev):
