@@ -349,10 +349,9 @@ def _call(s):
             else:
                 out[name] = s[name + "c"]
         return out
-    desc = _kept(s, "desc", lambda: fs.attention_desc(c["seqs"], c["heads"], s["table"].shape[1], new_tokens=c["new"],
-                                                      scale=c["d"] ** -0.5, window=c["window"]))
+    desc = _kept(s, "desc", lambda: fs.attention_desc(c["heads"], c["new"], c["d"] ** -0.5, c["window"]))
     kv = _kept(s, "cache", cache)
-    ws = _kept(s, "ws", lambda: torch.empty((max(256, fs.fs_paged_attention_workspace(desc, kv)),),
+    ws = _kept(s, "ws", lambda: torch.empty((max(256, fs.fs_paged_attention_workspace(desc, kv, s["table"])),),
                                             dtype=torch.uint8, device=DEV))
     out = empty("out", (c["seqs"] * c["new"], c["heads"], c["d"]))
     lse = empty("lse", (c["seqs"] * c["new"], c["heads"]), torch.float32)
