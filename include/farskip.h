@@ -716,6 +716,160 @@ fs_status fs_layer_norm_backward(const fs_norm_desc* desc, const void* dy, int64
                                  int64_t lddx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
                                  fs_stream stream);
 
+/* ---- The attention sublayer of a serving step in the far-skip window: rotary
+ * positions (and their backward pass, for training), appending keys and values
+ * to a paged cache, and the attention of new tokens over that cache.
+ *
+ * Conventions of these entry points, where they differ from the others'
+ *   Heads       q, k, v, out and the like are [tokens, heads, head_dim] with a
+ *               stride between tokens and one between heads, in elements; the
+ *               columns of a head lie together.  Tokens may hold their heads
+ *               together or heads their tokens; neither may overlap.  Pointers
+ *               are aligned to their elements; 16-byte aligned bases and
+ *               strides are faster.
+ *   Rounding    Angles are taken in 64 bits; products, sums and softmax
+ *               statistics are fp32; each output is rounded once.  The
+ *               attention's weights are rounded to bf16 before they meet bf16
+ *               values (both 8-bit and bf16 caches with dtype FS_BF16).
+ *   Overlap, Devices, Order, Graphs   as for the dense sublayer. */
+
+typedef enum {
+  FS_ROPE_HALVES = 0, /* column i turns with column i + rot_dim / 2 */
+  FS_ROPE_PAIRS = 1   /* column 2 i turns with column 2 i + 1 */
+} fs_rope_layout;
+
+typedef enum {
+  FS_ROPE_PLAIN = 0,  /* f_i = base^(-2 i / rot_dim) */
+  FS_ROPE_LINEAR = 1, /* f_i / factor */
+  FS_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)) for base: f_0 stays,
+                         the slowest becomes 1 / factor of itself (rot_dim > 2) */
+  FS_ROPE_PARTS = 3   /* f_i (g + (1 - g) / factor), g = clamp((t - low) / (high - low), 0, 1),
+                         t = trained_len f_i / (2 pi): the turns f_i makes over the
+                         trained length.  Fast pairs stay, slow ones are
+                         slowed by factor, those between by parts of both */
+} fs_rope_scaling;
+
+/* The rotation: pair i of the rot_dim columns from column `first` of a head,
+ * (a, b), at angle t = position * freqs[i], becomes
+ *   (mscale cos t a - mscale sin t b, mscale cos t b + mscale sin t a)
+ * in fp32, each product rounded.  Other columns stay as they are. */
+typedef struct {
+  int32_t layout;       /* fs_rope_layout */
+  int32_t first;        /* >= 0, first + rot_dim <= head_dim */
+  int32_t rot_dim;      /* even, >= 0 (0: nothing turns) */
+  double mscale;        /* factor of cos and sin */
+  const double* freqs;  /* [rot_dim / 2] radians a position (device memory) */
+} fs_rope;
+
+/* The frequencies of a rotation, in 64 bits.  `freqs` is HOST memory
+ * [rot_dim / 2]; no GPU work.  base and, where scaled, factor > 0; trained_len >
+ * 0 and low < high with FS_ROPE_PARTS (unused arguments are ignored). */
+fs_status fs_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                              double trained_len, double low, double high, double* freqs);
+
+typedef struct {
+  int32_t abi_version; /* FS_ABI_VERSION */
+  int32_t dtype;       /* fs_dtype of x and out */
+  int32_t tokens;      /* <= 2^24 */
+  int32_t heads;       /* <= 2^16 */
+  int32_t head_dim;    /* <= 512 */
+} fs_rotary_desc;
+
+/* Rotation of x [tokens, heads, head_dim] (token stride tsx, head stride hsx) by
+ * positions [tokens] int32 (any value; device memory) into out.  out may be x
+ * itself (same pointer and strides).  tokens == 0 is a valid no-op. */
+fs_status fs_rotary(const fs_rotary_desc* desc, const fs_rope* rope, const void* x, int64_t tsx,
+                    int64_t hsx, const int32_t* positions, void* out, int64_t tso, int64_t hso,
+                    fs_stream stream);
+
+/* Its backward pass: dx is dout turned back (by -t, with the same mscale).  dx
+ * may be dout itself. */
+fs_status fs_rotary_backward(const fs_rotary_desc* desc, const fs_rope* rope, const void* dout,
+                             int64_t tso, int64_t hso, const int32_t* positions, void* dx,
+                             int64_t tsx, int64_t hsx, fs_stream stream);
+
+/* A paged key-value cache.  Element (page, head, place, column) of k (v) is at
+ * k + page * page_stride + head * head_stride + place * place_stride + column;
+ * it is a row's element of dtype, or with codes == 1 an E4M3 code, whose block
+ * of 32 columns of the head (the last may be short) has the scale byte
+ * k_scales[((page * kv_heads + head) * page_size + place) * ceil(head_dim / 32) +
+ * column / 32], in the format of fs_saved's checkpoints. */
+typedef struct {
+  int32_t abi_version;  /* FS_ABI_VERSION */
+  int32_t dtype;        /* fs_dtype of q, k, v and out, and of the cache without codes */
+  int32_t codes;        /* 0 or 1 */
+  int32_t n_pages;      /* >= 0; n_pages * page_size <= 2^34 */
+  int32_t kv_heads;     /* 1 .. 4096 */
+  int32_t page_size;    /* tokens in a page: >= 1, any number */
+  int32_t head_dim;     /* a multiple of 8, <= 256 */
+  void* k;              /* 16-byte aligned; with codes 8-byte aligned */
+  void* v;
+  int64_t page_stride;  /* in elements, multiples of 8; place_stride <= 2^20 */
+  int64_t head_stride;
+  int64_t place_stride;
+  uint8_t* k_scales;    /* [n_pages, kv_heads, page_size, ceil(head_dim / 32)] with codes */
+  uint8_t* v_scales;
+} fs_kv_cache;
+
+/* Where a sequence's tokens are: token t of sequence b is at place t % page_size
+ * of page table[b * ldt + t / page_size].  table is int32 device memory
+ * [sequences, max_pages].  An entry outside of [0, n_pages) is a hole: its tokens
+ * are not written and not seen. */
+typedef struct {
+  const int32_t* table;
+  int64_t ldt;        /* >= max_pages */
+  int32_t sequences;  /* <= 2^20 */
+  int32_t max_pages;  /* max_pages * page_size <= 2^30 */
+} fs_page_table;
+
+/* Append: token t with position p = positions[t] of sequence b = seqs[t] (NULL:
+ * b = t) gets
+ *   q_out[t] = q[t] turned by p                        (q may be NULL)
+ *   k row at (b, p) = k[t] turned by p, v row at (b, p) = v[t]
+ * each rounded once, the cache's rows straight to codes where it holds codes.
+ * rope NULL: nothing turns.  A token with p < 0 or b outside of [0, sequences) is
+ * none: its q_out is 0, and nothing else is written.  p >= max_pages * page_size is
+ * a hole.  Of two tokens of one call at the same place either may be kept, or
+ * parts of both.
+ *   q, q_out [tokens, q_heads, head_dim]; k, v [tokens, kv_heads, head_dim] */
+fs_status fs_cache_append(const fs_kv_cache* cache, const fs_rope* rope, int32_t tokens,
+                          int32_t q_heads, const void* q, int64_t tsq, int64_t hsq, const void* k,
+                          int64_t tsk, int64_t hsk, const void* v, int64_t tsv, int64_t hsv,
+                          const int32_t* seqs, const int32_t* positions, const fs_page_table* pages,
+                          void* q_out, int64_t tso, int64_t hso, fs_stream stream);
+
+typedef struct {
+  int32_t abi_version; /* FS_ABI_VERSION */
+  int32_t q_heads;     /* a multiple of kv_heads, <= 2^16: head i reads key head
+                          i / (q_heads / kv_heads) */
+  int32_t new_tokens;  /* n >= 1: queries of each sequence, its last n tokens */
+  int32_t window;      /* 0, or how many tokens a query sees, itself included */
+  float scale;         /* factor of q . k; finite */
+} fs_attention_desc;
+
+/* Bytes of workspace of fs_paged_attention; of the page table only the sizes are
+ * read.  The workspace is 16-byte aligned. */
+fs_status fs_paged_attention_workspace(const fs_attention_desc* desc, const fs_kv_cache* cache,
+                                       const fs_page_table* pages, size_t* bytes);
+
+/* Attention of each sequence's last n tokens over its cached ones, themselves
+ * included.  Row b n + i of q, out and lse is the query at position
+ * p = lengths[b] - n + i; it sees the tokens j with 0 <= j <= p, j > p - window
+ * where there is one, and no hole at j:
+ *   s_j = scale q . k_j;  out = sum_j exp(s_j) v_j / sum_j exp(s_j)
+ *   lse = ln sum_j exp(s_j)
+ * A query that sees nothing (p < 0: a sequence shorter than n, or an empty one)
+ * gets out = 0 and lse = -infinity.  What is held at places that a query does not
+ * see does not reach it, NaNs included.
+ *   q, out   [sequences * n, q_heads, head_dim] dtype, at most 2^24 tokens
+ *   lengths  [sequences] int32: tokens in the cache; negative: 0, above max_pages *
+ *            page_size: that
+ *   lse      [sequences * n, q_heads] fp32 or NULL */
+fs_status fs_paged_attention(const fs_attention_desc* desc, const fs_kv_cache* cache, const void* q,
+                             int64_t tsq, int64_t hsq, const int32_t* lengths,
+                             const fs_page_table* pages, void* out, int64_t tso, int64_t hso,
+                             float* lse, void* ws, size_t ws_bytes, fs_stream stream);
+
 /* Per-kernel timing with HIP events recorded on the launch stream around
  * selected kernels.  fs_profile_read synchronises those events.
  * FS_K_GATE_UP / FS_K_DOWN time the routed experts' passes (and

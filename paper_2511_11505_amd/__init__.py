@@ -32,4 +32,9 @@ from ._lib import (  # noqa: F401
     fs_checkpoint_restore, fs_linear_workspace, fs_linear, fs_linear_backward,
     fs_layer_norm_workspace, fs_layer_norm, fs_layer_norm_backward,
 )
+from ._lib import (  # noqa: F401
+    FS_ROPE_HALVES, FS_ROPE_PAIRS, FS_ROPE_PLAIN, FS_ROPE_LINEAR, FS_ROPE_BASE, FS_ROPE_PARTS, fs_rope, fs_rotary_desc,
+    fs_kv_cache, fs_page_table, fs_attention_desc, rope, kv_cache, rotary_desc, attention_desc, fs_rope_frequencies,
+    fs_rotary, fs_rotary_backward, fs_cache_append, fs_paged_attention_workspace, fs_paged_attention,
+)
 from .sublayer import DenseSublayer, checkpoint_buffers, linear_desc, norm_desc  # noqa: F401

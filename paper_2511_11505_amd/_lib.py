@@ -20,6 +20,8 @@ FS_SOFTMAX, FS_SIGMOID = 0, 1
 (FS_OP_ROUTER_TOPK, FS_OP_DISPATCH_PACK, FS_OP_GROUPED_FFN, FS_OP_BLOCK, FS_OP_GROUPED_FFN_FP8,
  FS_OP_BLOCK_FP8, FS_OP_DISPATCH_PACK_FP8, FS_OP_LINEAR, FS_OP_LINEAR_BACKWARD) = range(9)
 FS_ACT_NONE, FS_ACT_RELU, FS_ACT_GELU, FS_ACT_SILU = range(4)
+FS_ROPE_HALVES, FS_ROPE_PAIRS = range(2)
+FS_ROPE_PLAIN, FS_ROPE_LINEAR, FS_ROPE_BASE, FS_ROPE_PARTS = range(4)
 (FS_K_ROUTER, FS_K_TOPK, FS_K_PLAN, FS_K_PACK, FS_K_GATE_UP, FS_K_DOWN,
  FS_K_COMBINE, FS_K_SHARED_GATE_UP, FS_K_SHARED_DOWN, FS_K_DISPATCH_COPY, FS_K_DENSE,
  FS_K_COMBINE_COPY, FS_K_ALLREDUCE_COPY, FS_K_QUANTIZE, FS_K_COUNT) = range(15)
@@ -70,6 +72,30 @@ class fs_saved(ctypes.Structure):
     _fields_ = [("rows", _vp), ("ld", _i64), ("codes", _vp), ("scales", _vp)]
 
 
+class fs_rope(ctypes.Structure):
+    _fields_ = [("layout", _i32), ("first", _i32), ("rot_dim", _i32), ("mscale", ctypes.c_double), ("freqs", _vp)]
+
+
+class fs_rotary_desc(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("abi_version", "dtype", "tokens", "heads", "head_dim")]
+
+
+class fs_kv_cache(ctypes.Structure):
+    _fields_ = ([(n, _i32) for n in ("abi_version", "dtype", "codes", "n_pages", "kv_heads", "page_size", "head_dim")]
+                + [("k", _vp), ("v", _vp), ("page_stride", _i64), ("head_stride", _i64), ("place_stride", _i64),
+                   ("k_scales", _vp), ("v_scales", _vp)])
+
+
+class fs_page_table(ctypes.Structure):
+    _fields_ = [("table", _vp), ("ldt", _i64), ("sequences", _i32), ("max_pages", _i32)]
+
+
+class fs_attention_desc(ctypes.Structure):
+    _fields_ = [("abi_version", _i32), ("q_heads", _i32), ("new_tokens", _i32), ("window", _i32), ("scale", _f32)]
+
+
+_pro, _prd, _pkv, _ppt, _pad = (ctypes.POINTER(t) for t in (fs_rope, fs_rotary_desc, fs_kv_cache, fs_page_table,
+                                                          fs_attention_desc))
 _pld, _pnd, _psv = (ctypes.POINTER(t) for t in (fs_linear_desc, fs_norm_desc, fs_saved))
 _SIGS = {
     "fs_status_string": (ctypes.c_char_p, [_i32]),
@@ -121,6 +147,13 @@ _SIGS = {
                              _psv, _vp]),
     "fs_layer_norm_backward": (_i32, [_pnd, _vp, _i64, _psv, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp,
                                       _vp, _vp, _sz, _vp]),
+    "fs_rope_frequencies": (_i32, [_i32, ctypes.c_double, _i32] + [ctypes.c_double] * 4 + [_vp]),
+    "fs_rotary": (_i32, [_prd, _pro, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp]),
+    "fs_rotary_backward": (_i32, [_prd, _pro, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp]),
+    "fs_cache_append": (_i32, [_pkv, _pro, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp,
+                               _vp, _ppt, _vp, _i64, _i64, _vp]),
+    "fs_paged_attention_workspace": (_i32, [_pad, _pkv, _ppt, ctypes.POINTER(_sz)]),
+    "fs_paged_attention": (_i32, [_pad, _pkv, _vp, _i64, _i64, _vp, _ppt, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
     "fs_profile_enable": (_i32, [_i32]),
     "fs_profile_select": (_i32, [ctypes.c_uint32]),
     "fs_profile_read": (_i32, [_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i64)]),
@@ -405,7 +438,8 @@ def _here(stream):
     global _gpu
     if _gpu is None:
         import torch
-        _ELEM.update({FS_F32: torch.float32, FS_BF16: torch.bfloat16, "u8": torch.uint8})
+        _ELEM.update({FS_F32: torch.float32, FS_BF16: torch.bfloat16, "u8": torch.uint8, "i32": torch.int32,
+                      "f64": torch.float64})
         _gpu = ((torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
                 if torch.cuda.is_available() else (lambda: -2, lambda device: 0))
         if torch.cuda.is_available():
@@ -552,6 +586,154 @@ def fs_layer_norm_backward(desc, dy, x, mean, rstd, gamma, dres, dx, dgamma, dbe
                                          _flat(gamma, "gamma", FS_F32, (c,), dev), rp, ldr, xp, ldx,
                                          _flat(dgamma, "dgamma", FS_F32, (c,), dev),
                                          _flat(dbeta, "dbeta", FS_F32, (c,), dev), wp, wb, s))
+
+
+# -------------------------------------------- the attention sublayer's entries
+# Heads are 3-D tensors [tokens, heads, head_dim] of unit column stride (their
+# other strides are passed on) or int addresses of gapless ones.
+def _heads(t, name, dtype, tokens, heads, d, dev):
+    """(address, token stride, head stride) of an argument."""
+    if t is None or isinstance(t, int):
+        return t, heads * d, d
+    if t.dtype is not _ELEM.get(dtype) or t.shape != (tokens, heads, d):
+        _bad(name, f"[{tokens}, {heads}, {d}] of the descriptor's type, not {list(t.shape)} of {t.dtype}")
+    ts, hs, step = t.stride()
+    if step != 1 and d > 1:
+        _bad(name, "of unit column stride")
+    if t.get_device() != dev:
+        _bad(name, "on the current GPU")
+    return t.data_ptr(), ts, hs
+
+
+def _pages(t, dev):
+    """fs_page_table of an int32 tensor [sequences, max_pages] of unit column
+    stride, or an fs_page_table."""
+    if isinstance(t, fs_page_table) or t is None:
+        return t
+    if t.dtype is not _ELEM.get("i32") or t.dim() != 2:
+        _bad("pages", f"2-D int32, not {list(t.shape)} of {t.dtype}")
+    b, n = t.shape
+    ld, step = t.stride()
+    if step != 1 and n > 1:
+        _bad("pages", "of unit column stride")
+    if t.get_device() != dev:
+        _bad("pages", "on the current GPU")
+    return fs_page_table(t.data_ptr(), ld if b > 1 else n, b, n)
+
+
+def _on(struct, name, dev):
+    """A cache or rope made of tensors: these have to be on the current GPU."""
+    at = getattr(struct, "device", None)
+    if at is not None and at != dev:
+        _bad(name, "on the current GPU")
+    return struct
+
+
+def rope(freqs, layout="halves", first=0, mscale=1.0):
+    """fs_rope of the frequencies [rot_dim / 2] (float64, on the GPU)."""
+    if layout not in ("halves", "pairs"):
+        raise ValueError(f"layout must be 'halves' or 'pairs', not {layout!r}")
+    _here(0)
+    r = fs_rope(("halves", "pairs").index(layout), first, 2 * freqs.numel(), mscale, None)
+    r.freqs = _flat(freqs, "freqs", "f64", (freqs.numel(),), freqs.get_device())
+    r.tensors, r.device = freqs, freqs.get_device()     # (the struct holds addresses only)
+    return r
+
+
+def kv_cache(k, v, k_scales=None, v_scales=None, dtype=None):
+    """fs_kv_cache of k and v, [pages, kv_heads, page_size, head_dim] tensors with
+    the same strides: rows of bf16 or fp32, or uint8 codes with their scales (then
+    dtype, "bf16" or "f32", is the type of the queries)."""
+    _here(0)
+    pages, heads, page, d = k.shape
+    dev = k.get_device()
+    kind = {"f32": FS_F32, "bf16": FS_BF16, None: FS_F32 if k.dtype is _ELEM[FS_F32] else FS_BF16}.get(dtype, dtype)
+    codes = k_scales is not None
+    if v.shape != k.shape or v.stride() != k.stride():
+        _bad("v", "of k's shape and strides")
+    for t, name in ((k, "k"), (v, "v")):
+        if t.dtype is not _ELEM["u8" if codes else kind]:
+            _bad(name, f"{_ELEM['u8' if codes else kind]}, not {t.dtype}")
+        if t.stride(3) != 1 and d > 1:
+            _bad(name, "of unit column stride")
+        if t.get_device() != dev:
+            _bad(name, "on one device")
+    nb = (pages, heads, page, (d + 31) // 32)
+    c = fs_kv_cache(FS_ABI_VERSION, kind, int(codes), pages, heads, page, d, k.data_ptr(), v.data_ptr(),
+                    *k.stride()[:3], _flat(k_scales, "k_scales", "u8", nb, dev), _flat(v_scales, "v_scales", "u8", nb, dev))
+    c.tensors, c.device = (k, v, k_scales, v_scales), dev
+    return c
+
+
+def rotary_desc(tokens, heads, head_dim, dtype="bf16"):
+    """fs_rotary_desc of [tokens, heads, head_dim]."""
+    return fs_rotary_desc(FS_ABI_VERSION, FS_F32 if dtype == "f32" else FS_BF16, tokens, heads, head_dim)
+
+
+def attention_desc(q_heads, new_tokens=1, scale=1.0, window=0):
+    """fs_attention_desc of each sequence's last new_tokens tokens."""
+    return fs_attention_desc(FS_ABI_VERSION, q_heads, new_tokens, window, scale)
+
+
+def fs_rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, trained_len=0.0, low=1.0, high=4.0):
+    """The frequencies of a rotation: a float64 CPU tensor [rot_dim / 2]."""
+    import torch
+    kinds = ("plain", "linear", "base", "parts")
+    if scaling not in kinds:
+        raise ValueError(f"scaling must be one of {kinds}, not {scaling!r}")
+    out = torch.empty((max(rot_dim, 0) // 2,), dtype=torch.float64)
+    _check(load().fs_rope_frequencies(rot_dim, base, kinds.index(scaling), factor, trained_len, low, high,
+                                      out.data_ptr()))
+    return out
+
+
+def fs_rotary(desc, rope, x, positions, out, stream=None):
+    dev, s = _here(stream)
+    dt, n, h, d = desc.dtype, desc.tokens, desc.heads, desc.head_dim
+    _check(load().fs_rotary(ctypes.byref(desc), _on(rope, "rope", dev), *_heads(x, "x", dt, n, h, d, dev),
+                            _flat(positions, "positions", "i32", (n,), dev), *_heads(out, "out", dt, n, h, d, dev), s))
+
+
+def fs_rotary_backward(desc, rope, dout, positions, dx, stream=None):
+    dev, s = _here(stream)
+    dt, n, h, d = desc.dtype, desc.tokens, desc.heads, desc.head_dim
+    _check(load().fs_rotary_backward(ctypes.byref(desc), _on(rope, "rope", dev),
+                                     *_heads(dout, "dout", dt, n, h, d, dev),
+                                     _flat(positions, "positions", "i32", (n,), dev),
+                                     *_heads(dx, "dx", dt, n, h, d, dev), s))
+
+
+def fs_cache_append(cache, rope, q, k, v, seqs, positions, pages, q_out, stream=None):
+    """q, q_out [tokens, q_heads, head_dim] or None; k, v [tokens, kv_heads,
+    head_dim]; seqs [tokens] or None, positions [tokens] int32."""
+    dev, s = _here(stream)
+    dt, d, n = cache.dtype, cache.head_dim, k.shape[0]
+    h = 0 if q is None else q.shape[1]
+    _check(load().fs_cache_append(_on(cache, "cache", dev), _on(rope, "rope", dev), n, h,
+                                  *_heads(q, "q", dt, n, h, d, dev), *_heads(k, "k", dt, n, cache.kv_heads, d, dev),
+                                  *_heads(v, "v", dt, n, cache.kv_heads, d, dev), _flat(seqs, "seqs", "i32", (n,), dev),
+                                  _flat(positions, "positions", "i32", (n,), dev), _pages(pages, dev),
+                                  *_heads(q_out, "q_out", dt, n, h, d, dev), s))
+
+
+def fs_paged_attention_workspace(desc, cache, pages):
+    out = _sz(0)
+    _check(load().fs_paged_attention_workspace(ctypes.byref(desc), cache, _pages(pages, _here(0)[0]), ctypes.byref(out)))
+    return out.value
+
+
+def fs_paged_attention(desc, cache, q, lengths, pages, out, ws, lse=None, stream=None):
+    """q, out [sequences * new_tokens, q_heads, head_dim]; lengths [sequences]
+    int32; lse [sequences * new_tokens, q_heads] fp32 or None."""
+    dev, s = _here(stream)
+    t = _pages(pages, dev)
+    dt, h, d = cache.dtype, desc.q_heads, cache.head_dim
+    n = t.sequences * desc.new_tokens
+    wp, wb = _space(ws, dev)
+    _check(load().fs_paged_attention(ctypes.byref(desc), _on(cache, "cache", dev), *_heads(q, "q", dt, n, h, d, dev),
+                                     _flat(lengths, "lengths", "i32", (t.sequences,), dev), t,
+                                     *_heads(out, "out", dt, n, h, d, dev), _flat(lse, "lse", FS_F32, (n, h), dev),
+                                     wp, wb, s))
 
 
 def fs_profile_enable(on=True):

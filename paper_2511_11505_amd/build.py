@@ -27,7 +27,9 @@ PER_FILE = {"router.hip": ["-ffp-contract=off"]}
 SOURCES = ["api.cpp", "router.hip", "dispatch.hip", "gemm.hip", "gemm_r64.hip", "gemm_r192_gateup.hip", "gemm_r192_down.hip",
            "gemm_r192_fp8.hip", "elementwise.hip", "fp8.hip",
            "standin.hip", "api_layer.cpp", "linear.hip", "linear_any.hip", "linear_few.hip", "linear_mid.hip", "linear_tile_fwd.hip",
-           "linear_tile_da.hip", "linear_tile_dw.hip", "norm.hip", "checkpoint.hip"]
+           "linear_tile_da.hip", "linear_tile_dw.hip", "norm.hip", "checkpoint.hip",
+           "api_attention.cpp", "rotary.hip", "attention.hip", "attention_bf16.hip", "attention_codes.hip",
+           "attention_f32.hip", "attention_codes_f32.hip"]
 
 
 def _compile(src):

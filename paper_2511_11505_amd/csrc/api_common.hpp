@@ -57,4 +57,43 @@ namespace {
 [[maybe_unused]] size_t align256(size_t b) { return (b + 255) / 256 * 256; }
 [[maybe_unused]] hipStream_t S(fs_stream s) { return reinterpret_cast<hipStream_t>(s); }
 
+#define TRY(expr)                 \
+  do {                            \
+    const fs_status st_ = (expr); \
+    if (st_ != FS_OK) return st_; \
+  } while (0)
+
+[[maybe_unused]] bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+// The kernels run on the stream's device, which has to be the current one.
+[[maybe_unused]] fs_status check_stream(fs_stream stream) {
+  hipStream_t s = S(stream);
+  if (!s) return FS_OK;
+  int cur = 0;
+  hipDevice_t dev = 0;
+  FS_HIP(hipGetDevice(&cur), "hipGetDevice");
+  FS_HIP(hipStreamGetDevice(s, &dev), "hipStreamGetDevice");
+  if ((int)dev != cur)
+    return fail(FS_ERR_INVALID, "the stream belongs to device " + std::to_string((int)dev) +
+                                    ", not the current device " + std::to_string(cur));
+  return FS_OK;
+}
+
+[[maybe_unused]] fs_status check_dtype(int32_t dtype) {
+  if (dtype != FS_F32 && dtype != FS_BF16) return fail(FS_ERR_INVALID, "dtype must be FS_F32 or FS_BF16");
+  return FS_OK;
+}
+
+[[maybe_unused]] int dt(int32_t dtype) { return dtype == FS_F32 ? 0 : 1; }
+
+// No exception (a message that finds no memory) leaves a C entry point.
+template <typename F>
+fs_status entry(F&& f) noexcept {
+  try {
+    return f();
+  } catch (...) {
+    return FS_ERR_INVALID;
+  }
+}
+
 }  // namespace

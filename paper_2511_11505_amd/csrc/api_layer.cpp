@@ -16,8 +16,6 @@ struct Mat {
   size_t es;
 };
 
-bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
 fs_status check_mat(const Mat& m) {
   if (!m.p) return fail(FS_ERR_INVALID, std::string(m.name) + " must not be NULL");
   if (!aligned_to(m.p, m.es))
@@ -82,31 +80,6 @@ Mat scales_of(const fs_saved* s, const char* name, int64_t rows, int64_t cols) {
   return {name, s && s->codes ? s->scales : nullptr, rows, blocks_of(cols), blocks_of(cols), 1};
 }
 
-#define TRY(expr)                 \
-  do {                            \
-    const fs_status st_ = (expr); \
-    if (st_ != FS_OK) return st_; \
-  } while (0)
-
-// The kernels run on the stream's device, which has to be the current one.
-fs_status check_stream(fs_stream stream) {
-  hipStream_t s = S(stream);
-  if (!s) return FS_OK;
-  int cur = 0;
-  hipDevice_t dev = 0;
-  FS_HIP(hipGetDevice(&cur), "hipGetDevice");
-  FS_HIP(hipStreamGetDevice(s, &dev), "hipStreamGetDevice");
-  if ((int)dev != cur)
-    return fail(FS_ERR_INVALID, "the stream belongs to device " + std::to_string((int)dev) +
-                                    ", not the current device " + std::to_string(cur));
-  return FS_OK;
-}
-
-fs_status check_dtype(int32_t dtype) {
-  if (dtype != FS_F32 && dtype != FS_BF16) return fail(FS_ERR_INVALID, "dtype must be FS_F32 or FS_BF16");
-  return FS_OK;
-}
-
 // Workgroups of a grid over r x c tiles of 64 (256 threads each; a grid holds
 // fewer than 2^32 threads).
 bool grid_ok(int64_t r, int64_t c) { return (r + 63) / 64 * ((c + 63) / 64) < ((int64_t)1 << 24); }
@@ -134,18 +107,6 @@ fs_status check_norm(const fs_norm_desc* d) {
   if (d->center != 0 && d->center != 1) return fail(FS_ERR_INVALID, "center must be 0/1");
   if (!(d->eps > 0.f) || !(d->eps < 1e30f)) return fail(FS_ERR_INVALID, "eps must be > 0 and finite");
   return FS_OK;
-}
-
-int dt(int32_t dtype) { return dtype == FS_F32 ? 0 : 1; }
-
-// No exception (a message that finds no memory) leaves a C entry point.
-template <typename F>
-fs_status entry(F&& f) noexcept {
-  try {
-    return f();
-  } catch (...) {
-    return FS_ERR_INVALID;
-  }
 }
 
 }  // namespace

@@ -1,0 +1,107 @@
+// Attention over a paged cache: which kernel runs, on how many workgroups.
+// (The kernels are in attention_kernel.hpp, instantiated in attention_*.hip.)
+
+#include <math.h>
+
+#include "attention.hpp"
+
+namespace fs {
+namespace {
+
+constexpr int kWorkgroups = 512;   // of a divided call: two for each CU
+constexpr int kMaxGroups = 1 << 16;
+
+int width_of(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+int cache_of(int dtype, const PagedCache& c) {
+  return c.codes ? (dtype == 0 ? CACHE_CODES_F32 : CACHE_CODES_BF16) : dtype == 0 ? CACHE_F32 : CACHE_BF16;
+}
+
+// Row tiles of an item: what the rows of a sequence need, up to what the
+// registers hold (a row tile takes D / 4 of them for its sums and D / 8, in fp32
+// D / 4, for its queries).
+int row_tiles(int dtype, int width, int rows) {
+  const int most = dtype == 0 ? (width == 256 ? 1 : 2) : (width == 256 ? 2 : 4);
+  const int need = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  return need < most ? need : most;
+}
+
+struct Shape {
+  int width, rt, group, rows, row_groups;
+  int64_t items;
+  int workers;
+};
+Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
+  Shape h;
+  h.width = width_of(c.d);
+  h.group = q_heads / c.kv_heads;
+  h.rows = n_new * h.group;
+  h.rt = row_tiles(dtype, h.width, h.rows);
+  h.row_groups = (h.rows + 16 * h.rt - 1) / (16 * h.rt);
+  h.items = (int64_t)c.sequences * h.row_groups;
+  // A sequence of at most four tiles a wave is not worth a second launch;
+  // beyond kAttnMaxItems, or that many workgroups, there is enough to fill the chip.
+  const int tile = dtype == 0 ? 16 : 32;
+  const int64_t most = ((int64_t)c.max_pages * c.page_size + tile - 1) / tile;
+  h.workers = 0;
+  if (h.items <= kAttnMaxItems && h.items * c.kv_heads <= kMaxGroups && most > 4 * kAttnWaves) {
+    const int64_t parts = (h.items * most + kAttnMinTiles - 1) / kAttnMinTiles;
+    h.workers = (kWorkgroups + c.kv_heads - 1) / c.kv_heads;
+    if (parts < h.workers) h.workers = (int)parts;
+  }
+  return h;
+}
+
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+int64_t part_rows(const Shape& h, const PagedCache& c) { return (int64_t)h.workers * c.kv_heads * 2 * 16 * h.rt; }
+
+template <int CACHE, int D, int RT>
+hipError_t run_pages(const AttnPlan& p, hipStream_t s) {
+  return p.c.page_size % 16 == 0 ? run_attention<CACHE, D, RT, true>(p, s) : run_attention<CACHE, D, RT, false>(p, s);
+}
+template <int CACHE>
+hipError_t run_cache(int width, int rt, const AttnPlan& p, hipStream_t s) {
+  constexpr bool f32 = CACHE == CACHE_F32 || CACHE == CACHE_CODES_F32;
+  if (width == 256) {
+    if constexpr (!f32)
+      if (rt == 2) return run_pages<CACHE, 256, 2>(p, s);
+    return run_pages<CACHE, 256, 1>(p, s);
+  }
+  if (rt == 4) {
+    if constexpr (!f32) return width == 64 ? run_pages<CACHE, 64, 4>(p, s) : run_pages<CACHE, 128, 4>(p, s);
+  }
+  if (rt == 2) return width == 64 ? run_pages<CACHE, 64, 2>(p, s) : run_pages<CACHE, 128, 2>(p, s);
+  return width == 64 ? run_pages<CACHE, 64, 1>(p, s) : run_pages<CACHE, 128, 1>(p, s);
+}
+
+}  // namespace
+
+size_t attention_ws_bytes(int dtype, int q_heads, int n_new, const PagedCache& c) {
+  const Shape h = shape_of(dtype, q_heads, n_new, c);
+  if (!h.workers) return 0;
+  const int64_t rows = part_rows(h, c);
+  return up(rows * h.width * 4) + up(rows * 8) + up(h.items * 8);
+}
+
+hipError_t launch_attention(int dtype, const AttnArgs& a, const PagedCache& c, void* ws, hipStream_t s) {
+  const Shape h = shape_of(dtype, a.q_heads, a.n_new, c);
+  AttnPlan p{};
+  p.a = a, p.c = c;
+  p.group = h.group, p.rows = h.rows, p.row_groups = h.row_groups, p.items = (int)h.items, p.workers = h.workers;
+  p.scale2 = (float)(a.scale * M_LOG2E);
+  if (h.workers) {
+    const int64_t rows = part_rows(h, c);
+    char* w = (char*)ws;
+    p.part = (float*)w;
+    p.stat = (float2*)(w + up(rows * h.width * 4));
+    p.span = (int2*)(w + up(rows * h.width * 4) + up(rows * 8));
+  }
+  switch (cache_of(dtype, c)) {
+    case CACHE_BF16: return run_cache<CACHE_BF16>(h.width, h.rt, p, s);
+    case CACHE_F32: return run_cache<CACHE_F32>(h.width, h.rt, p, s);
+    case CACHE_CODES_BF16: return run_cache<CACHE_CODES_BF16>(h.width, h.rt, p, s);
+    default: return run_cache<CACHE_CODES_F32>(h.width, h.rt, p, s);
+  }
+}
+
+}  // namespace fs

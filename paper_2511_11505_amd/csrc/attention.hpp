@@ -1,0 +1,30 @@
+// What the attention's kernels are given (attention_kernel.hpp), and their
+// launch (instantiated in attention_*.hip).
+#pragma once
+
+#include "internal.hpp"
+
+namespace fs {
+
+enum { CACHE_BF16 = 0, CACHE_F32 = 1, CACHE_CODES_BF16 = 2, CACHE_CODES_F32 = 3 };
+
+constexpr int kAttnWaves = 4;
+constexpr int kAttnMaxItems = 4096;    // of a divided call: 16 for each thread
+constexpr int kAttnMinTiles = 4;       // of a workgroup's part: one for each wave
+
+struct AttnPlan {
+  AttnArgs a;
+  PagedCache c;
+  int group, rows;         // query heads a key head; rows = n_new * group
+  int row_groups, items;   // items = sequences * row_groups
+  int workers;             // parts, each of kv_heads workgroups; 0: one for each item
+  float scale2;            // scale * log2(e)
+  float* part;             // [workers * kv_heads * 2][rows of an item][D]
+  float2* stat;            // [workers * kv_heads * 2][rows of an item]: m, l
+  int2* span;              // [items]: first and last part
+};
+
+template <int CACHE, int D, int RT, bool P16>
+hipError_t run_attention(const AttnPlan& p, hipStream_t s);
+
+}  // namespace fs

@@ -1,0 +1,24 @@
+// Attention over a bf16 cache: the kernels of each width and row count.
+
+#include "attention_kernel.hpp"
+
+namespace fs {
+
+template hipError_t run_attention<CACHE_BF16, 64, 1, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 64, 1, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 64, 2, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 64, 2, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 64, 4, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 64, 4, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 128, 1, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 128, 1, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 128, 2, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 128, 2, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 128, 4, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 128, 4, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 256, 1, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 256, 1, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 256, 2, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_BF16, 256, 2, false>(const AttnPlan&, hipStream_t);
+
+}  // namespace fs

@@ -1,0 +1,18 @@
+// Attention over an 8-bit cache, fp32 queries: the kernels of each width and row count.
+
+#include "attention_kernel.hpp"
+
+namespace fs {
+
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 2, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 2, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 2, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 2, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, false>(const AttnPlan&, hipStream_t);
+
+}  // namespace fs

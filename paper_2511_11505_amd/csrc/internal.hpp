@@ -231,6 +231,49 @@ hipError_t launch_linear(int dtype, int m, int n, int k, const void* a, int64_t 
                          int64_t ldw, const LinearOut& o, void* ws, hipStream_t s);
 hipError_t launch_linear_backward(int dtype, const LinearBack& b, void* ws, hipStream_t s);
 
+// ---- rotary positions and the append to a paged cache (rotary.hip)
+// Rows of heads: element (token, head, column) at p + token * ts + head * hs + column.
+struct HeadRows {
+  const void* p;
+  int64_t ts, hs;
+};
+struct Rope {
+  bool halves;      // column i with i + rot / 2; else 2 i with 2 i + 1
+  int first, rot;
+  double mscale;
+  const double* freqs;
+};
+struct RotaryArgs {
+  int tokens, q_heads, kv_heads, d;   // kv_heads == 0: no cache
+  bool back;                          // turned the other way
+  Rope rope;
+  const int32_t* positions;
+  HeadRows q, out, k, v;              // out: of q
+  const int32_t* seqs;                // or null
+};
+// The cache and where its tokens are (fs_kv_cache, fs_page_table).
+struct PagedCache {
+  int codes, n_pages, kv_heads, page_size, d;
+  void *k, *v;
+  int64_t page_stride, head_stride, place_stride;
+  uint8_t *k_scales, *v_scales;
+  const int32_t* table;
+  int64_t ldt;
+  int sequences, max_pages;
+};
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, const PagedCache& c, hipStream_t s);
+
+// ---- attention over a paged cache (attention*.hip)
+struct AttnArgs {
+  int q_heads, n_new, window;
+  float scale;
+  HeadRows q, out;
+  const int32_t* lengths;
+  float* lse;   // or null
+};
+size_t attention_ws_bytes(int dtype, int q_heads, int n_new, const PagedCache& c);
+hipError_t launch_attention(int dtype, const AttnArgs& a, const PagedCache& c, void* ws, hipStream_t s);
+
 // ---- stand-in collectives (standin.hip)
 // Copy `bytes` from src to dst with `workgroups` workgroups, taking at least
 // `seconds` (0: unpaced); see the kernel's comment for the schedule.

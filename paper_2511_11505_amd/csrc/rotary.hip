@@ -1,0 +1,215 @@
+// Rotary positions, their backward pass, and the append to a paged cache.
+//
+// Pair (a, b) at angle t = position * f becomes (c a - s b, c b + s a) with c =
+// m cos t and s = m sin t; the backward pass is the transposed turn, s with its
+// sign changed.  Angles are products in 64 bits (at position 10^6 a 32-bit
+// product is off by 0.03 radians), reduced by quarter turns in 64 bits.
+//
+// Memory bounds it: a row is read once and written once, and the angles of a
+// token are shared by all its heads.  A wave has one token: its lanes compute
+// one angle each into LDS, then take the token's rows (q, k and v heads alike),
+// 8 columns a lane and several rows at once, the cosines and sines of their
+// columns in registers.  A row's lanes read it whole before they write, and a
+// row is one wave's, so a row may be turned in place.
+
+#include "internal.hpp"
+#include "saved.hpp"
+
+#pragma clang fp contract(off)   // each product of a turn is rounded
+
+namespace fs {
+namespace {
+
+constexpr int kMaxPairs = 256;   // rot <= 512
+constexpr int kUnroll = 4;       // rows a lane has in flight
+
+// cos and sin of t (|t| < 2^40): t less n quarter turns, by the sum of two
+// 64-bit parts of pi / 2, then the Taylor series to r^15 (|r| <= pi / 4: what
+// is left out is below 2^-49).
+__device__ __forceinline__ void cos_sin(double t, double& c, double& s) {
+  const double n = rint(t * 0.63661977236758134308);
+  double r = fma(-n, 1.57079632679489655800, t);
+  r = fma(-n, 6.12323399573676603587e-17, r);
+  const double x = r * r;
+  double a = -1.0 / 1307674368000.0;                    // sin: r^15 / 15!
+  a = fma(a, x, 1.0 / 6227020800.0);
+  a = fma(a, x, -1.0 / 39916800.0);
+  a = fma(a, x, 1.0 / 362880.0);
+  a = fma(a, x, -1.0 / 5040.0);
+  a = fma(a, x, 1.0 / 120.0);
+  a = fma(a, x, -1.0 / 6.0);
+  a = fma(a * x, r, r);
+  double b = -1.0 / 87178291200.0;                      // cos: r^14 / 14!
+  b = fma(b, x, 1.0 / 479001600.0);
+  b = fma(b, x, -1.0 / 3628800.0);
+  b = fma(b, x, 1.0 / 40320.0);
+  b = fma(b, x, -1.0 / 720.0);
+  b = fma(b, x, 1.0 / 24.0);
+  b = fma(b, x, -0.5);
+  b = fma(b, x, 1.0);
+  const int quarter = (int)(n - 4.0 * floor(n * 0.25));
+  const double cc = (quarter & 1) ? a : b, ss = (quarter & 1) ? b : a;
+  c = (quarter == 1 || quarter == 2) ? -cc : cc;
+  s = (quarter & 2) ? -ss : ss;
+}
+
+// FAST: chunks of 8 columns turn with a whole chunk or within themselves;
+// otherwise columns take their partners one by one.
+template <typename T, bool FAST, bool CACHE>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs g, PagedCache pc, int lanes_log2, int splits,
+                                                     int rows_per_split) {
+  __shared__ float2 table[4][kMaxPairs];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+  const int token = (int)(id / splits), split = (int)(id % splits);
+  if (token >= g.tokens) return;
+
+  const int pos = g.positions[token];
+  const int pairs = g.rope.rot / 2;
+  bool live = true;
+  int64_t page = -1;
+  int place = 0;
+  if constexpr (CACHE) {
+    const int seq = g.seqs ? g.seqs[token] : token;
+    live = pos >= 0 && seq >= 0 && seq < pc.sequences;
+    if (live) {
+      const int slot = pos / pc.page_size;
+      place = pos - slot * pc.page_size;
+      if (slot < pc.max_pages) page = pc.table[(int64_t)seq * pc.ldt + slot];
+      if (page >= pc.n_pages) page = -1;
+    }
+  }
+  for (int p = lane; p < pairs; p += 64) {
+    double c, s;
+    cos_sin((double)pos * g.rope.freqs[p], c, s);
+    table[wave][p] = make_float2((float)(c * g.rope.mscale), (float)(s * (g.back ? -g.rope.mscale : g.rope.mscale)));
+  }
+  // (the wave's own writes: LDS serves a wave in order)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+
+  // this lane's columns and what they turn with
+  const int lpr = 1 << lanes_log2, per_wave = 64 >> lanes_log2;
+  const int c0 = (lane & (lpr - 1)) * 8, n = min(8, g.d - c0);
+  const bool halves = g.rope.halves;
+  float cs[8], sn[8];
+  uint32_t turns = 0, ahead = 0;    // bit i: column c0 + i turns; its partner is ahead
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int at = c0 + i - g.rope.first;
+    const bool t = i < n && at >= 0 && at < g.rope.rot;
+    const bool a = halves ? at < pairs : !(at & 1);     // first of its pair
+    const int p = halves ? (a ? at : at - pairs) : at >> 1;
+    const float2 w = t ? table[wave][p] : make_float2(1.f, 0.f);
+    cs[i] = w.x;
+    sn[i] = a ? -w.y : w.y;
+    turns |= (uint32_t)t << i;
+    ahead |= (uint32_t)a << i;
+  }
+  const int step = halves ? pairs : 1;
+
+  const int rows = g.q_heads + 2 * g.kv_heads;
+  const int end = min(rows, (split + 1) * rows_per_split);
+  for (int r0 = split * rows_per_split + (lane >> lanes_log2); r0 - (lane >> lanes_log2) < end;
+       r0 += kUnroll * per_wave) {
+    Raw8<T> own[kUnroll], other[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int r = r0 + u * per_wave;
+      own[u] = other[u] = {};
+      if (r >= end || n <= 0) continue;
+      const bool isq = !CACHE || r < g.q_heads;
+      const bool isk = CACHE && !isq && r < g.q_heads + g.kv_heads;
+      const HeadRows& h = isq ? g.q : isk ? g.k : g.v;
+      const int head = isq ? r : isk ? r - g.q_heads : r - g.q_heads - g.kv_heads;
+      const T* src = (const T*)h.p + (int64_t)token * h.ts + head * h.hs + c0;
+      own[u] = load8<T>(src, n);
+      if (turns && (isq || isk)) {
+        if constexpr (FAST) {
+          if (halves) other[u] = load8<T>(src + ((ahead & 1) ? pairs : -pairs), 8);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (turns >> i & 1) {
+              const T v = src[i + ((ahead >> i & 1) ? step : -step)];
+              if constexpr (sizeof(T) == 4) other[u].w[i] = __float_as_uint(v);
+              else other[u].w[i >> 1] |= (uint32_t)v << (16 * (i & 1));
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int r = r0 + u * per_wave;
+      const bool in = r < end && n > 0;
+      const bool isq = !CACHE || r < g.q_heads;
+      const bool isk = CACHE && !isq && r < g.q_heads + g.kv_heads;
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = own[u].get(i);
+        const float y = FAST && !halves ? own[u].get(i ^ 1) : other[u].get(i);
+        v[i] = (turns >> i & 1) && (isq || isk) ? x * cs[i] + y * sn[i] : x;
+      }
+      if (isq) {
+        if (CACHE && !live) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        }
+        if (in) store8<T>((T*)g.out.p + (int64_t)token * g.out.ts + r * g.out.hs + c0, v, n);
+      }
+      if constexpr (CACHE) {
+        const int head = isk ? r - g.q_heads : r - g.q_heads - g.kv_heads;
+        const bool put = in && !isq && live && page >= 0;
+        const int64_t at = page * pc.page_stride + head * pc.head_stride + place * pc.place_stride + c0;
+        if (pc.codes) {
+          const int b = ckpt_byte(block_max<LANES_NEXT>(put ? amax8(v) : 0));
+          if (put) {
+            store_codes((uint8_t*)(isk ? pc.k : pc.v) + at, ckpt_codes(v, b), 8);
+            if (c0 % kCkptBlock == 0)
+              (isk ? pc.k_scales : pc.v_scales)[((page * pc.kv_heads + head) * pc.page_size + place) *
+                                                    ((g.d + kCkptBlock - 1) / kCkptBlock) +
+                                                c0 / kCkptBlock] = (uint8_t)b;
+          }
+        } else if (put) {
+          store8<T>((T*)(isk ? pc.k : pc.v) + at, v, 8);
+        }
+      }
+    }
+  }
+}
+
+template <typename T>
+hipError_t run(const RotaryArgs& g, const PagedCache& pc, hipStream_t s) {
+  int lg = 2;
+  while ((8 << lg) < g.d) ++lg;
+  const int rows = g.q_heads + 2 * g.kv_heads, per_wave = 64 >> lg;
+  // A wave takes all of a token's rows while the tokens alone make 16 waves a
+  // CU (an angle is computed once); fewer tokens are split over more waves,
+  // down to one batch of rows in flight each.
+  const int batch = per_wave * kUnroll, most = (rows + batch - 1) / batch;
+  int splits = (int)((4096 + g.tokens - 1) / g.tokens);
+  splits = splits < most ? splits : most;
+  const int rps = (most + splits - 1) / splits * batch;
+  splits = (rows + rps - 1) / rps;
+  const bool halves = g.rope.halves;
+  const bool fast = g.d % 8 == 0 && (halves ? g.rope.first % 8 == 0 && g.rope.rot % 16 == 0 : g.rope.first % 2 == 0);
+  const dim3 grid((unsigned)cdiv64((int64_t)g.tokens * splits, 4));
+  if (g.kv_heads) {
+    if (fast) launch_k(rotary_kernel<T, true, true>, grid, 256, 0, s, g, pc, lg, splits, rps);
+    else launch_k(rotary_kernel<T, false, true>, grid, 256, 0, s, g, pc, lg, splits, rps);
+  } else {
+    if (fast) launch_k(rotary_kernel<T, true, false>, grid, 256, 0, s, g, pc, lg, splits, rps);
+    else launch_k(rotary_kernel<T, false, false>, grid, 256, 0, s, g, pc, lg, splits, rps);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, const PagedCache& c, hipStream_t s) {
+  return dtype == 0 ? run<float>(a, c, s) : run<bf16_t>(a, c, s);
+}
+
+}  // namespace fs

@@ -1,0 +1,471 @@
+"""Rotary positions, the append to a paged cache and paged attention on the GPU
+against the fp64 oracle.
+
+Tolerances are bounds, from the operations that round (2^-24 each in fp32, half a
+step of a stored type: bf16 2^-8 of the value, fp32 2^-24).
+
+Rotation: cos, sin, each product and the sum round once: 3 * 2^-24 of
+mscale (|a| + |b|), then the store.
+
+Attention: a score of d products errs by at most (d + 2) 2^-23 of sum |q k| scale
+(products and adds, and the factor scale log2 e with its own rounding); the
+exponential turns that into a relative error, and its own is at most 2^-21; a sum
+of L weights errs by L 2^-24 of it, the rescalings (at most one for each of 64 first
+tiles and each join) by 2^-20; a weight that is rounded to bf16 by 2^-8.  An output
+errs by that much of sum |weight v|, twice (sum of values, sum of weights), then
+the store."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_11505_amd as fs
+from oracle import attention as O
+from paper_2511_11505_amd import _lib as L
+from tests._util import f64
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+DEV = "cuda"
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+U = 2.0 ** -23
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def heads(g, tokens, n, d, dtype, pad=0, lead=0, head_major=False, scale=1.0):
+    """[tokens, n, d] view inside NaNs."""
+    a, b = (n, tokens) if head_major else (tokens, n)
+    full = torch.full((a * (b * d + pad) + pad + lead + 64,), float("nan"), dtype=TORCH[dtype], device=DEV)
+    v = full[lead:lead + a * (b * d + pad)].view(a, b * d + pad)[:, :b * d].unflatten(1, (b, d))
+    v = v.transpose(0, 1) if head_major else v
+    v.copy_(scale * torch.randn((tokens, n, d), generator=g, device=DEV))
+    return v
+
+
+class Out:
+    """An output inside a buffer of a sentinel, which has to stay."""
+
+    def __init__(self, tokens, n, d, dtype, pad=0, lead=0):
+        self.full = torch.full((tokens * (n * d + pad) + lead + 64,), -77.0, dtype=TORCH[dtype], device=DEV)
+        self.at = (tokens, n, d, pad, lead)
+        self.view = self.cut(self.full)
+
+    def cut(self, full):
+        tokens, n, d, pad, lead = self.at
+        return full[lead:lead + tokens * (n * d + pad)].view(tokens, n * d + pad)[:, :n * d].unflatten(1, (n, d))
+
+    def get(self):
+        rest = self.full.clone()
+        self.cut(rest).fill_(-77.0)
+        assert bool((rest == -77.0).all()), "wrote outside the output"
+        return f64(self.view)
+
+
+def near(got, want, tol):
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4],
+                           np.broadcast_to(tol, got.shape)[bad][:4])
+
+
+def turn_tol(x, freqs, layout, first, mscale, want, dtype):
+    a, b = O.pairs(2 * len(freqs), layout, first)
+    size = np.zeros(x.shape)
+    both = np.abs(x[..., a]) + np.abs(x[..., b])
+    size[..., a], size[..., b] = both, both
+    t = 3 * 2.0 ** -24 * abs(mscale) * size
+    return t + HALF[dtype] * (np.abs(want) + t)
+
+
+def spun(rot, layout, first=0, mscale=1.0, **kw):
+    f = fs.fs_rope_frequencies(rot, **kw)
+    return f.numpy(), fs.rope(f.to(DEV), layout=layout, first=first, mscale=mscale)
+
+
+# ------------------------------------------------------------------- rotary
+ROTARY = [  # tokens, heads, d, rot, first, pad, lead
+    (1, 1, 2, 2, 0, 0, 0), (1, 48, 128, 128, 0, 0, 0), (3, 5, 64, 64, 0, 0, 0), (5, 3, 75, 38, 3, 5, 1),
+    (257, 7, 128, 64, 64, 0, 0), (130, 9, 192, 64, 128, 8, 0), (17, 2, 256, 256, 0, 1, 0), (2, 3, 512, 512, 0, 0, 0),
+    (9, 1, 511, 500, 11, 3, 1), (33, 4, 96, 20, 4, 0, 0), (1, 300, 8, 8, 0, 0, 0), (4, 6, 16, 0, 5, 0, 0),
+    (700, 33, 72, 48, 16, 8, 0), (5000, 2, 24, 16, 8, 0, 0)]
+
+
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", ROTARY, ids=str)
+def test_rotary(case, dtype, layout):
+    tokens, n, d, rot, first, pad, lead = case
+    g = gen(tokens + d)
+    x = heads(g, tokens, n, d, dtype, pad, lead)
+    pos = torch.randint(-50, 1 << 20, (tokens,), generator=g, device=DEV, dtype=torch.int32)
+    freqs, rope = spun(rot, layout, first, 1.25, scaling="linear", factor=2.0)
+    desc = fs.rotary_desc(tokens, n, d, dtype)
+    for back, call in ((False, fs.fs_rotary), (True, fs.fs_rotary_backward)):
+        out = Out(tokens, n, d, dtype, pad, lead)
+        call(desc, rope, x, pos, out.view)
+        torch.cuda.synchronize()
+        want = O.rotary(f64(x), pos.cpu().numpy(), freqs, layout, first, 1.25, back)
+        near(out.get(), want, turn_tol(f64(x), freqs, layout, first, 1.25, want, dtype))
+        # in place: the same bits
+        y = heads(g, tokens, n, d, dtype, pad, lead)
+        y.copy_(x)
+        call(desc, rope, y, pos, y)
+        torch.cuda.synchronize()
+        assert torch.equal(y, out.view)
+
+
+def test_rotary_head_major():
+    """Heads that hold their tokens, and an output of the other order."""
+    g = gen(3)
+    x = heads(g, 65, 6, 64, "bf16", 8, head_major=True)
+    pos = torch.randint(0, 5000, (65,), generator=g, device=DEV, dtype=torch.int32)
+    freqs, rope = spun(32, "pairs", 16)
+    out = Out(65, 6, 64, "bf16")
+    fs.fs_rotary(fs.rotary_desc(65, 6, 64), rope, x, pos, out.view)
+    torch.cuda.synchronize()
+    want = O.rotary(f64(x), pos.cpu().numpy(), freqs, "pairs", 16)
+    near(out.get(), want, turn_tol(f64(x), freqs, "pairs", 16, 1.0, want, "bf16"))
+
+
+def test_rotary_far_positions():
+    """The ends of the positions' range: angles are products in 64 bits."""
+    pos = torch.tensor([2 ** 31 - 1, -2 ** 31, 2 ** 30 + 1, 0, 1], dtype=torch.int32, device=DEV)
+    x = heads(gen(5), 5, 2, 64, "f32")
+    freqs, rope = spun(64, "halves")
+    out = Out(5, 2, 64, "f32")
+    fs.fs_rotary(fs.rotary_desc(5, 2, 64, "f32"), rope, x, pos, out.view)
+    torch.cuda.synchronize()
+    want = O.rotary(f64(x), pos.cpu().numpy(), freqs, "halves")
+    # (angles of 2^31 radians in 64 bits: 2^-22 absolute, on both sides)
+    near(out.get(), want, turn_tol(f64(x), freqs, "halves", 0, 1.0, want, "f32") + 2.0 ** -21 * np.abs(f64(x)).max())
+    near(out.get()[3:], want[3:], turn_tol(f64(x), freqs, "halves", 0, 1.0, want, "f32")[3:])
+
+
+def test_rotary_keeps_what_is_beside():
+    """Infinities and NaNs stay in their pairs and in columns that do not turn."""
+    x = torch.randn((4, 2, 64), generator=gen(1), device=DEV)
+    x[0, 0, 3], x[1, 1, 60], x[2, 0, 40] = float("inf"), float("nan"), float("-inf")
+    pos = torch.tensor([1, 2, 3, 4], dtype=torch.int32, device=DEV)
+    freqs, rope = spun(32, "halves")
+    out = torch.empty_like(x)
+    fs.fs_rotary(fs.rotary_desc(4, 2, 64, "f32"), rope, x, pos, out)
+    torch.cuda.synchronize()
+    bad = ~torch.isfinite(out)
+    assert bad.nonzero().tolist() == [[0, 0, 3], [0, 0, 19], [1, 1, 60], [2, 0, 40]]
+    assert torch.isnan(out[1, 1, 60]) and out[2, 0, 40] == float("-inf")
+
+
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+def test_rotary_gradient_by_differences(layout):
+    """<dout, f(x + h e) - f(x - h e)> / 2 h is dx . e: f is linear, so the only
+    errors are roundings: of both outputs (3 * 2^-24 each), of dx and of the sums."""
+    g = gen(11)
+    x, dout, e = (heads(g, 6, 3, 48, "f32") for _ in range(3))
+    pos = torch.randint(0, 9000, (6,), generator=g, device=DEV, dtype=torch.int32)
+    _, rope = spun(32, layout, 8, 1.5)
+    desc = fs.rotary_desc(6, 3, 48, "f32")
+    up, down, dx = (torch.empty((6, 3, 48), device=DEV) for _ in range(3))
+    fs.fs_rotary(desc, rope, x + e, pos, up)
+    fs.fs_rotary(desc, rope, x - e, pos, down)
+    fs.fs_rotary_backward(desc, rope, dout, pos, dx)
+    torch.cuda.synchronize()
+    lhs = (f64(dout) * (f64(up) - f64(down))).sum() / 2
+    rhs = (f64(dx) * f64(e)).sum()
+    size = (np.abs(f64(dout)).sum() + np.abs(f64(e)).sum()) * 2 * 1.5 * 4 * (
+        np.abs(f64(x)).max() + np.abs(f64(e)).max() + np.abs(f64(dout)).max())
+    assert abs(lhs - rhs) <= 4 * 2.0 ** -24 * size
+
+
+# -------------------------------------------------------------------- cache
+class Cache:
+    """A cache of random values, or of NaNs, with the strides of a larger one
+    whose rest is a sentinel."""
+
+    def __init__(self, g, pages, kv, size, d, dtype, codes=False, order="heads", gap=0, poison=False):
+        shape = {"heads": (pages, kv, size, d + gap), "tokens": (pages, size, kv, d + gap)}[order]
+        dt = torch.uint8 if codes else TORCH[dtype]
+
+        def make():
+            full = torch.full(shape, 0x33 if codes else -77.0, dtype=dt, device=DEV)
+            v = full if order == "heads" else full.transpose(1, 2)
+            return full, v[..., :d]
+
+        self.full, self.k = make()
+        self.fullv, self.v = make()
+        self.ks = self.vs = None
+        self.d, self.codes, self.dtype = d, codes, dtype
+        if codes:
+            nb = (d + 31) // 32
+            self.ks, self.vs = (torch.full((pages, kv, size, nb), 255 if poison else 127, dtype=torch.uint8, device=DEV)
+                                for _ in range(2))
+        for x, s in ((self.k, self.ks), (self.v, self.vs)):
+            if poison:
+                x.fill_(0x7F if codes else float("nan"))
+            elif codes:
+                x.copy_(torch.randint(0, 127, x.shape, generator=g, device=DEV) * 1
+                        + 128 * torch.randint(0, 2, x.shape, generator=g, device=DEV))
+                x.bitwise_and_(0xBF)          # (below 2^1: softmaxes of more than one token)
+                s.copy_(torch.randint(124, 128, s.shape, generator=g, device=DEV))
+            else:
+                x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        self.struct = fs.kv_cache(self.k, self.v, self.ks, self.vs, dtype=dtype)
+
+    def values(self):
+        if self.codes:
+            return tuple(O.decoded(x.contiguous().cpu().numpy(), s.cpu().numpy())
+                         for x, s in ((self.k, self.ks), (self.v, self.vs)))
+        return f64(self.k), f64(self.v)
+
+    def gaps(self):
+        for full in (self.full, self.fullv):
+            rest = full[..., self.d:]
+            assert bool((rest == (0x33 if self.codes else -77.0)).all()), "wrote between the rows"
+
+
+def pages_of(g, lens, size, spare=2, width=None):
+    """A table with every sequence's pages in random order; other entries bad."""
+    counts = [(max(n, 0) + size - 1) // size for n in lens]
+    total = sum(counts) + spare
+    order = torch.randperm(total, generator=g, device=DEV).int()
+    full = torch.full((len(lens), (width or max(1, *counts, 1)) + 3), 2 ** 30, dtype=torch.int32, device=DEV)
+    table = full[:, :full.shape[1] - 3]
+    table.fill_(-1)
+    at = 0
+    for b, c in enumerate(counts):
+        table[b, :c] = order[at:at + c]
+        at += c
+    return table, total
+
+
+APPEND = [  # tokens per sequence, starts, q heads, kv heads, d, rot, first, page, layout, pad
+    ([1, 1, 1], [0, 17, 63], 4, 2, 128, 128, 0, 16, "halves", 0),
+    ([5, 0, 40], [3, 9, 0], 6, 3, 80, 40, 16, 21, "pairs", 3),
+    ([33], [31], 1, 1, 8, 8, 0, 1, "halves", 0),
+    ([7, 2], [100, 0], 40, 8, 128, 64, 64, 64, "halves", 8),
+    ([64, 64], [0, 5], 2, 2, 256, 256, 0, 7, "pairs", 0),
+    ([9], [0], 3, 3, 72, 20, 4, 5, "halves", 1),
+    ([300, 1], [10, 700], 5, 1, 64, 0, 0, 48, "halves", 0)]
+
+
+@pytest.mark.parametrize("order", ["heads", "tokens"])
+@pytest.mark.parametrize("kind", ["bf16", "f32", "bf16 codes", "f32 codes"])
+@pytest.mark.parametrize("case", APPEND, ids=str)
+def test_append(case, kind, order):
+    counts, starts, h, kv, d, rot, first, size, layout, pad = case
+    dtype, codes = kind.split()[0], "codes" in kind
+    g = gen(d + size)
+    table, pages = pages_of(g, [a + b for a, b in zip(counts, starts)], size)
+    cache = Cache(g, pages, kv, size, d, dtype, codes, order, gap=8)
+    before = cache.values()
+    seqs = [b for b, n in enumerate(counts) for _ in range(n)]
+    pos = [s + i for s, n in zip(starts, counts) for i in range(n)]
+    # tokens in any order, some of them none
+    perm = torch.randperm(len(seqs), generator=g, device=DEV).tolist()
+    seqs, pos = [seqs[i] for i in perm] + [0, -1, len(counts)], [pos[i] for i in perm] + [-1, 3, 3]
+    t = len(seqs)
+    qkv = heads(g, t, h + 2 * kv, d, dtype, pad)
+    q, k, v = qkv.split((h, kv, kv), dim=1)
+    freqs, rope = spun(rot, layout, first, 0.75)
+    out = Out(t, h, d, dtype, pad)
+    fs.fs_cache_append(cache.struct, rope, q, k, v, torch.tensor(seqs, dtype=torch.int32, device=DEV),
+                       torch.tensor(pos, dtype=torch.int32, device=DEV), table, out.view)
+    torch.cuda.synchronize()
+    cache.gaps()
+    Q, K, V = f64(q), f64(k), f64(v)
+    want = O.rotary(Q, pos, freqs, layout, first, 0.75)
+    tol = turn_tol(Q, freqs, layout, first, 0.75, want, dtype)
+    want[-3:], tol[-3:] = 0.0, 0.0
+    near(out.get(), want, tol)
+    turned = O.rotary(K, pos, freqs, layout, first, 0.75)
+    tol = turn_tol(K, freqs, layout, first, 0.75, turned, "f32" if codes else dtype)
+    got_k, got_v = cache.values()
+    tb = table.cpu().numpy()
+    old_k, old_v = before
+    if codes:
+        # half a code's step: 2^-4 of the value, of the least normal code (2^-6)
+        # of the block's scale below it; a block's scale may differ by a rounding
+        # of its largest value
+        _, scales = O.coded(turned)
+        step = 2.0 ** (np.repeat(scales.astype(float), 32, axis=-1)[..., :d] - 127)
+        tol = 2 * (tol + np.maximum(2.0 ** -4 * np.abs(turned), 2.0 ** -10 * step))
+        V = O.decoded(*O.coded(V))
+    near(got_k, O.append(old_k, turned, seqs, pos, tb), O.append(np.zeros(old_k.shape), tol, seqs, pos, tb))
+    near(got_v, O.append(old_v, V, seqs, pos, tb), 0.0)
+
+
+def test_append_turned_codes_are_those_of_the_fp32_rows():
+    """The codes of turned rows: an fp32 cache's rows, coded."""
+    g = gen(2)
+    table, pages = pages_of(g, [50], 16)
+    k, v = heads(g, 50, 2, 96, "f32"), heads(g, 50, 2, 96, "f32")
+    pos = torch.arange(50, dtype=torch.int32, device=DEV)
+    seqs = torch.zeros_like(pos)
+    _, rope = spun(96, "halves")
+    rows, coded = (Cache(g, pages, 2, 16, 96, "f32", codes) for codes in (False, True))
+    for c in (rows, coded):
+        fs.fs_cache_append(c.struct, rope, None, k, v, seqs, pos, table, None)
+    torch.cuda.synchronize()
+    for x, codes, scales in ((rows.k, coded.k, coded.ks), (rows.v, coded.v, coded.vs)):
+        at = [(int(table[0, p // 16]), p % 16) for p in range(50)]
+        want = O.coded(np.stack([f64(x[a, :, b]) for a, b in at]))
+        assert np.array_equal(want[0], np.stack([codes[a, :, b].cpu().numpy() for a, b in at]))
+        assert np.array_equal(want[1], np.stack([scales[a, :, b].cpu().numpy() for a, b in at]))
+
+
+def test_append_holes():
+    """Bad entries of the table, positions behind it, no sequence ids, no rotation;
+    infinities and NaNs as codes."""
+    g = gen(9)
+    table = torch.tensor([[-1, 0], [1, 7], [2 ** 31 - 1, -2 ** 31], [2, 3]], dtype=torch.int32, device=DEV)
+    for codes in (False, True):
+        cache = Cache(g, 4, 2, 4, 32, "bf16", codes)
+        before = cache.values()
+        k, v = heads(g, 4, 2, 32, "bf16"), heads(g, 4, 2, 32, "bf16")
+        k[3, 1, 5], v[3, 0, 0] = float("inf"), float("nan")
+        pos = torch.tensor([0, 5, 1, 6], dtype=torch.int32, device=DEV)
+        fs.fs_cache_append(cache.struct, None, None, k, v, None, pos, table, None)
+        fs.fs_cache_append(cache.struct, None, None, k, v, None, pos + 100, table, None)
+        torch.cuda.synchronize()
+        got = cache.values()
+        for x, (old, new) in zip((k, v), zip(before, got)):
+            changed = np.argwhere((old != new).any((1, 3)))
+            assert changed.tolist() == [[3, 2]]
+            want = f64(x[3])
+            if codes:
+                want = O.decoded(*O.coded(want))
+            assert np.array_equal(new[3, :, 2], want, equal_nan=True)
+
+
+# ---------------------------------------------------------------- attention
+LENGTHS = {"small": [0, 1, 2, 15, 16, 17, 31, 33], "mid": [63, 64, 65, 300, 1, 0, 129, 128], "long": [1000, 3, 2049, 0],
+           "one": [4097]}
+
+
+def check_attention(kind, h, kv, d, lens, size, new=1, window=0, pad=0, order="heads", gap=0, seed=0, scale=None,
+                    holes=(), lead=0):
+    dtype, codes = kind.split()[0], "codes" in kind
+    g = gen(seed + d + size + h)
+    table, pages = pages_of(g, lens, size)
+    cache = Cache(g, pages, kv, size, d, dtype, codes, order, gap, poison=True)
+    real = Cache(g, pages, kv, size, d, dtype, codes, order, gap)
+    # only the places that hold tokens are not NaN
+    for b, n in enumerate(lens):
+        for j in range(n):
+            a, p = int(table[b, j // size]), j % size
+            for x, y in ((cache.k, real.k), (cache.v, real.v), (cache.ks, real.ks), (cache.vs, real.vs)):
+                if x is not None:
+                    x[a, :, p] = y[a, :, p]
+            if size >= 16 and p == 0:      # whole pages at once
+                stop = min(size, n - j)
+                for x, y in ((cache.k, real.k), (cache.v, real.v), (cache.ks, real.ks), (cache.vs, real.vs)):
+                    if x is not None:
+                        x[a, :, :stop] = y[a, :, :stop]
+    for b, slot, value in holes:
+        table[b, slot] = value
+    t = len(lens) * new
+    q = heads(g, t, h, d, dtype, pad, lead)
+    scale = d ** -0.5 if scale is None else scale
+    desc = fs.attention_desc(h, new, scale, window)
+    need = fs.fs_paged_attention_workspace(desc, cache.struct, table)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+    out = Out(t, h, d, dtype, pad, lead)
+    lse = torch.full((t + 1, h), -77.0, device=DEV)
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    fs.fs_paged_attention(desc, cache.struct, q, lengths, table, out.view, (ws.data_ptr(), need), lse=lse[:t])
+    torch.cuda.synchronize()
+    assert bool((ws[need:] == 0xFF).all()) and bool((lse[t] == -77.0).all())
+    k, v = cache.values()
+    want, want_lse, mass, reach = O.attention(f64(q), k, v, lens, table.cpu().numpy(), new, float(np.float32(scale)),
+                                              window)
+    got, got_lse = out.get(), f64(lse[:t])
+    longest = max(lens)
+    err = np.expm1((d + 2) * U * reach) + 2.0 ** -21 + longest * 2.0 ** -24 + 2.0 ** -20
+    weight = err + (2.0 ** -8 if dtype == "bf16" else 0)
+    tol = (2 * weight)[..., None] * mass
+    near(got, want, tol + HALF[dtype] * (np.abs(want) + tol))
+    none = np.isneginf(want_lse)
+    assert np.array_equal(none, np.isneginf(got_lse)) and (got[none] == 0).all()
+    near(got_lse[~none], want_lse[~none], (2 * err + 2.0 ** -22 * np.abs(np.where(none, 0, want_lse)))[~none])
+    # the same call gives the same bits, without lse too
+    again = Out(t, h, d, dtype, pad, lead)
+    fs.fs_paged_attention(desc, cache.struct, q, lengths, table, again.view, (ws.data_ptr(), need))
+    torch.cuda.synchronize()
+    assert np.array_equal(again.get(), got)
+
+
+KINDS = ["bf16", "f32", "bf16 codes", "f32 codes"]
+
+
+@pytest.mark.parametrize("lens", ["small", "mid"])
+@pytest.mark.parametrize("size", [1, 5, 16, 48])
+@pytest.mark.parametrize("kind", KINDS)
+def test_attention(kind, size, lens):
+    check_attention(kind, 10, 2, 128, LENGTHS[lens], size)
+
+
+@pytest.mark.parametrize("d", [8, 64, 72, 96, 136, 192, 256])
+@pytest.mark.parametrize("kind", KINDS)
+def test_attention_widths(kind, d):
+    check_attention(kind, 3, 3, d, LENGTHS["small"], 16)
+    check_attention(kind, 4, 2, d, [70, 700, 5], 20, new=2)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("h,kv,new", [(1, 1, 1), (7, 1, 1), (16, 1, 1), (17, 1, 1), (32, 1, 1), (33, 1, 1), (64, 1, 1),
+                                      (65, 1, 2), (10, 5, 7), (40, 8, 4), (4, 4, 40)])
+def test_attention_rows(kind, h, kv, new):
+    """Query heads of a key head and new tokens, up to more rows than one tile
+    holds; sequences shorter than the new tokens."""
+    check_attention(kind, h, kv, 64, [90, 3, 0, 41], 16, new=new)
+    check_attention(kind, h, kv, 128, [600, 20], 16, new=new)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "bf16 codes"])
+@pytest.mark.parametrize("window", [1, 5, 16, 33, 200, 5000])
+@pytest.mark.parametrize("new", [1, 3])
+def test_attention_window(kind, window, new):
+    check_attention(kind, 4, 2, 128, LENGTHS["mid"], 16, new=new, window=window)
+    check_attention(kind, 4, 2, 64, LENGTHS["mid"], 7, new=new, window=window)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("lens", ["long", "one"])
+def test_attention_divided(kind, lens):
+    """Sequences in several parts, and parts of several sequences."""
+    check_attention(kind, 5, 1, 128, LENGTHS[lens], 16)
+    check_attention(kind, 6, 3, 72, LENGTHS[lens], 9, new=2)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "bf16 codes"])
+def test_attention_many_sequences(kind):
+    """More sequences than the scan has threads, and more than are divided."""
+    g = torch.Generator().manual_seed(4)
+    lens = torch.randint(0, 40, (600,), generator=g).tolist()
+    lens[77] = 900
+    check_attention(kind, 2, 1, 64, lens, 16)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32 codes"])
+def test_attention_strides(kind):
+    check_attention(kind, 6, 2, 80, [50, 130, 0], 16, order="tokens", gap=8, pad=3, lead=1)
+    check_attention(kind, 6, 2, 128, [50, 300, 0], 16, order="tokens", gap=0, pad=8)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "bf16 codes"])
+@pytest.mark.parametrize("size", [16, 5])
+def test_attention_holes(kind, size):
+    """Pages that are not there; a sequence without any."""
+    lens = [100, 16, 40, 33]
+    holes = [(0, 1, -1), (0, 3, 2 ** 31 - 1), (2, 0, -2 ** 31)] + [(1, i, 999) for i in range((16 + size - 1) // size)]
+    check_attention(kind, 4, 2, 64, lens, size, holes=holes)
+    check_attention(kind, 4, 2, 64, lens, size, holes=holes, new=3, window=20)
+
+
+def test_attention_scales():
+    """A factor of 0, a negative one, and one that leaves one token."""
+    for scale in (0.0, -0.5, 40.0):
+        check_attention("f32", 4, 2, 64, [5, 70, 33], 16, scale=scale)
+        check_attention("bf16", 4, 2, 64, [5, 70, 33], 16, scale=scale)
