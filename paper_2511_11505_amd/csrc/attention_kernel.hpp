@@ -22,8 +22,8 @@
 //  * The result again has a query row in each lane column: the statistics are
 //    per lane, and rescaling needs no exchange.
 //
-// A wave runs one tile ahead (16 KB of a bf16 cache of head_dim 128 in flight
-// beside the 16 KB in use).  The tokens of all sequences are divided evenly over
+// A wave holds one tile of keys and one of values: the next keys are on their way
+// while the values are multiplied, the next values while the keys are.  The tokens of all sequences are divided evenly over
 // a fixed number of workgroups whatever the lengths are (the host does not know
 // them); a workgroup's part may hold the end of one sequence, whole ones and
 // the start of another.  Parts of a sequence are joined by a second kernel in
@@ -70,6 +70,26 @@ __device__ __forceinline__ float row_sum(float v) {
 }
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 
+// Memory from a uniform address on; offsets at or above kNone read 0.
+constexpr uint32_t kNone = 0x80000000u;
+struct Buffer {
+  __amdgpu_buffer_rsrc_t r;
+  __device__ __forceinline__ explicit Buffer(const void* p)
+      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(kNone - 1), 0x20000)) {}
+  __device__ __forceinline__ uint32_t load1(uint32_t off) const { return __builtin_amdgcn_raw_buffer_load_b8(r, off, 0, 0); }
+  __device__ __forceinline__ uint32_t load2(uint32_t off) const { return __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0); }
+  __device__ __forceinline__ uint32_t load4(uint32_t off) const { return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0); }
+  __device__ __forceinline__ void load(u32x1_any& v, uint32_t off) const { v[0] = load4(off); }
+  __device__ __forceinline__ void load(u32x2_any& v, uint32_t off) const {
+    const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+    v[0] = x[0], v[1] = x[1];
+  }
+  __device__ __forceinline__ void load(u32x4_any& v, uint32_t off) const {
+    const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    v[0] = x[0], v[1] = x[1], v[2] = x[2], v[3] = x[3];
+  }
+};
+
 // What an item (a sequence, or a part of its rows) reads.
 struct Item {
   int seq, row0, nrows, len;
@@ -113,38 +133,38 @@ struct Attn {
   static constexpr int VT = 4 * NG;                          // tokens of V a lane holds
   static constexpr int NO = D / 16;                          // result tiles of a row tile
   static constexpr int STRIDE = D + 4;                       // LDS row (floats)
+  static constexpr int NB = D / kCkptBlock;                  // scale bytes of a full-width row
+  static constexpr int KW = (NB + 3) / 4;                    // words of a row's scales; of 4 rows': NB
   typedef typename std::conditional<kF32, float, bf16_t>::type T;
   typedef typename RawT<KE * ES>::type KRaw;
   typedef typename RawT<VE * ES>::type VRaw;
-  static_assert(TILE * 16 <= 16 * STRIDE, "a wave's probabilities fit its part of the LDS");
 
-  struct Tile {
-    KRaw k[NG][KC];
-    VRaw v[VC][VT];
-    uint8_t ks[kCodes ? NG : 1][KC], vs[VC][kCodes ? VT : 1];
-    uint32_t ok;     // bit t: token t has a place
-    bool full;       // every row sees every token
-  };
+  typedef uint32_t Frag __attribute__((ext_vector_type(4)));
 
   const AttnPlan& p;
-  float* lds;        // this wave's 16 rows of STRIDE
   const int lane, q, g, head;
   Item it;
   // pages: lane i has the offset (elements, of the head's part) of the group
   // (P16) or token window + i, or -1, and its index among the scale rows
   int window;
   int64_t base, srow;
-  int koff[KC], voff[VC];
-  int lim[RT], low[RT];
+  uint32_t koff[KC], voff[VC][4];   // bytes in a row; P16: from the group's start
+  int lim[RT], low[RT], newi[RT];
 
-  typedef uint32_t Frag __attribute__((ext_vector_type(kF32 ? KE : 4)));
   Frag qf[RT][KC];
   floatx4 o[RT][NO];
   float m[RT], l[RT];
   uint32_t seen[RT];
 
-  __device__ __forceinline__ Attn(const AttnPlan& plan, float* shared, int ln, int hd)
-      : p(plan), lds(shared), lane(ln), q(ln & 15), g(ln >> 4), head(hd) {}
+  // the tile
+  KRaw k[NG][KC];
+  VRaw v[VC][VT];
+  uint32_t ks[kCodes ? NG : 1][KW], vs[kCodes ? NG : 1][NB];   // scale bytes of a row; of rows 4 g .. 4 g + 3
+  uint32_t ok;     // bit t: token t has a place
+  bool full;       // every row sees every token
+
+  __device__ __forceinline__ Attn(const AttnPlan& plan, int ln, int hd)
+      : p(plan), lane(ln), q(ln & 15), g(ln >> 4), head(hd) {}
 
   __device__ __forceinline__ const uint8_t* kbase() const {
     return (const uint8_t*)p.c.k + (int64_t)head * p.c.head_stride * ES;
@@ -157,15 +177,26 @@ struct Attn {
   __device__ __forceinline__ void begin(const Item& item) {
     it = item;
     window = -(1 << 30);
+    // (columns past head_dim have offsets past every buffer)
+    const uint32_t step = P16 ? (uint32_t)p.c.place_stride : 0;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) koff[c] = min(c * 4 * KE + g * KE, p.c.d - KE) * ES;
+    for (int c = 0; c < KC; ++c) {
+      const int col = c * 4 * KE + g * KE;
+      koff[c] = col < p.c.d ? (q * step + col) * ES : kNone;
+    }
 #pragma unroll
-    for (int c = 0; c < VC; ++c) voff[c] = min(c * 16 * VE + q * VE, p.c.d - VE) * ES;
+    for (int c = 0; c < VC; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int col = c * 16 * VE + q * VE;
+        voff[c][r] = col < p.c.d ? ((g * 4 + r) * step + col) * ES : kNone;
+      }
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const int r = t * 16 + q;
       const bool in = r < it.nrows;
       const int row = it.row0 + (in ? r : 0), i = row / p.group;
+      newi[t] = i;
       lim[t] = it.len - p.a.n_new + i;
       low[t] = p.a.window ? lim[t] - p.a.window : -1;
       const T* src = (const T*)p.a.q.p + ((int64_t)it.seq * p.a.n_new + i) * p.a.q.ts +
@@ -200,71 +231,147 @@ struct Attn {
       }
     }
   }
-  // Place of token `tok` (within the tile; the lane's own) of a tile at window
-  // position w: element offset, and scale row.
-  __device__ __forceinline__ int64_t place(int w, int u, int r) const {
-    if constexpr (P16) return lane_i64(base, w * NG + u) + r * p.c.place_stride;
-    else return shfl_i64(base, w * TILE + u * 16 + r);
+  // Scale bytes of column blocks: a lane's columns of V in chunk c are of block
+  // vblock(c); K's chunk c of block kblock(c).
+  static constexpr int kblock(int c) { return c * 4 * KE / kCkptBlock; }
+  __device__ __forceinline__ int vblock(int c) const { return (c * 16 * VE + q * VE) / kCkptBlock; }
+  // Where the byte of row r (of four) and block b is among the words of four rows
+  // (b / 4 is the chunk at the largest width).
+  static constexpr int vword(int r, int c) { return NB == 8 ? r * 2 + (kF32 ? c / 2 : c) : r * NB / 4; }
+  static __device__ __forceinline__ int vshift(int r, int b) { return 8 * ((r * NB + b) % 4); }
+  __device__ __forceinline__ uint8_t kscale(int u, int c) const {
+    if constexpr (!kCodes) return 0;
+    return (uint8_t)(ks[u][kblock(c) / 4] >> (8 * (kblock(c) % 4)));
   }
-  __device__ __forceinline__ int64_t scale_row(int w, int u, int r) const {
-    if constexpr (P16) return lane_i64(srow, w * NG + u) + r;
-    else return shfl_i64(srow, w * TILE + u * 16 + r);
+  __device__ __forceinline__ uint8_t vscale(int i, int c) const {
+    if constexpr (!kCodes) return 0;
+    return (uint8_t)(vs[i / 4][vword(i % 4, c)] >> vshift(i % 4, vblock(c)));
   }
 
-  template <bool FULL>
-  __device__ __forceinline__ void load_rows(Tile& x, int tile, int w) {
-    const uint8_t *kb = kbase(), *vb = vbase();
+  // Finds the tile's tokens; at position w of the window.
+  __device__ __forceinline__ int find(int tile) {
+    find_pages(tile);
+    const int w = tile - window, t0 = tile * TILE;
+    if constexpr (P16) {
+      ok = lane_i64(base, w * NG) >= 0 ? 0xFFFFu : 0u;
+      if (NG > 1) ok |= lane_i64(base, w * NG + 1) >= 0 ? 0xFFFF0000u : 0u;
+    } else {
+      ok = (uint32_t)(__ballot(base >= 0) >> (w * TILE)) & (uint32_t)((1ull << TILE) - 1);
+    }
+    full = ok == (uint32_t)((1ull << TILE) - 1) && t0 >= it.lo_all && t0 + TILE <= it.hi_all;
+    return w;
+  }
+  // 0 where token `tok` of the tile is one that some row sees, else kNone (for an
+  // offset past every buffer: such loads give 0).
+  __device__ __forceinline__ uint32_t unseen(int tile, int tok) const {
+    const int t = tile * TILE + tok;
+    return (ok >> tok & 1) && t >= it.lo && t < it.hi ? 0u : kNone;
+  }
+
+  // P16: a buffer starts at the group, and a lane's offsets never change; else a
+  // lane's tokens' places come from the lanes that looked them up.
+  __device__ __forceinline__ void load_k(int tile, int w) {
     const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
-    auto there = [&](int tok) {
-      const int t = tile * TILE + tok;
-      return FULL || ((x.ok >> tok & 1) && t >= it.lo && t < it.hi);
-    };
+    uint32_t no[NG];
+#pragma unroll
+    for (int u = 0; u < NG; ++u) no[u] = 0;
+    if (!full) {
+#pragma unroll
+      for (int u = 0; u < NG; ++u) no[u] = unseen(tile, u * 16 + q);
+    }
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
-      const int64_t at = place(w, u, q) * ES;
-      const int64_t sr = kCodes ? scale_row(w, u, q) : 0;
-      const bool in = there(u * 16 + q);
+      if constexpr (P16) {
+        const Buffer b(kbase() + lane_i64(base, w * NG + u) * ES);
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        x.k[u][c] = {};
-        if (in) x.k[u][c] = *reinterpret_cast<const KRaw*>(kb + at + koff[c]);
+        for (int c = 0; c < KC; ++c) b.load(k[u][c], koff[c] | no[u]);
         if constexpr (kCodes) {
-          x.ks[u][c] = 0;
-          if (in) x.ks[u][c] = p.c.k_scales[sr * nb + koff[c] / kCkptBlock];
+          const Buffer sb(p.c.k_scales + lane_i64(srow, w * NG + u) * nb);
+          if (nb == NB) {
+#pragma unroll
+            for (int i = 0; i < KW; ++i) ks[u][i] = NB == 2 ? sb.load2(q * 2 | no[u]) : sb.load4((q * NB + 4 * i) | no[u]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < KW; ++i) ks[u][i] = 0;
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+              if (i < nb) ks[u][i / 4] |= sb.load1((q * nb + i) | no[u]) << (8 * (i % 4));
+          }
         }
-      }
-    }
+      } else {
+        const uint8_t* kb = kbase() + shfl_i64(base, w * TILE + u * 16 + q) * ES;
 #pragma unroll
-    for (int i = 0; i < VT; ++i) {
-      const int u = i / 4, r = g * 4 + i % 4;
-      const int64_t at = place(w, u, r) * ES;
-      const int64_t sr = kCodes ? scale_row(w, u, r) : 0;
-      const bool in = there(u * 16 + r);
-#pragma unroll
-      for (int c = 0; c < VC; ++c) {
-        x.v[c][i] = {};
-        if (in) x.v[c][i] = *reinterpret_cast<const VRaw*>(vb + at + voff[c]);
+        for (int c = 0; c < KC; ++c) {
+          k[u][c] = {};
+          if (!((koff[c] | no[u]) & kNone)) k[u][c] = *reinterpret_cast<const KRaw*>(kb + koff[c]);
+        }
         if constexpr (kCodes) {
-          x.vs[c][i] = 0;
-          if (in) x.vs[c][i] = p.c.v_scales[sr * nb + voff[c] / kCkptBlock];
+          const uint8_t* sb = p.c.k_scales + shfl_i64(srow, w * TILE + u * 16 + q) * nb;
+#pragma unroll
+          for (int i = 0; i < KW; ++i) ks[u][i] = 0;
+#pragma unroll
+          for (int i = 0; i < NB; ++i)
+            if (i < nb && !no[u]) ks[u][i / 4] |= (uint32_t)sb[i] << (8 * (i % 4));
         }
       }
     }
   }
 
-  __device__ __forceinline__ void load(Tile& x, int tile) {
-    find_pages(tile);
-    const int w = tile - window;
-    if constexpr (P16) {
-      x.ok = lane_i64(base, w * NG) >= 0 ? 0xFFFFu : 0u;
-      if (NG > 1) x.ok |= lane_i64(base, w * NG + 1) >= 0 ? 0xFFFF0000u : 0u;
-    } else {
-      x.ok = (uint32_t)(__ballot(base >= 0) >> (w * TILE)) & (uint32_t)((1ull << TILE) - 1);
+  __device__ __forceinline__ void load_v(int tile, int w) {
+    const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
+    uint32_t no[VT];
+#pragma unroll
+    for (int i = 0; i < VT; ++i) no[i] = 0;
+    if (!full) {
+#pragma unroll
+      for (int i = 0; i < VT; ++i) no[i] = unseen(tile, (i / 4) * 16 + g * 4 + i % 4);
     }
-    const int t0 = tile * TILE;
-    x.full = x.ok == (uint32_t)((1ull << TILE) - 1) && t0 >= it.lo_all && t0 + TILE <= it.hi_all;
-    if (x.full) load_rows<true>(x, tile, w);
-    else load_rows<false>(x, tile, w);
+#pragma unroll
+    for (int u = 0; u < NG; ++u) {
+      if constexpr (P16) {
+        const Buffer b(vbase() + lane_i64(base, w * NG + u) * ES);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int c = 0; c < VC; ++c) b.load(v[c][u * 4 + r], voff[c][r] | no[u * 4 + r]);
+        if constexpr (kCodes) {
+          const Buffer sb(p.c.v_scales + lane_i64(srow, w * NG + u) * nb);
+          if (full && nb == NB) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) vs[u][i] = sb.load4(g * 4 * NB + 4 * i);
+          } else {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) vs[u][i] = 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int c = 0; c < VC; ++c)
+                vs[u][vword(r, c)] |= sb.load1(((g * 4 + r) * nb + vblock(c)) | no[u * 4 + r] | (voff[c][r] & kNone))
+                                      << vshift(r, vblock(c));
+          }
+        }
+      } else {
+        if constexpr (kCodes) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i) vs[u][i] = 0;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = u * 4 + r, from = w * TILE + u * 16 + g * 4 + r;
+          const uint8_t* vb = vbase() + shfl_i64(base, from) * ES;
+          const int64_t sr = kCodes ? shfl_i64(srow, from) : 0;
+#pragma unroll
+          for (int c = 0; c < VC; ++c) {
+            const bool in = !((voff[c][r] | no[i]) & kNone);
+            v[c][i] = {};
+            if (in) v[c][i] = *reinterpret_cast<const VRaw*>(vb + voff[c][r]);
+            if constexpr (kCodes) {
+              if (in) vs[u][vword(r, c)] |= (uint32_t)p.c.v_scales[sr * nb + vblock(c)] << vshift(r, vblock(c));
+            }
+          }
+        }
+      }
+    }
   }
 
   // ---- operands
@@ -277,43 +384,40 @@ struct Attn {
   }
   static __device__ __forceinline__ float scale_of(uint8_t b) { return __uint_as_float((uint32_t)b << 23); }
 
-  __device__ __forceinline__ Frag kfrag(const Tile& x, int u, int c) const {
+  __device__ __forceinline__ Frag kfrag(int u, int c) const {
     Frag f;
     if constexpr (CACHE == CACHE_CODES_BF16) {
-      const float s = scale_of(x.ks[u][c]);
-      f[0] = pair_bf16(x.k[u][c][0], s, false), f[1] = pair_bf16(x.k[u][c][0], s, true);
-      f[2] = pair_bf16(x.k[u][c][1], s, false), f[3] = pair_bf16(x.k[u][c][1], s, true);
+      const float s = scale_of(kscale(u, c));
+      f[0] = pair_bf16(k[u][c][0], s, false), f[1] = pair_bf16(k[u][c][0], s, true);
+      f[2] = pair_bf16(k[u][c][1], s, false), f[3] = pair_bf16(k[u][c][1], s, true);
     } else if constexpr (CACHE == CACHE_CODES_F32) {
-      float v[8];
-      ckpt_values(make_uint2(x.k[u][c][0], 0), x.ks[u][c], v);
+      float v4[8];
+      ckpt_values(make_uint2(k[u][c][0], 0), kscale(u, c), v4);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = __float_as_uint(v[i]);
+      for (int i = 0; i < 4; ++i) f[i] = __float_as_uint(v4[i]);
     } else {
-      f = x.k[u][c];
+      f = k[u][c];
     }
-    // (columns past head_dim were loaded from inside the row; Q is 0 there, but
-    // 0 times an infinity is not)
-    if ((c + 1) * 4 * KE > p.c.d && c * 4 * KE + g * KE >= p.c.d) f = Frag{};
     return f;
   }
   // Columns of token slot i as loaded from memory, in the product's type.
   typedef uint32_t VWords __attribute__((ext_vector_type(kF32 ? 4 : VE / 2)));
-  __device__ __forceinline__ VWords vwords(const VRaw& raw, uint8_t sb) const {
+  __device__ __forceinline__ VWords vwords(int i, int c) const {
     VWords f;
     if constexpr (CACHE == CACHE_CODES_BF16) {
-      const float s = scale_of(sb);
+      const float s = scale_of(vscale(i, c));
 #pragma unroll
       for (int j = 0; j < VE / 4; ++j) {
-        f[2 * j] = pair_bf16(raw[j], s, false);
-        f[2 * j + 1] = pair_bf16(raw[j], s, true);
+        f[2 * j] = pair_bf16(v[c][i][j], s, false);
+        f[2 * j + 1] = pair_bf16(v[c][i][j], s, true);
       }
     } else if constexpr (CACHE == CACHE_CODES_F32) {
-      float v[8];
-      ckpt_values(make_uint2(raw[0], 0), sb, v);
+      float v4[8];
+      ckpt_values(make_uint2(v[c][i][0], 0), vscale(i, c), v4);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = __float_as_uint(v[i]);
+      for (int j = 0; j < 4; ++j) f[j] = __float_as_uint(v4[j]);
     } else {
-      f = raw;
+      f = v[c][i];
     }
     return f;
   }
@@ -322,47 +426,53 @@ struct Attn {
     else return __uint_as_float((j & 1) ? (f[j / 2] & 0xFFFF0000u) : (f[j / 2] << 16));
   }
 
-  // ---- one tile
-  __device__ __forceinline__ void compute(const Tile& x, int tile) {
-    Frag kf[NG][KC];
+  // ---- one tile: scores, then weights, then the sums of values
+  __device__ __forceinline__ void scores(float (&pr)[RT][VT]) const {
 #pragma unroll
-    for (int u = 0; u < NG; ++u)
+    for (int u = 0; u < NG; ++u) {
+      floatx4 s[RT];
 #pragma unroll
-      for (int c = 0; c < KC; ++c) kf[u][c] = kfrag(x, u, c);
-    float pr[RT][VT];
+      for (int t = 0; t < RT; ++t) s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      floatx4 s[NG];
+      for (int c = 0; c < KC; ++c) {
+        const Frag f = kfrag(u, c);
 #pragma unroll
-      for (int u = 0; u < NG; ++u) {
-        s[u] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < KC; ++c) {
+        for (int t = 0; t < RT; ++t) {
           if constexpr (kF32) {
 #pragma unroll
             for (int i = 0; i < KE; ++i)
-              s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[u][c][i]), __uint_as_float(qf[t][c][i]),
-                                                          s[u], 0, 0, 0);
+              s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f[i]), __uint_as_float(qf[t][c][i]), s[t], 0,
+                                                          0, 0);
           } else {
-            s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[u][c]),
-                                                           __builtin_bit_cast(bf16x8, qf[t][c]), s[u], 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f),
+                                                           __builtin_bit_cast(bf16x8, qf[t][c]), s[t], 0, 0, 0);
           }
         }
       }
-      float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < VT; ++i) {
-        float v = s[i / 4][i % 4] * p.scale2;
-        if (!x.full) {
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) pr[t][u * 4 + r] = s[t][r] * p.scale2;
+    }
+  }
+
+  __device__ __forceinline__ void weights(float (&pr)[RT][VT], int tile, uint32_t okay, bool all) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      if (!all) {
+#pragma unroll
+        for (int i = 0; i < VT; ++i) {
           const int tok = (i / 4) * 16 + g * 4 + i % 4, at = tile * TILE + tok;
-          const bool vis = (x.ok >> tok & 1) && at <= lim[t] && at > low[t];
-          v = vis ? v : -INFINITY;
+          const bool vis = (okay >> tok & 1) && at <= lim[t] && at > low[t];
+          pr[t][i] = vis ? pr[t][i] : -INFINITY;
           seen[t] |= (uint32_t)vis;
         }
-        pr[t][i] = v;
-        mx = fmaxf(mx, v);
+      } else {
+        seen[t] = 1;
       }
-      if (x.full) seen[t] = 1;
+      float mx = pr[t][0];
+#pragma unroll
+      for (int i = 1; i < VT; ++i) mx = fmaxf(mx, pr[t][i]);
       mx = fmaxf(m[t], row_max(mx));
       const float mu = mx == -INFINITY ? 0.f : mx;
       if (__any(mx > m[t])) {
@@ -380,8 +490,10 @@ struct Attn {
       }
       l[t] += sum;
     }
+  }
 
-    if (!x.full && p.a.n_new > 1) {
+  __device__ __forceinline__ void add_values(const float (&pr)[RT][VT], int tile, bool all) {
+    if (!all && p.a.n_new > 1) {
       // Rows that see different tokens: a value that is not finite must not
       // reach, as 0 times itself, a row that does not see it.
       uint32_t bad = 0;
@@ -389,28 +501,58 @@ struct Attn {
       for (int c = 0; c < VC; ++c)
 #pragma unroll
         for (int i = 0; i < VT; ++i) {
-          const VWords f = vwords(x.v[c][i], x.vs[c][kCodes ? i : 0]);
+          const VWords f = vwords(i, c);
 #pragma unroll
           for (int j = 0; j < VE; ++j) bad |= (__float_as_uint(velem(f, j)) & 0x7F800000u) == 0x7F800000u;
         }
       if (__any(bad)) {
-        values_one_by_one(x, tile, pr);
+        // One new token's rows at a time, with what they do not see set to 0.
+        for (int i = it.row0 / p.group; i <= (it.row0 + it.nrows - 1) / p.group; ++i) {
+          const int at = it.len - p.a.n_new + i;
+          uint32_t keep = 0;
+#pragma unroll
+          for (int j = 0; j < VT; ++j) {
+            const int tok = tile * TILE + (j / 4) * 16 + g * 4 + j % 4;
+            keep |= (uint32_t)(tok <= at && (!p.a.window || tok > at - p.a.window)) << j;
+          }
+          values<true>(pr, keep, i);
+        }
         return;
       }
     }
+    values<false>(pr, 0, 0);
+  }
 
+  // O += V^T P^T.  ONLY: of the rows of new token `who`, from the tokens `keep`.
+  template <bool ONLY>
+  __device__ __forceinline__ void values(const float (&pr)[RT][VT], uint32_t keep, int who) {
+    auto add = [&](int t, int n, auto product) {
+      if constexpr (ONLY) {
+        const floatx4 v = product(floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[t][n][r] += newi[t] == who ? v[r] : 0.f;
+      } else {
+        o[t][n] = product(o[t][n]);
+      }
+    };
+    auto words = [&](int c, int i) {
+      VWords f = vwords(i, c);
+      if (ONLY && !(keep >> i & 1)) f = VWords{};
+      return f;
+    };
     if constexpr (kF32) {
 #pragma unroll
       for (int i = 0; i < VT; ++i)
 #pragma unroll
         for (int c = 0; c < VC; ++c) {
-          const VWords f = vwords(x.v[c][i], x.vs[c][kCodes ? i : 0]);
+          const VWords f = words(c, i);
 #pragma unroll
           for (int j = 0; j < VE; ++j)
 #pragma unroll
             for (int t = 0; t < RT; ++t)
-              o[t][c * VE + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f[j]), pr[t][i],
-                                                                      o[t][c * VE + j], 0, 0, 0);
+              add(t, c * VE + j, [&](floatx4 acc) {
+                return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f[j]), pr[t][i], acc, 0, 0, 0);
+              });
         }
     } else {
       bf16x8 pf[RT];
@@ -422,7 +564,7 @@ struct Attn {
       for (int c = 0; c < VC; ++c) {
         VWords f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = vwords(x.v[c][i], x.vs[c][kCodes ? i : 0]);
+        for (int i = 0; i < 8; ++i) f[i] = words(c, i);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
           Frag a;
@@ -431,67 +573,31 @@ struct Attn {
             a[i] = __builtin_amdgcn_perm(f[2 * i + 1][j / 2], f[2 * i][j / 2], (j & 1) ? 0x07060302u : 0x05040100u);
 #pragma unroll
           for (int t = 0; t < RT; ++t)
-            o[t][c * VE + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[t],
-                                                                       o[t][c * VE + j], 0, 0, 0);
+            add(t, c * VE + j, [&](floatx4 acc) {
+              return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[t], acc, 0, 0, 0);
+            });
         }
       }
     }
   }
 
-  // The values of a tile token by token, each only for the rows that see it
-  // (rare: some value is not finite).
-  __device__ __forceinline__ void values_one_by_one(const Tile& x, int tile, const float (&pr)[RT][VT]) {
-    const uint8_t* vb = vbase();
-    [[maybe_unused]] const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
-    const int w = tile - window;
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-#pragma unroll
-      for (int i = 0; i < VT; ++i) lds[((i / 4) * 16 + g * 4 + i % 4) * 16 + q] = pr[t][i];
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll 1
-      for (int tok = 0; tok < TILE; ++tok) {
-        const int at = tile * TILE + tok;
-        if (!(x.ok >> tok & 1) || at < it.lo || at >= it.hi) continue;
-        const bool vis = at <= lim[t] && at > low[t];
-        const float pv = lds[tok * 16 + q];
-        const int64_t off = P16 ? lane_i64(base, w * NG + tok / 16) + (tok % 16) * p.c.place_stride
-                                : lane_i64(base, w * TILE + tok);
-#pragma unroll
-        for (int c = 0; c < VC; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int col = min(c * 16 * VE + (4 * g + r) * VE, p.c.d - VE);
-            const VRaw raw = *reinterpret_cast<const VRaw*>(vb + (off + col) * ES);
-            uint8_t sb = 0;
-            if constexpr (kCodes) {
-              const int64_t sr = P16 ? lane_i64(srow, w * NG + tok / 16) + tok % 16 : lane_i64(srow, w * TILE + tok);
-              sb = p.c.v_scales[sr * nb + col / kCkptBlock];
-            }
-            const VWords f = vwords(raw, sb);
-#pragma unroll
-            for (int j = 0; j < VE; ++j) o[t][c * VE + j][r] += vis ? pv * velem(f, j) : 0.f;
-          }
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-  }
-
   __device__ __forceinline__ void tiles(int from, int to) {
-    Tile a, b;
     if (from >= to) return;
-    load(a, from);
-    for (int t = from;; t += 2) {
-      if (t + 1 < to) load(b, t + 1);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(a, t);
-      if (t + 1 >= to) return;
-      if (t + 2 < to) load(a, t + 2);
-      __builtin_amdgcn_sched_barrier(0);
-      compute(b, t + 1);
-      if (t + 2 >= to) return;
+    int w = find(from);
+    load_k(from, w);
+    load_v(from, w);
+    for (int t = from; t < to; ++t) {
+      const uint32_t okay = ok;
+      const bool all = full;
+      float pr[RT][VT];
+      scores(pr);
+      if (t + 1 < to) {
+        w = find(t + 1);
+        load_k(t + 1, w);
+      }
+      weights(pr, t, okay, all);
+      add_values(pr, t, all);
+      if (t + 1 < to) load_v(t + 1, w);
     }
   }
 };
@@ -515,8 +621,14 @@ __device__ __forceinline__ void finish_row(const AttnPlan& p, const Item& it, in
   }
 }
 
+// Waves of a SIMD: two while 256 registers hold a wave.
+template <int D, int RT>
+constexpr int attn_per_simd() {
+  return D * RT <= 128 ? 2 : 1;
+}
+
 template <int CACHE, int D, int RT, bool P16>
-__global__ __launch_bounds__(64 * kAttnWaves) void attention_kernel(AttnPlan p) {
+__global__ __launch_bounds__(64 * kAttnWaves, (attn_per_simd<D, RT>())) void attention_kernel(AttnPlan p) {
   typedef Attn<CACHE, D, RT, P16> A;
   typedef typename A::T T;
   __shared__ __align__(16) float rows[kAttnWaves][16][A::STRIDE];
@@ -571,7 +683,7 @@ __global__ __launch_bounds__(64 * kAttnWaves) void attention_kernel(AttnPlan p) 
     left = 1;   // one item
   }
 
-  A s(p, &rows[wave][0][0], lane, head);
+  A s(p, lane, head);
   while (left > 0) {
     const Item it = item_of<A::TILE, A::R>(p, item);
     const int from = (int)at;

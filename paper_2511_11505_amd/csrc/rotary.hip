@@ -53,19 +53,76 @@ __device__ __forceinline__ void cos_sin(double t, double& c, double& s) {
   s = (quarter & 2) ? -ss : ss;
 }
 
+// The rows of a token in batches of kUnroll * (64 / lanes of a row), of q, then of
+// k, then of v.
+struct Batches {
+  int size, q, kv;   // rows of a batch; batches of q, of each of k and v
+};
+
 // FAST: chunks of 8 columns turn with a whole chunk or within themselves;
 // otherwise columns take their partners one by one.
 template <typename T, bool FAST, bool CACHE>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs g, PagedCache pc, int lanes_log2, int splits,
-                                                     int rows_per_split) {
-  __shared__ float2 table[4][kMaxPairs];
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs g, PagedCache pc, Batches bt, int lanes_log2,
+                                                     int splits, int per_split) {
+  __shared__ __align__(16) float2 table[4][kMaxPairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  const int token = (int)(id / splits), split = (int)(id % splits);
+  const int token = (int)(id / splits);
   if (token >= g.tokens) return;
+  int batch = (int)(id % splits) * per_split;
+  const int last = min(batch + per_split, bt.q + 2 * bt.kv);
+
+  const int pairs = g.rope.rot / 2;
+  const bool halves = g.rope.halves;
+  const int per_wave = 64 >> lanes_log2, row0 = lane >> lanes_log2;
+  const int c0 = (lane & ((1 << lanes_log2) - 1)) * 8, n = min(8, g.d - c0);
+  uint32_t turns = 0, ahead = 0;    // bit i: column c0 + i turns; its partner is ahead
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int at = c0 + i - g.rope.first;
+    turns |= (uint32_t)(i < n && at >= 0 && at < g.rope.rot) << i;
+    ahead |= (uint32_t)(halves ? at < pairs : !(at & 1)) << i;
+  }
+
+  enum { Q, K, V };
+  Raw8<T> own[kUnroll], other[kUnroll];
+  auto fetch = [&](int part, int first, int heads) {
+    const HeadRows& h = part == Q ? g.q : part == K ? g.k : g.v;
+    const T* base = (const T*)h.p + (int64_t)token * h.ts + c0;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int r = first + u * per_wave + row0;
+      own[u] = other[u] = {};
+      if (r >= heads || n <= 0) continue;
+      const T* src = base + r * h.hs;
+      own[u] = load8<T>(src, n);
+      if (turns && part != V) {
+        if constexpr (FAST) {
+          if (halves) other[u] = load8<T>(src + ((ahead & 1) ? pairs : -pairs), 8);
+        } else {
+          const int step = halves ? pairs : 1;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (turns >> i & 1) {
+              const T v = src[i + ((ahead >> i & 1) ? step : -step)];
+              if constexpr (sizeof(T) == 4) other[u].w[i] = __float_as_uint(v);
+              else other[u].w[i >> 1] |= (uint32_t)v << (16 * (i & 1));
+            }
+        }
+      }
+    }
+  };
+  int part, first, heads;
+  auto find = [&](int b) {
+    part = !CACHE || b < bt.q ? Q : b < bt.q + bt.kv ? K : V;
+    first = (part == Q ? b : part == K ? b - bt.q : b - bt.q - bt.kv) * bt.size;
+    heads = part == Q ? g.q_heads : g.kv_heads;
+  };
+  // the first rows are on their way while the angles are made
+  find(batch);
+  fetch(part, first, heads);
 
   const int pos = g.positions[token];
-  const int pairs = g.rope.rot / 2;
   bool live = true;
   int64_t page = -1;
   int place = 0;
@@ -88,95 +145,57 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs g, PagedCache pc
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-
-  // this lane's columns and what they turn with
-  const int lpr = 1 << lanes_log2, per_wave = 64 >> lanes_log2;
-  const int c0 = (lane & (lpr - 1)) * 8, n = min(8, g.d - c0);
-  const bool halves = g.rope.halves;
   float cs[8], sn[8];
-  uint32_t turns = 0, ahead = 0;    // bit i: column c0 + i turns; its partner is ahead
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int at = c0 + i - g.rope.first;
-    const bool t = i < n && at >= 0 && at < g.rope.rot;
-    const bool a = halves ? at < pairs : !(at & 1);     // first of its pair
-    const int p = halves ? (a ? at : at - pairs) : at >> 1;
-    const float2 w = t ? table[wave][p] : make_float2(1.f, 0.f);
+    const bool a = ahead >> i & 1;
+    const float2 w = (turns >> i & 1) ? table[wave][halves ? (a ? at : at - pairs) : at >> 1] : make_float2(1.f, 0.f);
     cs[i] = w.x;
     sn[i] = a ? -w.y : w.y;
-    turns |= (uint32_t)t << i;
-    ahead |= (uint32_t)a << i;
   }
-  const int step = halves ? pairs : 1;
 
-  const int rows = g.q_heads + 2 * g.kv_heads;
-  const int end = min(rows, (split + 1) * rows_per_split);
-  for (int r0 = split * rows_per_split + (lane >> lanes_log2); r0 - (lane >> lanes_log2) < end;
-       r0 += kUnroll * per_wave) {
-    Raw8<T> own[kUnroll], other[kUnroll];
+  for (;;) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int r = r0 + u * per_wave;
-      own[u] = other[u] = {};
-      if (r >= end || n <= 0) continue;
-      const bool isq = !CACHE || r < g.q_heads;
-      const bool isk = CACHE && !isq && r < g.q_heads + g.kv_heads;
-      const HeadRows& h = isq ? g.q : isk ? g.k : g.v;
-      const int head = isq ? r : isk ? r - g.q_heads : r - g.q_heads - g.kv_heads;
-      const T* src = (const T*)h.p + (int64_t)token * h.ts + head * h.hs + c0;
-      own[u] = load8<T>(src, n);
-      if (turns && (isq || isk)) {
-        if constexpr (FAST) {
-          if (halves) other[u] = load8<T>(src + ((ahead & 1) ? pairs : -pairs), 8);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (turns >> i & 1) {
-              const T v = src[i + ((ahead >> i & 1) ? step : -step)];
-              if constexpr (sizeof(T) == 4) other[u].w[i] = __float_as_uint(v);
-              else other[u].w[i >> 1] |= (uint32_t)v << (16 * (i & 1));
-            }
-        }
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int r = r0 + u * per_wave;
-      const bool in = r < end && n > 0;
-      const bool isq = !CACHE || r < g.q_heads;
-      const bool isk = CACHE && !isq && r < g.q_heads + g.kv_heads;
+      const int r = first + u * per_wave + row0;
+      const bool in = r < heads && n > 0;
       float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = own[u].get(i);
-        const float y = FAST && !halves ? own[u].get(i ^ 1) : other[u].get(i);
-        v[i] = (turns >> i & 1) && (isq || isk) ? x * cs[i] + y * sn[i] : x;
+      for (int i = 0; i < 8; ++i) v[i] = own[u].get(i);
+      if (part != V) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float y = FAST && !halves ? own[u].get(i ^ 1) : other[u].get(i);
+          const float t = own[u].get(i) * cs[i] + y * sn[i];
+          v[i] = (turns >> i & 1) ? t : v[i];
+        }
       }
-      if (isq) {
+      if (!CACHE || part == Q) {
         if (CACHE && !live) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = 0.f;
         }
         if (in) store8<T>((T*)g.out.p + (int64_t)token * g.out.ts + r * g.out.hs + c0, v, n);
-      }
-      if constexpr (CACHE) {
-        const int head = isk ? r - g.q_heads : r - g.q_heads - g.kv_heads;
-        const bool put = in && !isq && live && page >= 0;
-        const int64_t at = page * pc.page_stride + head * pc.head_stride + place * pc.place_stride + c0;
+      } else if (live && page >= 0) {
+        uint8_t *base = (uint8_t*)(part == K ? pc.k : pc.v), *scales = part == K ? pc.k_scales : pc.v_scales;
+        const int64_t at = page * pc.page_stride + r * pc.head_stride + place * pc.place_stride + c0;
         if (pc.codes) {
-          const int b = ckpt_byte(block_max<LANES_NEXT>(put ? amax8(v) : 0));
-          if (put) {
-            store_codes((uint8_t*)(isk ? pc.k : pc.v) + at, ckpt_codes(v, b), 8);
+          const int b = ckpt_byte(block_max<LANES_NEXT>(amax8(v)));
+          if (in) {
+            store_codes(base + at, ckpt_codes(v, b), 8);
             if (c0 % kCkptBlock == 0)
-              (isk ? pc.k_scales : pc.v_scales)[((page * pc.kv_heads + head) * pc.page_size + place) *
-                                                    ((g.d + kCkptBlock - 1) / kCkptBlock) +
-                                                c0 / kCkptBlock] = (uint8_t)b;
+              scales[((page * pc.kv_heads + r) * pc.page_size + place) * ((g.d + kCkptBlock - 1) / kCkptBlock) +
+                     c0 / kCkptBlock] = (uint8_t)b;
           }
-        } else if (put) {
-          store8<T>((T*)(isk ? pc.k : pc.v) + at, v, 8);
+        } else if (in) {
+          store8<T>((T*)base + at, v, 8);
         }
       }
     }
+    if (++batch >= last) break;
+    find(batch);
+    fetch(part, first, heads);
   }
 }
 
@@ -184,25 +203,24 @@ template <typename T>
 hipError_t run(const RotaryArgs& g, const PagedCache& pc, hipStream_t s) {
   int lg = 2;
   while ((8 << lg) < g.d) ++lg;
-  const int rows = g.q_heads + 2 * g.kv_heads, per_wave = 64 >> lg;
+  Batches bt;
+  bt.size = (64 >> lg) * kUnroll;
+  bt.q = (g.q_heads + bt.size - 1) / bt.size;
+  bt.kv = (g.kv_heads + bt.size - 1) / bt.size;
   // A wave takes all of a token's rows while the tokens alone make 16 waves a
   // CU (an angle is computed once); fewer tokens are split over more waves,
   // down to one batch of rows in flight each.
-  const int batch = per_wave * kUnroll, most = (rows + batch - 1) / batch;
-  int splits = (int)((4096 + g.tokens - 1) / g.tokens);
-  splits = splits < most ? splits : most;
-  const int rps = (most + splits - 1) / splits * batch;
-  splits = (rows + rps - 1) / rps;
+  const int batches = bt.q + 2 * bt.kv;
+  int splits = (int)((16384 + g.tokens - 1) / g.tokens);
+  splits = splits < batches ? splits : batches;
+  const int per_split = (batches + splits - 1) / splits;
+  splits = (batches + per_split - 1) / per_split;
   const bool halves = g.rope.halves;
   const bool fast = g.d % 8 == 0 && (halves ? g.rope.first % 8 == 0 && g.rope.rot % 16 == 0 : g.rope.first % 2 == 0);
   const dim3 grid((unsigned)cdiv64((int64_t)g.tokens * splits, 4));
-  if (g.kv_heads) {
-    if (fast) launch_k(rotary_kernel<T, true, true>, grid, 256, 0, s, g, pc, lg, splits, rps);
-    else launch_k(rotary_kernel<T, false, true>, grid, 256, 0, s, g, pc, lg, splits, rps);
-  } else {
-    if (fast) launch_k(rotary_kernel<T, true, false>, grid, 256, 0, s, g, pc, lg, splits, rps);
-    else launch_k(rotary_kernel<T, false, false>, grid, 256, 0, s, g, pc, lg, splits, rps);
-  }
+  auto go = [&](auto kernel) { launch_k(kernel, grid, 256, 0, s, g, pc, bt, lg, splits, per_split); };
+  if (g.kv_heads) fast ? go(rotary_kernel<T, true, true>) : go(rotary_kernel<T, false, true>);
+  else fast ? go(rotary_kernel<T, true, false>) : go(rotary_kernel<T, false, false>);
   return hipGetLastError();
 }
 
