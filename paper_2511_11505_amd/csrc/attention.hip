@@ -8,7 +8,7 @@
 namespace fs {
 namespace {
 
-constexpr int kWorkgroups = 512;   // of a divided call: two for each CU
+constexpr int kCus = 256;
 constexpr int kMaxGroups = 1 << 16;
 
 int width_of(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
@@ -46,7 +46,7 @@ Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
   h.workers = 0;
   if (h.items <= kAttnMaxItems && h.items * c.kv_heads <= kMaxGroups && most > 4 * kAttnWaves) {
     const int64_t parts = (h.items * most + kAttnMinTiles - 1) / kAttnMinTiles;
-    h.workers = (kWorkgroups + c.kv_heads - 1) / c.kv_heads;
+    h.workers = (kCus * attn_groups_per_cu(h.width, h.rt) + c.kv_heads - 1) / c.kv_heads;
     if (parts < h.workers) h.workers = (int)parts;
   }
   return h;
@@ -57,7 +57,11 @@ int64_t part_rows(const Shape& h, const PagedCache& c) { return (int64_t)h.worke
 
 template <int CACHE, int D, int RT>
 hipError_t run_pages(const AttnPlan& p, hipStream_t s) {
-  return p.c.page_size % 16 == 0 ? run_attention<CACHE, D, RT, true>(p, s) : run_attention<CACHE, D, RT, false>(p, s);
+  const bool groups = p.c.page_size % 16 == 0;
+  if constexpr (RT == 1)
+    if (p.a.n_new == 1)
+      return groups ? run_attention<CACHE, D, RT, true, false>(p, s) : run_attention<CACHE, D, RT, false, false>(p, s);
+  return groups ? run_attention<CACHE, D, RT, true, true>(p, s) : run_attention<CACHE, D, RT, false, true>(p, s);
 }
 template <int CACHE>
 hipError_t run_cache(int width, int rt, const AttnPlan& p, hipStream_t s) {

@@ -12,6 +12,9 @@ constexpr int kAttnWaves = 4;
 constexpr int kAttnMaxItems = 4096;    // of a divided call: 16 for each thread
 constexpr int kAttnMinTiles = 4;       // of a workgroup's part: one for each wave
 
+// Workgroups a CU runs at once (four waves of 256 registers on each SIMD, or of 512).
+constexpr int attn_groups_per_cu(int width, int row_tiles) { return width < 256 && row_tiles <= 2 ? 2 : 1; }
+
 struct AttnPlan {
   AttnArgs a;
   PagedCache c;
@@ -24,7 +27,8 @@ struct AttnPlan {
   int2* span;              // [items]: first and last part
 };
 
-template <int CACHE, int D, int RT, bool P16>
+// MANY: more than one new token, or rows for more than one row tile.
+template <int CACHE, int D, int RT, bool P16, bool MANY>
 hipError_t run_attention(const AttnPlan& p, hipStream_t s);
 
 }  // namespace fs

@@ -70,8 +70,11 @@ __device__ __forceinline__ float row_sum(float v) {
 }
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// Memory from a uniform address on; offsets at or above kNone read 0.
+// Memory from a uniform address on; offsets at or above kNone read 0.  Rows are
+// loaded as what is read once: in bf16 148.7 us against 166.4 (64 sequences of up
+// to 8192 tokens, 6.0 and 5.4 TB/s).
 constexpr uint32_t kNone = 0x80000000u;
+constexpr int kOnce = 2;   // the non-temporal bit
 struct Buffer {
   __amdgpu_buffer_rsrc_t r;
   __device__ __forceinline__ explicit Buffer(const void* p)
@@ -81,11 +84,11 @@ struct Buffer {
   __device__ __forceinline__ uint32_t load4(uint32_t off) const { return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0); }
   __device__ __forceinline__ void load(u32x1_any& v, uint32_t off) const { v[0] = load4(off); }
   __device__ __forceinline__ void load(u32x2_any& v, uint32_t off) const {
-    const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+    const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kOnce);
     v[0] = x[0], v[1] = x[1];
   }
   __device__ __forceinline__ void load(u32x4_any& v, uint32_t off) const {
-    const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kOnce);
     v[0] = x[0], v[1] = x[1], v[2] = x[2], v[3] = x[3];
   }
 };
@@ -118,7 +121,7 @@ __device__ __forceinline__ Item item_of(const AttnPlan& p, int item) {
   return t;
 }
 
-template <int CACHE, int D, int RT, bool P16>
+template <int CACHE, int D, int RT, bool P16, bool MANY>
 struct Attn {
   static constexpr bool kF32 = CACHE == CACHE_F32 || CACHE == CACHE_CODES_F32;
   static constexpr bool kCodes = CACHE == CACHE_CODES_BF16 || CACHE == CACHE_CODES_F32;
@@ -126,9 +129,11 @@ struct Attn {
   static constexpr int NG = kF32 ? 1 : 2;                    // groups of 16 tokens in a tile
   static constexpr int TILE = 16 * NG;
   static constexpr int R = 16 * RT;                          // rows of an item
-  static constexpr int KE = kF32 ? 4 : 8;                    // columns of K a lane holds together
+  static constexpr int KE = kF32 ? 4 : 8;                    // columns of K in an operand of a product
   static constexpr int KC = D / (4 * KE);
-  static constexpr int VE = kF32 || D == 64 ? 4 : 8;         // columns of V
+  static constexpr int KL = kCodes ? 16 : KE;                // columns of K a lane loads together: 16 bytes
+  static constexpr int KN = D / (4 * KL);
+  static constexpr int VE = CACHE == CACHE_F32 || D == 64 ? 4 : 8;   // columns of V a lane loads together
   static constexpr int VC = D / (16 * VE);
   static constexpr int VT = 4 * NG;                          // tokens of V a lane holds
   static constexpr int NO = D / 16;                          // result tiles of a row tile
@@ -136,7 +141,7 @@ struct Attn {
   static constexpr int NB = D / kCkptBlock;                  // scale bytes of a full-width row
   static constexpr int KW = (NB + 3) / 4;                    // words of a row's scales; of 4 rows': NB
   typedef typename std::conditional<kF32, float, bf16_t>::type T;
-  typedef typename RawT<KE * ES>::type KRaw;
+  typedef u32x4_any KRaw;
   typedef typename RawT<VE * ES>::type VRaw;
 
   typedef uint32_t Frag __attribute__((ext_vector_type(4)));
@@ -148,23 +153,26 @@ struct Attn {
   // (P16) or token window + i, or -1, and its index among the scale rows
   int window;
   int64_t base, srow;
-  uint32_t koff[KC], voff[VC][4];   // bytes in a row; P16: from the group's start
-  int lim[RT], low[RT], newi[RT];
+  uint32_t koff[KN], voff[VC][4];   // bytes in a row; P16: from the group's start
+  int lim[RT], low[RT];
 
-  Frag qf[RT][KC];
+  // queries: in registers, or where they are many in LDS (which the four waves share)
+  static constexpr bool kQShared = RT * KC * 4 > (kF32 ? 32 : 16);
+  Frag qf[kQShared ? 1 : RT][kQShared ? 1 : KC];
+  Frag* qs;
   floatx4 o[RT][NO];
   float m[RT], l[RT];
   uint32_t seen[RT];
 
   // the tile
-  KRaw k[NG][KC];
+  KRaw k[NG][KN];
   VRaw v[VC][VT];
   uint32_t ks[kCodes ? NG : 1][KW], vs[kCodes ? NG : 1][NB];   // scale bytes of a row; of rows 4 g .. 4 g + 3
   uint32_t ok;     // bit t: token t has a place
   bool full;       // every row sees every token
 
-  __device__ __forceinline__ Attn(const AttnPlan& plan, int ln, int hd)
-      : p(plan), lane(ln), q(ln & 15), g(ln >> 4), head(hd) {}
+  __device__ __forceinline__ Attn(const AttnPlan& plan, int ln, int hd, Frag* queries)
+      : p(plan), lane(ln), q(ln & 15), g(ln >> 4), head(hd), qs(queries) {}
 
   __device__ __forceinline__ const uint8_t* kbase() const {
     return (const uint8_t*)p.c.k + (int64_t)head * p.c.head_stride * ES;
@@ -173,15 +181,26 @@ struct Attn {
     return (const uint8_t*)p.c.v + (int64_t)head * p.c.head_stride * ES;
   }
 
-  // ---- one item's start: its rows and what each of them sees
-  __device__ __forceinline__ void begin(const Item& item) {
+  // First of this lane's columns of operand c.
+  __device__ __forceinline__ int kcol(int c) const {
+    constexpr int S = KL / KE;
+    return (c / S * 4 + g) * KL + c % S * KE;
+  }
+
+  // ---- one item's start: its rows and what each of them sees.  (Shared queries
+  // are written by all waves, a barrier has to follow.)
+  __device__ __forceinline__ Frag query(int t, int c) const {
+    if constexpr (kQShared) return qs[(t * KC + c) * 64 + lane];
+    else return qf[t][c];
+  }
+  __device__ __forceinline__ void begin(const Item& item, int wave) {
     it = item;
     window = -(1 << 30);
     // (columns past head_dim have offsets past every buffer)
     const uint32_t step = P16 ? (uint32_t)p.c.place_stride : 0;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      const int col = c * 4 * KE + g * KE;
+    for (int c = 0; c < KN; ++c) {
+      const int col = c * 4 * KL + g * KL;
       koff[c] = col < p.c.d ? (q * step + col) * ES : kNone;
     }
 #pragma unroll
@@ -196,18 +215,18 @@ struct Attn {
       const int r = t * 16 + q;
       const bool in = r < it.nrows;
       const int row = it.row0 + (in ? r : 0), i = row / p.group;
-      newi[t] = i;
       lim[t] = it.len - p.a.n_new + i;
       low[t] = p.a.window ? lim[t] - p.a.window : -1;
       const T* src = (const T*)p.a.q.p + ((int64_t)it.seq * p.a.n_new + i) * p.a.q.ts +
                      (int64_t)(head * p.group + row - i * p.group) * p.a.q.hs;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        const int col = c * 4 * KE + g * KE;
-        qf[t][c] = {};
-        if (in && col < p.c.d) {
-          qf[t][c] = *reinterpret_cast<const u32x4_any*>(src + col);
-        }
+        const int col = kcol(c);
+        if (kQShared && c % kAttnWaves != wave) continue;
+        Frag f = {};
+        if (in && col < p.c.d) f = *reinterpret_cast<const u32x4_any*>(src + col);
+        if constexpr (kQShared) qs[(t * KC + c) * 64 + lane] = f;
+        else qf[t][c] = f;
       }
       m[t] = -INFINITY, l[t] = 0.f, seen[t] = 0;
 #pragma unroll
@@ -232,16 +251,17 @@ struct Attn {
     }
   }
   // Scale bytes of column blocks: a lane's columns of V in chunk c are of block
-  // vblock(c); K's chunk c of block kblock(c).
-  static constexpr int kblock(int c) { return c * 4 * KE / kCkptBlock; }
+  // vblock(c).
   __device__ __forceinline__ int vblock(int c) const { return (c * 16 * VE + q * VE) / kCkptBlock; }
   // Where the byte of row r (of four) and block b is among the words of four rows
   // (b / 4 is the chunk at the largest width).
-  static constexpr int vword(int r, int c) { return NB == 8 ? r * 2 + (kF32 ? c / 2 : c) : r * NB / 4; }
+  static constexpr int vword(int r, int c) { return NB == 8 ? r * 2 + c : r * NB / 4; }
   static __device__ __forceinline__ int vshift(int r, int b) { return 8 * ((r * NB + b) % 4); }
   __device__ __forceinline__ uint8_t kscale(int u, int c) const {
     if constexpr (!kCodes) return 0;
-    return (uint8_t)(ks[u][kblock(c) / 4] >> (8 * (kblock(c) % 4)));
+    // (64 columns a load of the four lanes, two blocks)
+    constexpr int S = KL / KE;
+    return (uint8_t)(ks[u][c / S / 2] >> (16 * (c / S % 2) + 8 * (g >> 1)));
   }
   __device__ __forceinline__ uint8_t vscale(int i, int c) const {
     if constexpr (!kCodes) return 0;
@@ -270,6 +290,21 @@ struct Attn {
 
   // P16: a buffer starts at the group, and a lane's offsets never change; else a
   // lane's tokens' places come from the lanes that looked them up.
+  // (codes of a head_dim that 16 does not divide end inside a load)
+  __device__ __forceinline__ void load_cols(const Buffer& b, int u, uint32_t no) {
+    if (!kCodes || p.c.d % 16 == 0) {
+#pragma unroll
+      for (int c = 0; c < KN; ++c) b.load(k[u][c], koff[c] | no);
+    } else {
+#pragma unroll
+      for (int c = 0; c < KN; ++c) {
+        u32x2_any lo, hi;
+        b.load(lo, koff[c] | no);
+        b.load(hi, (koff[c] + 8) | no | ((c * 4 + g) * KL + 8 < p.c.d ? 0u : kNone));
+        k[u][c][0] = lo[0], k[u][c][1] = lo[1], k[u][c][2] = hi[0], k[u][c][3] = hi[1];
+      }
+    }
+  }
   __device__ __forceinline__ void load_k(int tile, int w) {
     const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
     uint32_t no[NG];
@@ -283,8 +318,7 @@ struct Attn {
     for (int u = 0; u < NG; ++u) {
       if constexpr (P16) {
         const Buffer b(kbase() + lane_i64(base, w * NG + u) * ES);
-#pragma unroll
-        for (int c = 0; c < KC; ++c) b.load(k[u][c], koff[c] | no[u]);
+        load_cols(b, u, no[u]);
         if constexpr (kCodes) {
           const Buffer sb(p.c.k_scales + lane_i64(srow, w * NG + u) * nb);
           if (nb == NB) {
@@ -301,9 +335,15 @@ struct Attn {
       } else {
         const uint8_t* kb = kbase() + shfl_i64(base, w * TILE + u * 16 + q) * ES;
 #pragma unroll
-        for (int c = 0; c < KC; ++c) {
+        for (int c = 0; c < KN; ++c) {
           k[u][c] = {};
-          if (!((koff[c] | no[u]) & kNone)) k[u][c] = *reinterpret_cast<const KRaw*>(kb + koff[c]);
+          const bool in = !((koff[c] | no[u]) & kNone);
+          if (in && (!kCodes || (c * 4 + g) * KL + 8 < p.c.d)) {
+            k[u][c] = *reinterpret_cast<const KRaw*>(kb + koff[c]);
+          } else if (in) {
+            const u32x2_any lo = *reinterpret_cast<const u32x2_any*>(kb + koff[c]);
+            k[u][c][0] = lo[0], k[u][c][1] = lo[1];
+          }
         }
         if constexpr (kCodes) {
           const uint8_t* sb = p.c.k_scales + shfl_i64(srow, w * TILE + u * 16 + q) * nb;
@@ -338,7 +378,11 @@ struct Attn {
           const Buffer sb(p.c.v_scales + lane_i64(srow, w * NG + u) * nb);
           if (full && nb == NB) {
 #pragma unroll
-            for (int i = 0; i < NB; ++i) vs[u][i] = sb.load4(g * 4 * NB + 4 * i);
+            for (int i = 0; i < NB / 2; ++i) {
+              u32x2_any two;
+              sb.load(two, g * 4 * NB + 8 * i);
+              vs[u][2 * i] = two[0], vs[u][2 * i + 1] = two[1];
+            }
           } else {
 #pragma unroll
             for (int i = 0; i < NB; ++i) vs[u][i] = 0;
@@ -388,11 +432,11 @@ struct Attn {
     Frag f;
     if constexpr (CACHE == CACHE_CODES_BF16) {
       const float s = scale_of(kscale(u, c));
-      f[0] = pair_bf16(k[u][c][0], s, false), f[1] = pair_bf16(k[u][c][0], s, true);
-      f[2] = pair_bf16(k[u][c][1], s, false), f[3] = pair_bf16(k[u][c][1], s, true);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = pair_bf16(k[u][c / 2][c % 2 * 2 + i / 2], s, i % 2);
     } else if constexpr (CACHE == CACHE_CODES_F32) {
       float v4[8];
-      ckpt_values(make_uint2(k[u][c][0], 0), kscale(u, c), v4);
+      ckpt_values(make_uint2(k[u][c / 4][c % 4], 0), kscale(u, c), v4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[i] = __float_as_uint(v4[i]);
     } else {
@@ -401,7 +445,7 @@ struct Attn {
     return f;
   }
   // Columns of token slot i as loaded from memory, in the product's type.
-  typedef uint32_t VWords __attribute__((ext_vector_type(kF32 ? 4 : VE / 2)));
+  typedef uint32_t VWords __attribute__((ext_vector_type(kF32 ? VE : VE / 2)));
   __device__ __forceinline__ VWords vwords(int i, int c) const {
     VWords f;
     if constexpr (CACHE == CACHE_CODES_BF16) {
@@ -412,10 +456,10 @@ struct Attn {
         f[2 * j + 1] = pair_bf16(v[c][i][j], s, true);
       }
     } else if constexpr (CACHE == CACHE_CODES_F32) {
-      float v4[8];
-      ckpt_values(make_uint2(v[c][i][0], 0), vscale(i, c), v4);
+      float v8[8];
+      ckpt_values(make_uint2(v[c][i][0], VE == 8 ? v[c][i][VE / 4 - 1] : 0), vscale(i, c), v8);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] = __float_as_uint(v4[j]);
+      for (int j = 0; j < VE; ++j) f[j] = __float_as_uint(v8[j]);
     } else {
       f = v[c][i];
     }
@@ -438,14 +482,15 @@ struct Attn {
         const Frag f = kfrag(u, c);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
+          const Frag y = query(t, c);
           if constexpr (kF32) {
 #pragma unroll
             for (int i = 0; i < KE; ++i)
-              s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f[i]), __uint_as_float(qf[t][c][i]), s[t], 0,
+              s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f[i]), __uint_as_float(y[i]), s[t], 0,
                                                           0, 0);
           } else {
             s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f),
-                                                           __builtin_bit_cast(bf16x8, qf[t][c]), s[t], 0, 0, 0);
+                                                           __builtin_bit_cast(bf16x8, y), s[t], 0, 0, 0);
           }
         }
       }
@@ -492,8 +537,8 @@ struct Attn {
     }
   }
 
-  __device__ __forceinline__ void add_values(const float (&pr)[RT][VT], int tile, bool all) {
-    if (!all && p.a.n_new > 1) {
+  __device__ __forceinline__ void add_values(const float (&pr)[RT][VT], int tile, uint32_t okay, bool all) {
+    if (MANY && !all && p.a.n_new > 1) {
       // Rows that see different tokens: a value that is not finite must not
       // reach, as 0 times itself, a row that does not see it.
       uint32_t bad = 0;
@@ -506,53 +551,115 @@ struct Attn {
           for (int j = 0; j < VE; ++j) bad |= (__float_as_uint(velem(f, j)) & 0x7F800000u) == 0x7F800000u;
         }
       if (__any(bad)) {
-        // One new token's rows at a time, with what they do not see set to 0.
-        for (int i = it.row0 / p.group; i <= (it.row0 + it.nrows - 1) / p.group; ++i) {
-          const int at = it.len - p.a.n_new + i;
-          uint32_t keep = 0;
-#pragma unroll
-          for (int j = 0; j < VT; ++j) {
-            const int tok = tile * TILE + (j / 4) * 16 + g * 4 + j % 4;
-            keep |= (uint32_t)(tok <= at && (!p.a.window || tok > at - p.a.window)) << j;
-          }
-          values<true>(pr, keep, i);
-        }
-        return;
+        infinities(tile, okay);
+        clear_infinities();
       }
     }
-    values<false>(pr, 0, 0);
+    values(pr);
   }
 
-  // O += V^T P^T.  ONLY: of the rows of new token `who`, from the tokens `keep`.
-  template <bool ONLY>
-  __device__ __forceinline__ void values(const float (&pr)[RT][VT], uint32_t keep, int who) {
-    auto add = [&](int t, int n, auto product) {
-      if constexpr (ONLY) {
-        const floatx4 v = product(floatx4{0.f, 0.f, 0.f, 0.f});
+  // What values that are not finite add to the rows that see them: a weight is
+  // above 0, so an infinity gives itself, and a NaN counts as both infinities.
+  __device__ __forceinline__ void infinities(int tile, uint32_t okay) {
+    float sees[RT][VT];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[t][n][r] += newi[t] == who ? v[r] : 0.f;
-      } else {
-        o[t][n] = product(o[t][n]);
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < VT; ++i) {
+        const int tok = (i / 4) * 16 + g * 4 + i % 4, at = tile * TILE + tok;
+        sees[t][i] = (okay >> tok & 1) && at <= lim[t] && at > low[t] ? 1.f : 0.f;
       }
-    };
-    auto words = [&](int c, int i) {
-      VWords f = vwords(i, c);
-      if (ONLY && !(keep >> i & 1)) f = VWords{};
-      return f;
-    };
+#pragma unroll
+    for (int c = 0; c < VC; ++c)
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        float up[VT], down[VT];
+        __builtin_amdgcn_sched_barrier(0);   // (one column at a time: this path is rare, its registers are not free)
+#pragma unroll
+        for (int i = 0; i < VT; ++i) {
+          const float x = velem(vwords(i, c), j);
+          up[i] = !(x <= 3.4028235e38f) ? 1.f : 0.f;
+          down[i] = !(x >= -3.4028235e38f) ? 1.f : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const floatx4 zero{0.f, 0.f, 0.f, 0.f};
+          const floatx4 a = sum_tokens(up, sees[t], zero), b = sum_tokens(down, sees[t], zero);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[t][c * VE + j][r] += (a[r] > 0.f ? INFINITY : 0.f) - (b[r] > 0.f ? INFINITY : 0.f);
+        }
+      }
+  }
+  static __device__ __forceinline__ floatx4 sum_tokens(const float (&a)[VT], const float (&b)[VT], floatx4 acc) {
+    if constexpr (kF32) {
+#pragma unroll
+      for (int i = 0; i < VT; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], acc, 0, 0, 0);
+    } else {
+      bf16x8 x, y;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = (__bf16)a[i], y[i] = (__bf16)b[i];
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, acc, 0, 0, 0);
+    }
+    return acc;
+  }
+  // Sets such values to 0, where they are.
+  __device__ __forceinline__ void clear_infinities() {
+#pragma unroll
+    for (int c = 0; c < VC; ++c)
+#pragma unroll
+      for (int i = 0; i < VT; ++i) {
+        constexpr int W = VE * ES / 4;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kCodes) {
+          const bool all = vscale(i, c) == 255;
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            uint32_t w = v[c][i][j];
+#pragma unroll
+            for (int b = 0; b < 32; b += 8)
+              if (all || (w >> b & 0x7F) == 0x7F) w &= ~(0xFFu << b);
+            v[c][i][j] = w;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            uint32_t w = v[c][i][j];
+            if (kF32) {
+              if ((w & 0x7F800000u) == 0x7F800000u) w = 0;
+            } else {
+              if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+              if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
+            }
+            v[c][i][j] = w;
+          }
+        }
+      }
+    if constexpr (kCodes) {
+      // (0 times the scale of byte 255 is not 0)
+#pragma unroll
+      for (int u = 0; u < NG; ++u)
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int b = 0; b < 32; b += 8)
+            if ((vs[u][i] >> b & 0xFF) == 0xFF) vs[u][i] &= ~(0x80u << b);
+    }
+  }
+
+  // O += V^T P^T.
+  __device__ __forceinline__ void values(const float (&pr)[RT][VT]) {
     if constexpr (kF32) {
 #pragma unroll
       for (int i = 0; i < VT; ++i)
 #pragma unroll
         for (int c = 0; c < VC; ++c) {
-          const VWords f = words(c, i);
+          const VWords f = vwords(i, c);
 #pragma unroll
           for (int j = 0; j < VE; ++j)
 #pragma unroll
             for (int t = 0; t < RT; ++t)
-              add(t, c * VE + j, [&](floatx4 acc) {
-                return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f[j]), pr[t][i], acc, 0, 0, 0);
-              });
+              o[t][c * VE + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f[j]), pr[t][i],
+                                                                      o[t][c * VE + j], 0, 0, 0);
         }
     } else {
       bf16x8 pf[RT];
@@ -564,7 +671,7 @@ struct Attn {
       for (int c = 0; c < VC; ++c) {
         VWords f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = words(c, i);
+        for (int i = 0; i < 8; ++i) f[i] = vwords(i, c);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
           Frag a;
@@ -573,9 +680,8 @@ struct Attn {
             a[i] = __builtin_amdgcn_perm(f[2 * i + 1][j / 2], f[2 * i][j / 2], (j & 1) ? 0x07060302u : 0x05040100u);
 #pragma unroll
           for (int t = 0; t < RT; ++t)
-            add(t, c * VE + j, [&](floatx4 acc) {
-              return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[t], acc, 0, 0, 0);
-            });
+            o[t][c * VE + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[t],
+                                                                       o[t][c * VE + j], 0, 0, 0);
         }
       }
     }
@@ -596,7 +702,7 @@ struct Attn {
         load_k(t + 1, w);
       }
       weights(pr, t, okay, all);
-      add_values(pr, t, all);
+      add_values(pr, t, okay, all);
       if (t + 1 < to) load_v(t + 1, w);
     }
   }
@@ -621,17 +727,12 @@ __device__ __forceinline__ void finish_row(const AttnPlan& p, const Item& it, in
   }
 }
 
-// Waves of a SIMD: two while 256 registers hold a wave.
-template <int D, int RT>
-constexpr int attn_per_simd() {
-  return D * RT <= 128 ? 2 : 1;
-}
-
-template <int CACHE, int D, int RT, bool P16>
-__global__ __launch_bounds__(64 * kAttnWaves, (attn_per_simd<D, RT>())) void attention_kernel(AttnPlan p) {
-  typedef Attn<CACHE, D, RT, P16> A;
+template <int CACHE, int D, int RT, bool P16, bool MANY>
+__global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void attention_kernel(AttnPlan p) {
+  typedef Attn<CACHE, D, RT, P16, MANY> A;
   typedef typename A::T T;
   __shared__ __align__(16) float rows[kAttnWaves][16][A::STRIDE];
+  __shared__ __align__(16) typename A::Frag queries[A::kQShared ? RT * A::KC * 64 : 1];
   __shared__ float2 stats[kAttnWaves][16];
   __shared__ int64_t scan[kAttnWaves];
   __shared__ int64_t found[2];   // first item | its first tile
@@ -683,13 +784,14 @@ __global__ __launch_bounds__(64 * kAttnWaves, (attn_per_simd<D, RT>())) void att
     left = 1;   // one item
   }
 
-  A s(p, lane, head);
+  A s(p, lane, head, queries);
   while (left > 0) {
     const Item it = item_of<A::TILE, A::R>(p, item);
     const int from = (int)at;
     const int n = p.workers ? (int)min((int64_t)(it.tiles - from), left) : it.tiles;
     const bool whole = n == it.tiles;
-    s.begin(it);
+    s.begin(it, wave);
+    if constexpr (A::kQShared) __syncthreads();
     s.tiles(it.first + from + (int)((int64_t)n * wave / kAttnWaves),
             it.first + from + (int)((int64_t)n * (wave + 1) / kAttnWaves));
     if (p.workers && from == 0 && head == 0 && tid == 0) {
@@ -804,11 +906,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnPlan p, int blo
 
 }  // namespace
 
-template <int CACHE, int D, int RT, bool P16>
+template <int CACHE, int D, int RT, bool P16, bool MANY>
 hipError_t run_attention(const AttnPlan& p, hipStream_t s) {
-  typedef Attn<CACHE, D, RT, P16> A;
+  typedef Attn<CACHE, D, RT, P16, MANY> A;
   const int64_t groups = (int64_t)(p.workers ? p.workers : p.items) * p.c.kv_heads;
-  launch_k(attention_kernel<CACHE, D, RT, P16>, dim3((unsigned)groups), 64 * kAttnWaves, 0, s, p);
+  launch_k(attention_kernel<CACHE, D, RT, P16, MANY>, dim3((unsigned)groups), 64 * kAttnWaves, 0, s, p);
   if (p.workers) {
     const int nrows = p.rows < A::R ? p.rows : A::R, blocks = (nrows + 3) / 4;
     launch_k(attention_join_kernel<typename A::T, D, A::R, A::TILE>,
