@@ -164,12 +164,14 @@ struct Attn {
   float m[RT], l[RT];
   uint32_t seen[RT];
 
-  // the tile
-  KRaw k[NG][KN];
-  VRaw v[VC][VT];
-  uint32_t ks[kCodes ? NG : 1][KW], vs[kCodes ? NG : 1][NB];   // scale bytes of a row; of rows 4 g .. 4 g + 3
-  uint32_t ok;     // bit t: token t has a place
-  bool full;       // every row sees every token
+  struct Tile {
+    KRaw k[NG][KN];
+    VRaw v[VC][VT];
+    uint32_t ks[kCodes ? NG : 1][KW], vs[kCodes ? NG : 1][NB];   // scale bytes of a row; of rows 4 g .. 4 g + 3
+    int at, w;       // which tile, at which position of the window
+    uint32_t ok;     // bit t: token t has a place
+    bool full;       // every row sees every token
+  };
 
   __device__ __forceinline__ Attn(const AttnPlan& plan, int ln, int hd, Frag* queries)
       : p(plan), lane(ln), q(ln & 15), g(ln >> 4), head(hd), qs(queries) {}
@@ -257,114 +259,116 @@ struct Attn {
   // (b / 4 is the chunk at the largest width).
   static constexpr int vword(int r, int c) { return NB == 8 ? r * 2 + c : r * NB / 4; }
   static __device__ __forceinline__ int vshift(int r, int b) { return 8 * ((r * NB + b) % 4); }
-  __device__ __forceinline__ uint8_t kscale(int u, int c) const {
+  __device__ __forceinline__ uint8_t kscale(const Tile& x, int u, int c) const {
     if constexpr (!kCodes) return 0;
     // (64 columns a load of the four lanes, two blocks)
     constexpr int S = KL / KE;
-    return (uint8_t)(ks[u][c / S / 2] >> (16 * (c / S % 2) + 8 * (g >> 1)));
+    return (uint8_t)(x.ks[u][c / S / 2] >> (16 * (c / S % 2) + 8 * (g >> 1)));
   }
-  __device__ __forceinline__ uint8_t vscale(int i, int c) const {
+  __device__ __forceinline__ uint8_t vscale(const Tile& x, int i, int c) const {
     if constexpr (!kCodes) return 0;
-    return (uint8_t)(vs[i / 4][vword(i % 4, c)] >> vshift(i % 4, vblock(c)));
+    return (uint8_t)(x.vs[i / 4][vword(i % 4, c)] >> vshift(i % 4, vblock(c)));
   }
 
   // Finds the tile's tokens; at position w of the window.
-  __device__ __forceinline__ int find(int tile) {
+  __device__ __forceinline__ void find(Tile& x, int tile) {
     find_pages(tile);
     const int w = tile - window, t0 = tile * TILE;
+    x.at = tile, x.w = w;
     if constexpr (P16) {
-      ok = lane_i64(base, w * NG) >= 0 ? 0xFFFFu : 0u;
-      if (NG > 1) ok |= lane_i64(base, w * NG + 1) >= 0 ? 0xFFFF0000u : 0u;
+      x.ok = lane_i64(base, w * NG) >= 0 ? 0xFFFFu : 0u;
+      if (NG > 1) x.ok |= lane_i64(base, w * NG + 1) >= 0 ? 0xFFFF0000u : 0u;
     } else {
-      ok = (uint32_t)(__ballot(base >= 0) >> (w * TILE)) & (uint32_t)((1ull << TILE) - 1);
+      x.ok = (uint32_t)(__ballot(base >= 0) >> (w * TILE)) & (uint32_t)((1ull << TILE) - 1);
     }
-    full = ok == (uint32_t)((1ull << TILE) - 1) && t0 >= it.lo_all && t0 + TILE <= it.hi_all;
-    return w;
+    x.full = x.ok == (uint32_t)((1ull << TILE) - 1) && t0 >= it.lo_all && t0 + TILE <= it.hi_all;
   }
   // 0 where token `tok` of the tile is one that some row sees, else kNone (for an
   // offset past every buffer: such loads give 0).
-  __device__ __forceinline__ uint32_t unseen(int tile, int tok) const {
-    const int t = tile * TILE + tok;
-    return (ok >> tok & 1) && t >= it.lo && t < it.hi ? 0u : kNone;
+  __device__ __forceinline__ uint32_t unseen(const Tile& x, int tok) const {
+    const int t = x.at * TILE + tok;
+    return (x.ok >> tok & 1) && t >= it.lo && t < it.hi ? 0u : kNone;
   }
 
   // P16: a buffer starts at the group, and a lane's offsets never change; else a
   // lane's tokens' places come from the lanes that looked them up.
   // (codes of a head_dim that 16 does not divide end inside a load)
-  __device__ __forceinline__ void load_cols(const Buffer& b, int u, uint32_t no) {
+  __device__ __forceinline__ void load_cols(Tile& x, const Buffer& b, int u, uint32_t no) const {
     if (!kCodes || p.c.d % 16 == 0) {
 #pragma unroll
-      for (int c = 0; c < KN; ++c) b.load(k[u][c], koff[c] | no);
+      for (int c = 0; c < KN; ++c) b.load(x.k[u][c], koff[c] | no);
     } else {
 #pragma unroll
       for (int c = 0; c < KN; ++c) {
         u32x2_any lo, hi;
         b.load(lo, koff[c] | no);
         b.load(hi, (koff[c] + 8) | no | ((c * 4 + g) * KL + 8 < p.c.d ? 0u : kNone));
-        k[u][c][0] = lo[0], k[u][c][1] = lo[1], k[u][c][2] = hi[0], k[u][c][3] = hi[1];
+        x.k[u][c][0] = lo[0], x.k[u][c][1] = lo[1], x.k[u][c][2] = hi[0], x.k[u][c][3] = hi[1];
       }
     }
   }
-  __device__ __forceinline__ void load_k(int tile, int w) {
+  __device__ __forceinline__ void load_k(Tile& x) const {
+    const int w = x.w;
     const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
     uint32_t no[NG];
 #pragma unroll
     for (int u = 0; u < NG; ++u) no[u] = 0;
-    if (!full) {
+    if (!x.full) {
 #pragma unroll
-      for (int u = 0; u < NG; ++u) no[u] = unseen(tile, u * 16 + q);
+      for (int u = 0; u < NG; ++u) no[u] = unseen(x, u * 16 + q);
     }
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
       if constexpr (P16) {
         const Buffer b(kbase() + lane_i64(base, w * NG + u) * ES);
-        load_cols(b, u, no[u]);
+        load_cols(x, b, u, no[u]);
         if constexpr (kCodes) {
           const Buffer sb(p.c.k_scales + lane_i64(srow, w * NG + u) * nb);
           if (nb == NB) {
 #pragma unroll
-            for (int i = 0; i < KW; ++i) ks[u][i] = NB == 2 ? sb.load2(q * 2 | no[u]) : sb.load4((q * NB + 4 * i) | no[u]);
+            for (int i = 0; i < KW; ++i) x.ks[u][i] = NB == 2 ? sb.load2(q * 2 | no[u]) : sb.load4((q * NB + 4 * i) | no[u]);
           } else {
 #pragma unroll
-            for (int i = 0; i < KW; ++i) ks[u][i] = 0;
+            for (int i = 0; i < KW; ++i) x.ks[u][i] = 0;
 #pragma unroll
             for (int i = 0; i < NB; ++i)
-              if (i < nb) ks[u][i / 4] |= sb.load1((q * nb + i) | no[u]) << (8 * (i % 4));
+              if (i < nb) x.ks[u][i / 4] |= sb.load1((q * nb + i) | no[u]) << (8 * (i % 4));
           }
         }
       } else {
         const uint8_t* kb = kbase() + shfl_i64(base, w * TILE + u * 16 + q) * ES;
 #pragma unroll
         for (int c = 0; c < KN; ++c) {
-          k[u][c] = {};
+          x.k[u][c] = {};
           const bool in = !((koff[c] | no[u]) & kNone);
           if (in && (!kCodes || (c * 4 + g) * KL + 8 < p.c.d)) {
-            k[u][c] = *reinterpret_cast<const KRaw*>(kb + koff[c]);
+            x.k[u][c] = *reinterpret_cast<const KRaw*>(kb + koff[c]);
           } else if (in) {
             const u32x2_any lo = *reinterpret_cast<const u32x2_any*>(kb + koff[c]);
-            k[u][c][0] = lo[0], k[u][c][1] = lo[1];
+            x.k[u][c][0] = lo[0], x.k[u][c][1] = lo[1];
           }
         }
         if constexpr (kCodes) {
           const uint8_t* sb = p.c.k_scales + shfl_i64(srow, w * TILE + u * 16 + q) * nb;
 #pragma unroll
-          for (int i = 0; i < KW; ++i) ks[u][i] = 0;
+          for (int i = 0; i < KW; ++i) x.ks[u][i] = 0;
 #pragma unroll
           for (int i = 0; i < NB; ++i)
-            if (i < nb && !no[u]) ks[u][i / 4] |= (uint32_t)sb[i] << (8 * (i % 4));
+            if (i < nb && !no[u]) x.ks[u][i / 4] |= (uint32_t)sb[i] << (8 * (i % 4));
         }
       }
     }
   }
 
-  __device__ __forceinline__ void load_v(int tile, int w) {
+  __device__ __forceinline__ void load_v(Tile& x) const {
+    const int w = x.w;
     const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
     uint32_t no[VT];
 #pragma unroll
     for (int i = 0; i < VT; ++i) no[i] = 0;
-    if (!full) {
+    if (!x.full) {
 #pragma unroll
-      for (int i = 0; i < VT; ++i) no[i] = unseen(tile, (i / 4) * 16 + g * 4 + i % 4);
+      for (int i = 0; i < VT; ++i) no[i] = unseen(x, (i / 4) * 16 + g * 4 + i % 4);
     }
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
@@ -373,31 +377,31 @@ struct Attn {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int c = 0; c < VC; ++c) b.load(v[c][u * 4 + r], voff[c][r] | no[u * 4 + r]);
+          for (int c = 0; c < VC; ++c) b.load(x.v[c][u * 4 + r], voff[c][r] | no[u * 4 + r]);
         if constexpr (kCodes) {
           const Buffer sb(p.c.v_scales + lane_i64(srow, w * NG + u) * nb);
-          if (full && nb == NB) {
+          if (x.full && nb == NB) {
 #pragma unroll
             for (int i = 0; i < NB / 2; ++i) {
               u32x2_any two;
               sb.load(two, g * 4 * NB + 8 * i);
-              vs[u][2 * i] = two[0], vs[u][2 * i + 1] = two[1];
+              x.vs[u][2 * i] = two[0], x.vs[u][2 * i + 1] = two[1];
             }
           } else {
 #pragma unroll
-            for (int i = 0; i < NB; ++i) vs[u][i] = 0;
+            for (int i = 0; i < NB; ++i) x.vs[u][i] = 0;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
               for (int c = 0; c < VC; ++c)
-                vs[u][vword(r, c)] |= sb.load1(((g * 4 + r) * nb + vblock(c)) | no[u * 4 + r] | (voff[c][r] & kNone))
+                x.vs[u][vword(r, c)] |= sb.load1(((g * 4 + r) * nb + vblock(c)) | no[u * 4 + r] | (voff[c][r] & kNone))
                                       << vshift(r, vblock(c));
           }
         }
       } else {
         if constexpr (kCodes) {
 #pragma unroll
-          for (int i = 0; i < NB; ++i) vs[u][i] = 0;
+          for (int i = 0; i < NB; ++i) x.vs[u][i] = 0;
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -407,10 +411,10 @@ struct Attn {
 #pragma unroll
           for (int c = 0; c < VC; ++c) {
             const bool in = !((voff[c][r] | no[i]) & kNone);
-            v[c][i] = {};
-            if (in) v[c][i] = *reinterpret_cast<const VRaw*>(vb + voff[c][r]);
+            x.v[c][i] = {};
+            if (in) x.v[c][i] = *reinterpret_cast<const VRaw*>(vb + voff[c][r]);
             if constexpr (kCodes) {
-              if (in) vs[u][vword(r, c)] |= (uint32_t)p.c.v_scales[sr * nb + vblock(c)] << vshift(r, vblock(c));
+              if (in) x.vs[u][vword(r, c)] |= (uint32_t)p.c.v_scales[sr * nb + vblock(c)] << vshift(r, vblock(c));
             }
           }
         }
@@ -428,40 +432,40 @@ struct Attn {
   }
   static __device__ __forceinline__ float scale_of(uint8_t b) { return __uint_as_float((uint32_t)b << 23); }
 
-  __device__ __forceinline__ Frag kfrag(int u, int c) const {
+  __device__ __forceinline__ Frag kfrag(const Tile& x, int u, int c) const {
     Frag f;
     if constexpr (CACHE == CACHE_CODES_BF16) {
-      const float s = scale_of(kscale(u, c));
+      const float s = scale_of(kscale(x, u, c));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = pair_bf16(k[u][c / 2][c % 2 * 2 + i / 2], s, i % 2);
+      for (int i = 0; i < 4; ++i) f[i] = pair_bf16(x.k[u][c / 2][c % 2 * 2 + i / 2], s, i % 2);
     } else if constexpr (CACHE == CACHE_CODES_F32) {
       float v4[8];
-      ckpt_values(make_uint2(k[u][c / 4][c % 4], 0), kscale(u, c), v4);
+      ckpt_values(make_uint2(x.k[u][c / 4][c % 4], 0), kscale(x, u, c), v4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[i] = __float_as_uint(v4[i]);
     } else {
-      f = k[u][c];
+      f = x.k[u][c];
     }
     return f;
   }
   // Columns of token slot i as loaded from memory, in the product's type.
   typedef uint32_t VWords __attribute__((ext_vector_type(kF32 ? VE : VE / 2)));
-  __device__ __forceinline__ VWords vwords(int i, int c) const {
+  __device__ __forceinline__ VWords vwords(const Tile& x, int i, int c) const {
     VWords f;
     if constexpr (CACHE == CACHE_CODES_BF16) {
-      const float s = scale_of(vscale(i, c));
+      const float s = scale_of(vscale(x, i, c));
 #pragma unroll
       for (int j = 0; j < VE / 4; ++j) {
-        f[2 * j] = pair_bf16(v[c][i][j], s, false);
-        f[2 * j + 1] = pair_bf16(v[c][i][j], s, true);
+        f[2 * j] = pair_bf16(x.v[c][i][j], s, false);
+        f[2 * j + 1] = pair_bf16(x.v[c][i][j], s, true);
       }
     } else if constexpr (CACHE == CACHE_CODES_F32) {
       float v8[8];
-      ckpt_values(make_uint2(v[c][i][0], VE == 8 ? v[c][i][VE / 4 - 1] : 0), vscale(i, c), v8);
+      ckpt_values(make_uint2(x.v[c][i][0], VE == 8 ? x.v[c][i][VE / 4 - 1] : 0), vscale(x, i, c), v8);
 #pragma unroll
       for (int j = 0; j < VE; ++j) f[j] = __float_as_uint(v8[j]);
     } else {
-      f = v[c][i];
+      f = x.v[c][i];
     }
     return f;
   }
@@ -471,7 +475,7 @@ struct Attn {
   }
 
   // ---- one tile: scores, then weights, then the sums of values
-  __device__ __forceinline__ void scores(float (&pr)[RT][VT]) const {
+  __device__ __forceinline__ void scores(const Tile& x, float (&pr)[RT][VT]) const {
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
       floatx4 s[RT];
@@ -479,7 +483,7 @@ struct Attn {
       for (int t = 0; t < RT; ++t) s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        const Frag f = kfrag(u, c);
+        const Frag f = kfrag(x, u, c);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           const Frag y = query(t, c);
@@ -537,7 +541,7 @@ struct Attn {
     }
   }
 
-  __device__ __forceinline__ void add_values(const float (&pr)[RT][VT], int tile, uint32_t okay, bool all) {
+  __device__ __forceinline__ void add_values(Tile& x, const float (&pr)[RT][VT], int tile, uint32_t okay, bool all) {
     if (MANY && !all && p.a.n_new > 1) {
       // Rows that see different tokens: a value that is not finite must not
       // reach, as 0 times itself, a row that does not see it.
@@ -546,21 +550,21 @@ struct Attn {
       for (int c = 0; c < VC; ++c)
 #pragma unroll
         for (int i = 0; i < VT; ++i) {
-          const VWords f = vwords(i, c);
+          const VWords f = vwords(x, i, c);
 #pragma unroll
           for (int j = 0; j < VE; ++j) bad |= (__float_as_uint(velem(f, j)) & 0x7F800000u) == 0x7F800000u;
         }
       if (__any(bad)) {
-        infinities(tile, okay);
-        clear_infinities();
+        infinities(x, tile, okay);
+        clear_infinities(x);
       }
     }
-    values(pr);
+    values(x, pr);
   }
 
   // What values that are not finite add to the rows that see them: a weight is
   // above 0, so an infinity gives itself, and a NaN counts as both infinities.
-  __device__ __forceinline__ void infinities(int tile, uint32_t okay) {
+  __device__ __forceinline__ void infinities(const Tile& x, int tile, uint32_t okay) {
     float sees[RT][VT];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
@@ -577,9 +581,9 @@ struct Attn {
         __builtin_amdgcn_sched_barrier(0);   // (one column at a time: this path is rare, its registers are not free)
 #pragma unroll
         for (int i = 0; i < VT; ++i) {
-          const float x = velem(vwords(i, c), j);
-          up[i] = !(x <= 3.4028235e38f) ? 1.f : 0.f;
-          down[i] = !(x >= -3.4028235e38f) ? 1.f : 0.f;
+          const float e = velem(vwords(x, i, c), j);
+          up[i] = !(e <= 3.4028235e38f) ? 1.f : 0.f;
+          down[i] = !(e >= -3.4028235e38f) ? 1.f : 0.f;
         }
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
@@ -603,7 +607,7 @@ struct Attn {
     return acc;
   }
   // Sets such values to 0, where they are.
-  __device__ __forceinline__ void clear_infinities() {
+  __device__ __forceinline__ void clear_infinities(Tile& x) {
 #pragma unroll
     for (int c = 0; c < VC; ++c)
 #pragma unroll
@@ -611,26 +615,26 @@ struct Attn {
         constexpr int W = VE * ES / 4;
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kCodes) {
-          const bool all = vscale(i, c) == 255;
+          const bool all = vscale(x, i, c) == 255;
 #pragma unroll
           for (int j = 0; j < W; ++j) {
-            uint32_t w = v[c][i][j];
+            uint32_t w = x.v[c][i][j];
 #pragma unroll
             for (int b = 0; b < 32; b += 8)
               if (all || (w >> b & 0x7F) == 0x7F) w &= ~(0xFFu << b);
-            v[c][i][j] = w;
+            x.v[c][i][j] = w;
           }
         } else {
 #pragma unroll
           for (int j = 0; j < W; ++j) {
-            uint32_t w = v[c][i][j];
+            uint32_t w = x.v[c][i][j];
             if (kF32) {
               if ((w & 0x7F800000u) == 0x7F800000u) w = 0;
             } else {
               if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
               if ((w & 0x7F800000u) == 0x7F800000u) w &= 0xFFFFu;
             }
-            v[c][i][j] = w;
+            x.v[c][i][j] = w;
           }
         }
       }
@@ -642,18 +646,18 @@ struct Attn {
         for (int i = 0; i < NB; ++i)
 #pragma unroll
           for (int b = 0; b < 32; b += 8)
-            if ((vs[u][i] >> b & 0xFF) == 0xFF) vs[u][i] &= ~(0x80u << b);
+            if ((x.vs[u][i] >> b & 0xFF) == 0xFF) x.vs[u][i] &= ~(0x80u << b);
     }
   }
 
   // O += V^T P^T.
-  __device__ __forceinline__ void values(const float (&pr)[RT][VT]) {
+  __device__ __forceinline__ void values(const Tile& x, const float (&pr)[RT][VT]) {
     if constexpr (kF32) {
 #pragma unroll
       for (int i = 0; i < VT; ++i)
 #pragma unroll
         for (int c = 0; c < VC; ++c) {
-          const VWords f = vwords(i, c);
+          const VWords f = vwords(x, i, c);
 #pragma unroll
           for (int j = 0; j < VE; ++j)
 #pragma unroll
@@ -671,7 +675,7 @@ struct Attn {
       for (int c = 0; c < VC; ++c) {
         VWords f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = vwords(i, c);
+        for (int i = 0; i < 8; ++i) f[i] = vwords(x, i, c);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
           Frag a;
@@ -687,23 +691,49 @@ struct Attn {
     }
   }
 
+  // Two tiles where they are small: a wave should have 8 KB on their way while it
+  // computes.
+  static constexpr bool kDouble = TILE * D * ES <= 4096 && (D == 64 || !MANY);
+
+  __device__ __forceinline__ void load(Tile& x, int tile) {
+    find(x, tile);
+    load_k(x);
+    load_v(x);
+  }
+  __device__ __forceinline__ void compute(Tile& x) {
+    float pr[RT][VT];
+    scores(x, pr);
+    weights(pr, x.at, x.ok, x.full);
+    add_values(x, pr, x.at, x.ok, x.full);
+  }
   __device__ __forceinline__ void tiles(int from, int to) {
     if (from >= to) return;
-    int w = find(from);
-    load_k(from, w);
-    load_v(from, w);
-    for (int t = from; t < to; ++t) {
-      const uint32_t okay = ok;
-      const bool all = full;
-      float pr[RT][VT];
-      scores(pr);
-      if (t + 1 < to) {
-        w = find(t + 1);
-        load_k(t + 1, w);
+    Tile a;
+    load(a, from);
+    if constexpr (kDouble) {
+      Tile b;
+      for (int t = from;; t += 2) {
+        if (t + 1 < to) load(b, t + 1);
+        compute(a);
+        if (t + 1 >= to) return;
+        if (t + 2 < to) load(a, t + 2);
+        compute(b);
+        if (t + 2 >= to) return;
       }
-      weights(pr, t, okay, all);
-      add_values(pr, t, okay, all);
-      if (t + 1 < to) load_v(t + 1, w);
+    } else {
+      for (int t = from; t < to; ++t) {
+        const uint32_t okay = a.ok;
+        const bool all = a.full;
+        float pr[RT][VT];
+        scores(a, pr);
+        if (t + 1 < to) {
+          find(a, t + 1);
+          load_k(a);
+        }
+        weights(pr, t, okay, all);
+        add_values(a, pr, t, okay, all);
+        if (t + 1 < to) load_v(a);
+      }
     }
   }
 };
