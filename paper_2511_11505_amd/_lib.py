@@ -74,6 +74,7 @@ class fs_saved(ctypes.Structure):
 
 class fs_rope(ctypes.Structure):
     _fields_ = [("layout", _i32), ("first", _i32), ("rot_dim", _i32), ("mscale", ctypes.c_double), ("freqs", _vp)]
+    device = None       # of the tensors it was made of
 
 
 class fs_rotary_desc(ctypes.Structure):
@@ -84,6 +85,7 @@ class fs_kv_cache(ctypes.Structure):
     _fields_ = ([(n, _i32) for n in ("abi_version", "dtype", "codes", "n_pages", "kv_heads", "page_size", "head_dim")]
                 + [("k", _vp), ("v", _vp), ("page_stride", _i64), ("head_stride", _i64), ("place_stride", _i64),
                    ("k_scales", _vp), ("v_scales", _vp)])
+    device = None       # of the tensors it was made of
 
 
 class fs_page_table(ctypes.Structure):
@@ -591,26 +593,37 @@ def fs_layer_norm_backward(desc, dy, x, mean, rstd, gamma, dres, dx, dgamma, dbe
 # -------------------------------------------- the attention sublayer's entries
 # Heads are 3-D tensors [tokens, heads, head_dim] of unit column stride (their
 # other strides are passed on) or int addresses of gapless ones.
-def _heads(t, name, dtype, tokens, heads, d, dev):
+def _heads(t, name, elem, shape, dev):
     """(address, token stride, head stride) of an argument."""
     if t is None or isinstance(t, int):
-        return t, heads * d, d
-    if t.dtype is not _ELEM.get(dtype) or t.shape != (tokens, heads, d):
-        _bad(name, f"[{tokens}, {heads}, {d}] of the descriptor's type, not {list(t.shape)} of {t.dtype}")
+        return t, shape[1] * shape[2], shape[2]
+    if t.dtype is not elem or t.shape != shape:
+        _bad(name, f"{list(shape)} of the descriptor's type, not {list(t.shape)} of {t.dtype}")
     ts, hs, step = t.stride()
-    if step != 1 and d > 1:
+    if step != 1 and shape[2] > 1:
         _bad(name, "of unit column stride")
     if t.get_device() != dev:
         _bad(name, "on the current GPU")
     return t.data_ptr(), ts, hs
 
 
+def _ints(t, name, n, dev):
+    """Address of a gapless int32 vector."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not _ELEM["i32"] or t.shape != (n,) or not t.is_contiguous():
+        _bad(name, f"[{n}] contiguous int32, not {list(t.shape)} of {t.dtype}")
+    if t.get_device() != dev:
+        _bad(name, "on the current GPU")
+    return t.data_ptr()
+
+
 def _pages(t, dev):
     """fs_page_table of an int32 tensor [sequences, max_pages] of unit column
     stride, or an fs_page_table."""
-    if isinstance(t, fs_page_table) or t is None:
+    if t is None or isinstance(t, fs_page_table):
         return t
-    if t.dtype is not _ELEM.get("i32") or t.dim() != 2:
+    if t.dtype is not _ELEM["i32"] or t.dim() != 2:
         _bad("pages", f"2-D int32, not {list(t.shape)} of {t.dtype}")
     b, n = t.shape
     ld, step = t.stride()
@@ -622,9 +635,9 @@ def _pages(t, dev):
 
 
 def _on(struct, name, dev):
-    """A cache or rope made of tensors: these have to be on the current GPU."""
-    at = getattr(struct, "device", None)
-    if at is not None and at != dev:
+    """A cache or rope: where it is made of tensors, these have to be on the
+    current GPU."""
+    if struct is not None and struct.device != dev and struct.device is not None:
         _bad(name, "on the current GPU")
     return struct
 
@@ -689,31 +702,30 @@ def fs_rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, trai
 
 def fs_rotary(desc, rope, x, positions, out, stream=None):
     dev, s = _here(stream)
-    dt, n, h, d = desc.dtype, desc.tokens, desc.heads, desc.head_dim
-    _check(load().fs_rotary(ctypes.byref(desc), _on(rope, "rope", dev), *_heads(x, "x", dt, n, h, d, dev),
-                            _flat(positions, "positions", "i32", (n,), dev), *_heads(out, "out", dt, n, h, d, dev), s))
+    shape, elem = (desc.tokens, desc.heads, desc.head_dim), _ELEM.get(desc.dtype)
+    _check(load().fs_rotary(desc, _on(rope, "rope", dev), *_heads(x, "x", elem, shape, dev),
+                            _ints(positions, "positions", shape[0], dev), *_heads(out, "out", elem, shape, dev), s))
 
 
 def fs_rotary_backward(desc, rope, dout, positions, dx, stream=None):
     dev, s = _here(stream)
-    dt, n, h, d = desc.dtype, desc.tokens, desc.heads, desc.head_dim
-    _check(load().fs_rotary_backward(ctypes.byref(desc), _on(rope, "rope", dev),
-                                     *_heads(dout, "dout", dt, n, h, d, dev),
-                                     _flat(positions, "positions", "i32", (n,), dev),
-                                     *_heads(dx, "dx", dt, n, h, d, dev), s))
+    shape, elem = (desc.tokens, desc.heads, desc.head_dim), _ELEM.get(desc.dtype)
+    _check(load().fs_rotary_backward(desc, _on(rope, "rope", dev), *_heads(dout, "dout", elem, shape, dev),
+                                     _ints(positions, "positions", shape[0], dev),
+                                     *_heads(dx, "dx", elem, shape, dev), s))
 
 
 def fs_cache_append(cache, rope, q, k, v, seqs, positions, pages, q_out, stream=None):
     """q, q_out [tokens, q_heads, head_dim] or None; k, v [tokens, kv_heads,
     head_dim]; seqs [tokens] or None, positions [tokens] int32."""
     dev, s = _here(stream)
-    dt, d, n = cache.dtype, cache.head_dim, k.shape[0]
-    h = 0 if q is None else q.shape[1]
-    _check(load().fs_cache_append(_on(cache, "cache", dev), _on(rope, "rope", dev), n, h,
-                                  *_heads(q, "q", dt, n, h, d, dev), *_heads(k, "k", dt, n, cache.kv_heads, d, dev),
-                                  *_heads(v, "v", dt, n, cache.kv_heads, d, dev), _flat(seqs, "seqs", "i32", (n,), dev),
-                                  _flat(positions, "positions", "i32", (n,), dev), _pages(pages, dev),
-                                  *_heads(q_out, "q_out", dt, n, h, d, dev), s))
+    elem, d, n = _ELEM.get(cache.dtype), cache.head_dim, k.shape[0]
+    rows, kv = (n, 0 if q is None else q.shape[1], d), (n, cache.kv_heads, d)
+    _check(load().fs_cache_append(_on(cache, "cache", dev), _on(rope, "rope", dev), n, rows[1],
+                                  *_heads(q, "q", elem, rows, dev), *_heads(k, "k", elem, kv, dev),
+                                  *_heads(v, "v", elem, kv, dev), _ints(seqs, "seqs", n, dev),
+                                  _ints(positions, "positions", n, dev), _pages(pages, dev),
+                                  *_heads(q_out, "q_out", elem, rows, dev), s))
 
 
 def fs_paged_attention_workspace(desc, cache, pages):
@@ -726,13 +738,12 @@ def fs_paged_attention(desc, cache, q, lengths, pages, out, ws, lse=None, stream
     """q, out [sequences * new_tokens, q_heads, head_dim]; lengths [sequences]
     int32; lse [sequences * new_tokens, q_heads] fp32 or None."""
     dev, s = _here(stream)
-    t = _pages(pages, dev)
-    dt, h, d = cache.dtype, desc.q_heads, cache.head_dim
-    n = t.sequences * desc.new_tokens
+    t, elem = _pages(pages, dev), _ELEM.get(cache.dtype)
+    shape = (t.sequences * desc.new_tokens, desc.q_heads, cache.head_dim)
     wp, wb = _space(ws, dev)
-    _check(load().fs_paged_attention(ctypes.byref(desc), _on(cache, "cache", dev), *_heads(q, "q", dt, n, h, d, dev),
-                                     _flat(lengths, "lengths", "i32", (t.sequences,), dev), t,
-                                     *_heads(out, "out", dt, n, h, d, dev), _flat(lse, "lse", FS_F32, (n, h), dev),
+    _check(load().fs_paged_attention(desc, _on(cache, "cache", dev), *_heads(q, "q", elem, shape, dev),
+                                     _ints(lengths, "lengths", t.sequences, dev), t,
+                                     *_heads(out, "out", elem, shape, dev), _flat(lse, "lse", FS_F32, shape[:2], dev),
                                      wp, wb, s))
 
 

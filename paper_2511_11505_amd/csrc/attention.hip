@@ -55,13 +55,18 @@ Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 int64_t part_rows(const Shape& h, const PagedCache& c) { return (int64_t)h.workers * c.kv_heads * 2 * 16 * h.rt; }
 
+template <int CACHE, int D, int RT, int PAGES>
+hipError_t run_new(const AttnPlan& p, hipStream_t s) {
+  if constexpr (RT == 1)
+    if (p.a.n_new == 1) return run_attention<CACHE, D, RT, PAGES, false>(p, s);
+  return run_attention<CACHE, D, RT, PAGES, true>(p, s);
+}
 template <int CACHE, int D, int RT>
 hipError_t run_pages(const AttnPlan& p, hipStream_t s) {
-  const bool groups = p.c.page_size % 16 == 0;
-  if constexpr (RT == 1)
-    if (p.a.n_new == 1)
-      return groups ? run_attention<CACHE, D, RT, true, false>(p, s) : run_attention<CACHE, D, RT, false, false>(p, s);
-  return groups ? run_attention<CACHE, D, RT, true, true>(p, s) : run_attention<CACHE, D, RT, false, true>(p, s);
+  if (p.c.page_size % 16) return run_new<CACHE, D, RT, PAGES_ANY>(p, s);
+  if constexpr (CACHE == CACHE_CODES_BF16 || CACHE == CACHE_CODES_F32)
+    if (p.c.d <= D - 32) return run_new<CACHE, D, RT, PAGES_GROUPS_SHORT>(p, s);
+  return run_new<CACHE, D, RT, PAGES_GROUPS>(p, s);
 }
 template <int CACHE>
 hipError_t run_cache(int width, int rt, const AttnPlan& p, hipStream_t s) {

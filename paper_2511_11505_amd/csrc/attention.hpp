@@ -8,6 +8,10 @@ namespace fs {
 
 enum { CACHE_BF16 = 0, CACHE_F32 = 1, CACHE_CODES_BF16 = 2, CACHE_CODES_F32 = 3 };
 
+// Pages: of any size; of whole groups of 16 tokens; of whole groups, with codes of
+// fewer blocks in a row than the kernel's width has.
+enum { PAGES_ANY = 0, PAGES_GROUPS = 1, PAGES_GROUPS_SHORT = 2 };
+
 constexpr int kAttnWaves = 4;
 constexpr int kAttnMaxItems = 4096;    // of a divided call: 16 for each thread
 constexpr int kAttnMinTiles = 4;       // of a workgroup's part: one for each wave
@@ -28,7 +32,7 @@ struct AttnPlan {
 };
 
 // MANY: more than one new token, or rows for more than one row tile.
-template <int CACHE, int D, int RT, bool P16, bool MANY>
+template <int CACHE, int D, int RT, int PAGES, bool MANY>
 hipError_t run_attention(const AttnPlan& p, hipStream_t s);
 
 }  // namespace fs

@@ -4,21 +4,29 @@
 
 namespace fs {
 
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, true, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, true, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, false, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, false, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 2, true, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 2, false, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, true, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, true, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, false, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, false, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 2, true, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 2, false, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, true, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, true, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, false, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, false, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_ANY, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS_SHORT, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_ANY, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS_SHORT, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_ANY, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS_SHORT, false>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
 
 }  // namespace fs

@@ -42,6 +42,7 @@ template <int BYTES> struct RawT;
 template <> struct RawT<16> { typedef u32x4_any type; };
 template <> struct RawT<8> { typedef u32x2_any type; };
 typedef uint32_t u32x1_any __attribute__((ext_vector_type(1), aligned(1)));
+typedef uint16_t u16_any __attribute__((aligned(1)));
 template <> struct RawT<4> { typedef u32x1_any type; };
 
 __device__ __forceinline__ int lane_i(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
@@ -121,8 +122,9 @@ __device__ __forceinline__ Item item_of(const AttnPlan& p, int item) {
   return t;
 }
 
-template <int CACHE, int D, int RT, bool P16, bool MANY>
+template <int CACHE, int D, int RT, int PAGES, bool MANY>
 struct Attn {
+  static constexpr bool P16 = PAGES != PAGES_ANY;
   static constexpr bool kF32 = CACHE == CACHE_F32 || CACHE == CACHE_CODES_F32;
   static constexpr bool kCodes = CACHE == CACHE_CODES_BF16 || CACHE == CACHE_CODES_F32;
   static constexpr int ES = kCodes ? 1 : kF32 ? 4 : 2;       // bytes of a cache element
@@ -139,7 +141,8 @@ struct Attn {
   static constexpr int NO = D / 16;                          // result tiles of a row tile
   static constexpr int STRIDE = D + 4;                       // LDS row (floats)
   static constexpr int NB = D / kCkptBlock;                  // scale bytes of a full-width row
-  static constexpr int KW = (NB + 3) / 4;                    // words of a row's scales; of 4 rows': NB
+  static constexpr int KW = (NB + 3) / 4;                    // words of a row's scales
+  static constexpr int VW = NB == 2 && P16 ? 2 : 4 * KW;     // words of four rows'
   typedef typename std::conditional<kF32, float, bf16_t>::type T;
   typedef u32x4_any KRaw;
   typedef typename RawT<VE * ES>::type VRaw;
@@ -153,6 +156,7 @@ struct Attn {
   // (P16) or token window + i, or -1, and its index among the scale rows
   int window;
   int64_t base, srow;
+  bool last;
   uint32_t koff[KN], voff[VC][4];   // bytes in a row; P16: from the group's start
   int lim[RT], low[RT];
 
@@ -167,10 +171,11 @@ struct Attn {
   struct Tile {
     KRaw k[NG][KN];
     VRaw v[VC][VT];
-    uint32_t ks[kCodes ? NG : 1][KW], vs[kCodes ? NG : 1][NB];   // scale bytes of a row; of rows 4 g .. 4 g + 3
+    uint32_t ks[kCodes ? NG : 1][KW], vs[kCodes ? NG : 1][VW];   // scale bytes of a row; of rows 4 g .. 4 g + 3
     int at, w;       // which tile, at which position of the window
     uint32_t ok;     // bit t: token t has a place
     bool full;       // every row sees every token
+    bool edge;       // of row_scales
   };
 
   __device__ __forceinline__ Attn(const AttnPlan& plan, int ln, int hd, Frag* queries)
@@ -203,7 +208,7 @@ struct Attn {
 #pragma unroll
     for (int c = 0; c < KN; ++c) {
       const int col = c * 4 * KL + g * KL;
-      koff[c] = col < p.c.d ? (q * step + col) * ES : kNone;
+      koff[c] = col < p.c.d ? (q * step + col) * ES : kNone;   // (of P16)
     }
 #pragma unroll
     for (int c = 0; c < VC; ++c)
@@ -242,28 +247,37 @@ struct Attn {
     if (tile < window + PER) return;
     window = tile;
     const int t = tile * TILE + (P16 ? lane * 16 : lane);
-    base = -1, srow = 0;
+    base = -1, srow = 0, last = false;
     if (t < it.hi && t >= (P16 ? it.lo - 15 : it.lo)) {
       const int slot = t / p.c.page_size, place = t - slot * p.c.page_size;
       const int page = p.c.table[(int64_t)it.seq * p.c.ldt + slot];
       if (page >= 0 && page < p.c.n_pages) {
         base = (int64_t)page * p.c.page_stride + (int64_t)place * p.c.place_stride;
         srow = ((int64_t)page * p.c.kv_heads + head) * p.c.page_size + place;
+        if constexpr (kCodes) {
+          const int64_t rows = (int64_t)p.c.n_pages * p.c.kv_heads * p.c.page_size;
+          const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
+          last = (rows - srow - (P16 ? 15 : 0)) * nb < kRowBytes;
+        }
       }
     }
   }
   // Scale bytes of column blocks: a lane's columns of V in chunk c are of block
   // vblock(c).
   __device__ __forceinline__ int vblock(int c) const { return (c * 16 * VE + q * VE) / kCkptBlock; }
-  // Where the byte of row r (of four) and block b is among the words of four rows
-  // (b / 4 is the chunk at the largest width).
-  static constexpr int vword(int r, int c) { return NB == 8 ? r * 2 + c : r * NB / 4; }
-  static __device__ __forceinline__ int vshift(int r, int b) { return 8 * ((r * NB + b) % 4); }
+  // Where the byte of row r (of four) and block b is: two rows to a word in groups
+  // of 64 columns (they are loaded together), else words of its own (b / 4 is the
+  // chunk at the largest width).
+  static constexpr int vword(int r, int c) { return VW == 2 ? r / 2 : KW == 2 ? r * 2 + c : r; }
+  static __device__ __forceinline__ int vshift(int r, int b) { return 8 * (VW == 2 ? r % 2 * 2 + b : b % 4); }
   __device__ __forceinline__ uint8_t kscale(const Tile& x, int u, int c) const {
     if constexpr (!kCodes) return 0;
-    // (64 columns a load of the four lanes, two blocks)
+    // (64 columns a load of the four lanes, two blocks; bytes past the row's are
+    // another row's, and 0 times what they stand for may not be 0)
     constexpr int S = KL / KE;
-    return (uint8_t)(x.ks[u][c / S / 2] >> (16 * (c / S % 2) + 8 * (g >> 1)));
+    const int word = c / S / 2, past = (p.c.d + kCkptBlock - 1) / kCkptBlock - 4 * word;
+    const uint32_t mask = PAGES == PAGES_GROUPS || past >= 4 ? ~0u : past <= 0 ? 0u : (1u << (8 * past)) - 1;
+    return (uint8_t)((x.ks[u][word] & mask) >> (16 * (c / S % 2) + 8 * (g >> 1)));
   }
   __device__ __forceinline__ uint8_t vscale(const Tile& x, int i, int c) const {
     if constexpr (!kCodes) return 0;
@@ -281,6 +295,7 @@ struct Attn {
     } else {
       x.ok = (uint32_t)(__ballot(base >= 0) >> (w * TILE)) & (uint32_t)((1ull << TILE) - 1);
     }
+    x.edge = kCodes && (__ballot(last) >> (P16 ? w * NG : w * TILE)) & ((1ull << (P16 ? NG : TILE)) - 1);
     x.full = x.ok == (uint32_t)((1ull << TILE) - 1) && t0 >= it.lo_all && t0 + TILE <= it.hi_all;
   }
   // 0 where token `tok` of the tile is one that some row sees, else kNone (for an
@@ -290,136 +305,175 @@ struct Attn {
     return (x.ok >> tok & 1) && t >= it.lo && t < it.hi ? 0u : kNone;
   }
 
-  // P16: a buffer starts at the group, and a lane's offsets never change; else a
-  // lane's tokens' places come from the lanes that looked them up.
-  // (codes of a head_dim that 16 does not divide end inside a load)
-  __device__ __forceinline__ void load_cols(Tile& x, const Buffer& b, int u, uint32_t no) const {
-    if (!kCodes || p.c.d % 16 == 0) {
+  // The scale bytes of one row as whole words.  Where a row has fewer bytes, the
+  // rest are the next row's; one by one, where it is not sure that there is a next
+  // row, or this one.
+  static constexpr int kRowBytes = NB == 2 ? 2 : 4 * KW;
+  template <bool FAST>
+  __device__ __forceinline__ void row_scales(const uint8_t* scales, int64_t row, bool in, uint32_t* out) const {
+    const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
+    const uint8_t* at = scales + row * nb;
+    if constexpr (FAST) {
+      if constexpr (NB == 2) {
+        out[0] = *reinterpret_cast<const u16_any*>(at);
+      } else {
 #pragma unroll
-      for (int c = 0; c < KN; ++c) b.load(x.k[u][c], koff[c] | no);
+        for (int i = 0; i < KW; ++i) out[i] = (*reinterpret_cast<const u32x1_any*>(at + 4 * i))[0];
+      }
     } else {
 #pragma unroll
-      for (int c = 0; c < KN; ++c) {
-        u32x2_any lo, hi;
-        b.load(lo, koff[c] | no);
-        b.load(hi, (koff[c] + 8) | no | ((c * 4 + g) * KL + 8 < p.c.d ? 0u : kNone));
-        x.k[u][c][0] = lo[0], x.k[u][c][1] = lo[1], x.k[u][c][2] = hi[0], x.k[u][c][3] = hi[1];
-      }
+      for (int i = 0; i < KW; ++i) out[i] = 0;
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        if (in && i < nb) out[i / 4] |= (uint32_t)at[i] << (8 * (i % 4));
     }
   }
-  __device__ __forceinline__ void load_k(Tile& x) const {
-    const int w = x.w;
-    const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
-    uint32_t no[NG];
-#pragma unroll
-    for (int u = 0; u < NG; ++u) no[u] = 0;
-    if (!x.full) {
-#pragma unroll
-      for (int u = 0; u < NG; ++u) no[u] = unseen(x, u * 16 + q);
-    }
+
+  // P16: a buffer starts at the group, and a lane's offsets never change (past
+  // head_dim they are kNone, for 0); else a lane's tokens' places come from the
+  // lanes that looked them up, and columns past head_dim are loaded from inside the
+  // row (kfrag clears them).  FAST: a full tile; its loads have no branches
+  // between them, else they would wait for one another.  (PAGES_GROUPS has none in
+  // any tile.)
+  template <bool FAST>
+  __device__ __forceinline__ void k_rows(Tile& x) const {
+    const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock, w = x.w;
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
+      uint32_t no = 0;
+      if (!FAST && !x.full) no = unseen(x, u * 16 + q);
       if constexpr (P16) {
         const Buffer b(kbase() + lane_i64(base, w * NG + u) * ES);
-        load_cols(x, b, u, no[u]);
+        if (!kCodes || p.c.d % 16 == 0) {
+#pragma unroll
+          for (int c = 0; c < KN; ++c) b.load(x.k[u][c], koff[c] | no);
+        } else {
+          // (codes that end inside a load)
+#pragma unroll
+          for (int c = 0; c < KN; ++c) {
+            u32x2_any lo, hi;
+            b.load(lo, koff[c] | no);
+            b.load(hi, (koff[c] + 8) | no | ((c * 4 + g) * KL + 8 < p.c.d ? 0u : kNone));
+            x.k[u][c][0] = lo[0], x.k[u][c][1] = lo[1], x.k[u][c][2] = hi[0], x.k[u][c][3] = hi[1];
+          }
+        }
         if constexpr (kCodes) {
-          const Buffer sb(p.c.k_scales + lane_i64(srow, w * NG + u) * nb);
-          if (nb == NB) {
+          const int64_t row = lane_i64(srow, w * NG + u);
+          if constexpr (PAGES == PAGES_GROUPS) {
+            const Buffer sb(p.c.k_scales + row * nb);
 #pragma unroll
-            for (int i = 0; i < KW; ++i) x.ks[u][i] = NB == 2 ? sb.load2(q * 2 | no[u]) : sb.load4((q * NB + 4 * i) | no[u]);
+            for (int i = 0; i < KW; ++i) x.ks[u][i] = NB == 2 ? sb.load2(q * 2 | no) : sb.load4((q * NB + 4 * i) | no);
           } else {
-#pragma unroll
-            for (int i = 0; i < KW; ++i) x.ks[u][i] = 0;
-#pragma unroll
-            for (int i = 0; i < NB; ++i)
-              if (i < nb) x.ks[u][i / 4] |= sb.load1((q * nb + i) | no[u]) << (8 * (i % 4));
+            row_scales<FAST>(p.c.k_scales, row + q, !no, x.ks[u]);
           }
         }
       } else {
         const uint8_t* kb = kbase() + shfl_i64(base, w * TILE + u * 16 + q) * ES;
+        if constexpr (FAST) {
+          if (!kCodes || p.c.d % 16 == 0) {
 #pragma unroll
-        for (int c = 0; c < KN; ++c) {
-          x.k[u][c] = {};
-          const bool in = !((koff[c] | no[u]) & kNone);
-          if (in && (!kCodes || (c * 4 + g) * KL + 8 < p.c.d)) {
-            x.k[u][c] = *reinterpret_cast<const KRaw*>(kb + koff[c]);
-          } else if (in) {
-            const u32x2_any lo = *reinterpret_cast<const u32x2_any*>(kb + koff[c]);
-            x.k[u][c][0] = lo[0], x.k[u][c][1] = lo[1];
+            for (int c = 0; c < KN; ++c) x.k[u][c] = *reinterpret_cast<const KRaw*>(kb + kin(c, 0, KL));
+          } else {
+#pragma unroll
+            for (int c = 0; c < KN; ++c) {
+              const u32x2_any lo = *reinterpret_cast<const u32x2_any*>(kb + kin(c, 0, 8));
+              const u32x2_any hi = *reinterpret_cast<const u32x2_any*>(kb + kin(c, 8, 8));
+              x.k[u][c][0] = lo[0], x.k[u][c][1] = lo[1], x.k[u][c][2] = hi[0], x.k[u][c][3] = hi[1];
+            }
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < KN; ++c) {
+            x.k[u][c] = {};
+            if constexpr (kCodes) {
+#pragma unroll
+              for (int h = 0; h < KL; h += 8) {
+                u32x2_any v = {};
+                if (!no && (c * 4 + g) * KL + h < p.c.d) v = *reinterpret_cast<const u32x2_any*>(kb + kin(c, h, 8));
+                x.k[u][c][h / 4] = v[0], x.k[u][c][h / 4 + 1] = v[1];
+              }
+            } else {
+              if (!no && (c * 4 + g) * KL < p.c.d) x.k[u][c] = *reinterpret_cast<const KRaw*>(kb + kin(c, 0, KL));
+            }
           }
         }
-        if constexpr (kCodes) {
-          const uint8_t* sb = p.c.k_scales + shfl_i64(srow, w * TILE + u * 16 + q) * nb;
-#pragma unroll
-          for (int i = 0; i < KW; ++i) x.ks[u][i] = 0;
-#pragma unroll
-          for (int i = 0; i < NB; ++i)
-            if (i < nb && !no[u]) x.ks[u][i / 4] |= (uint32_t)sb[i] << (8 * (i % 4));
-        }
+        if constexpr (kCodes) row_scales<FAST>(p.c.k_scales, shfl_i64(srow, w * TILE + u * 16 + q), !no, x.ks[u]);
       }
     }
   }
+  // Byte offset in a row of `n` of this lane's columns of load c from its h-th, or
+  // of the row's last n.
+  __device__ __forceinline__ uint32_t kin(int c, int h, int n) const {
+    return (uint32_t)min((c * 4 + g) * KL + h, p.c.d - n) * ES;
+  }
 
-  __device__ __forceinline__ void load_v(Tile& x) const {
-    const int w = x.w;
-    const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock;
-    uint32_t no[VT];
-#pragma unroll
-    for (int i = 0; i < VT; ++i) no[i] = 0;
-    if (!x.full) {
-#pragma unroll
-      for (int i = 0; i < VT; ++i) no[i] = unseen(x, (i / 4) * 16 + g * 4 + i % 4);
-    }
+  template <bool FAST>
+  __device__ __forceinline__ void v_rows(Tile& x) const {
+    const int nb = (p.c.d + kCkptBlock - 1) / kCkptBlock, w = x.w;
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
+      uint32_t no[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) no[r] = 0;
+      if (!FAST && !x.full) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) no[r] = unseen(x, u * 16 + g * 4 + r);
+      }
       if constexpr (P16) {
         const Buffer b(vbase() + lane_i64(base, w * NG + u) * ES);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int c = 0; c < VC; ++c) b.load(x.v[c][u * 4 + r], voff[c][r] | no[u * 4 + r]);
+          for (int c = 0; c < VC; ++c) b.load(x.v[c][u * 4 + r], voff[c][r] | no[r]);
         if constexpr (kCodes) {
-          const Buffer sb(p.c.v_scales + lane_i64(srow, w * NG + u) * nb);
-          if (x.full && nb == NB) {
+          const int64_t row = lane_i64(srow, w * NG + u);
+          const Buffer sb(p.c.v_scales + row * nb);
+          if constexpr (PAGES == PAGES_GROUPS) {
+            // (also of rows that nobody sees: add_values clears those)
 #pragma unroll
-            for (int i = 0; i < NB / 2; ++i) {
+            for (int i = 0; i < VW / 2; ++i) {
               u32x2_any two;
-              sb.load(two, g * 4 * NB + 8 * i);
+              sb.load(two, (g * 4 * NB + 8 * i) | (x.ok >> (16 * u) & 1 ? 0u : kNone));
               x.vs[u][2 * i] = two[0], x.vs[u][2 * i + 1] = two[1];
             }
-          } else {
-#pragma unroll
-            for (int i = 0; i < NB; ++i) x.vs[u][i] = 0;
+          } else if constexpr (VW == 2) {
+            x.vs[u][0] = x.vs[u][1] = 0;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
+              x.vs[u][r / 2] |= sb.load1(((g * 4 + r) * nb + vblock(0)) | no[r] | (voff[0][r] & kNone))
+                                << vshift(r, vblock(0));
+          } else {
 #pragma unroll
-              for (int c = 0; c < VC; ++c)
-                x.vs[u][vword(r, c)] |= sb.load1(((g * 4 + r) * nb + vblock(c)) | no[u * 4 + r] | (voff[c][r] & kNone))
-                                      << vshift(r, vblock(c));
+            for (int r = 0; r < 4; ++r) row_scales<FAST>(p.c.v_scales, row + g * 4 + r, !no[r], &x.vs[u][r * KW]);
           }
         }
       } else {
-        if constexpr (kCodes) {
-#pragma unroll
-          for (int i = 0; i < NB; ++i) x.vs[u][i] = 0;
-        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int i = u * 4 + r, from = w * TILE + u * 16 + g * 4 + r;
           const uint8_t* vb = vbase() + shfl_i64(base, from) * ES;
-          const int64_t sr = kCodes ? shfl_i64(srow, from) : 0;
 #pragma unroll
           for (int c = 0; c < VC; ++c) {
-            const bool in = !((voff[c][r] | no[i]) & kNone);
-            x.v[c][i] = {};
-            if (in) x.v[c][i] = *reinterpret_cast<const VRaw*>(vb + voff[c][r]);
-            if constexpr (kCodes) {
-              if (in) x.vs[u][vword(r, c)] |= (uint32_t)p.c.v_scales[sr * nb + vblock(c)] << vshift(r, vblock(c));
+            const uint8_t* at = vb + (uint32_t)min(c * 16 * VE + q * VE, p.c.d - VE) * ES;
+            if constexpr (FAST) {
+              x.v[c][i] = *reinterpret_cast<const VRaw*>(at);
+            } else {
+              x.v[c][i] = {};
+              if (!no[r]) x.v[c][i] = *reinterpret_cast<const VRaw*>(at);
             }
           }
+          if constexpr (kCodes) row_scales<FAST>(p.c.v_scales, shfl_i64(srow, from), !no[r], &x.vs[u][r * KW]);
         }
       }
     }
+  }
+  __device__ __forceinline__ void load_k(Tile& x) const {
+    if (PAGES != PAGES_GROUPS && x.full && !x.edge) k_rows<true>(x);
+    else k_rows<false>(x);
+  }
+  __device__ __forceinline__ void load_v(Tile& x) const {
+    if (PAGES != PAGES_GROUPS && x.full && !x.edge) v_rows<true>(x);
+    else v_rows<false>(x);
   }
 
   // ---- operands
@@ -446,6 +500,8 @@ struct Attn {
     } else {
       f = x.k[u][c];
     }
+    // (Q is 0 past head_dim, but 0 times an infinity is not)
+    if (!P16 && kcol(c) >= p.c.d) f = Frag{};
     return f;
   }
   // Columns of token slot i as loaded from memory, in the product's type.
@@ -542,6 +598,21 @@ struct Attn {
   }
 
   __device__ __forceinline__ void add_values(Tile& x, const float (&pr)[RT][VT], int tile, uint32_t okay, bool all) {
+    if (kCodes && PAGES == PAGES_GROUPS && !all) {
+      // scales of rows that nobody sees (0 times what they stand for may not be 0)
+#pragma unroll
+      for (int i = 0; i < VT; ++i) {
+        const int tok = (i / 4) * 16 + g * 4 + i % 4, at = tile * TILE + tok;
+        const bool some = (okay >> tok & 1) && at >= it.lo && at < it.hi;
+        uint32_t* w = &x.vs[i / 4][vword(i % 4, 0)];
+        if constexpr (VW == 2) {
+          w[0] &= some ? ~0u : i % 2 ? 0xFFFFu : 0xFFFF0000u;
+        } else {
+#pragma unroll
+          for (int j = 0; j < KW; ++j) w[j] = some ? w[j] : 0u;
+        }
+      }
+    }
     if (MANY && !all && p.a.n_new > 1) {
       // Rows that see different tokens: a value that is not finite must not
       // reach, as 0 times itself, a row that does not see it.
@@ -643,7 +714,7 @@ struct Attn {
 #pragma unroll
       for (int u = 0; u < NG; ++u)
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
+        for (int i = 0; i < VW; ++i)
 #pragma unroll
           for (int b = 0; b < 32; b += 8)
             if ((x.vs[u][i] >> b & 0xFF) == 0xFF) x.vs[u][i] &= ~(0x80u << b);
@@ -757,9 +828,9 @@ __device__ __forceinline__ void finish_row(const AttnPlan& p, const Item& it, in
   }
 }
 
-template <int CACHE, int D, int RT, bool P16, bool MANY>
+template <int CACHE, int D, int RT, int PAGES, bool MANY>
 __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void attention_kernel(AttnPlan p) {
-  typedef Attn<CACHE, D, RT, P16, MANY> A;
+  typedef Attn<CACHE, D, RT, PAGES, MANY> A;
   typedef typename A::T T;
   __shared__ __align__(16) float rows[kAttnWaves][16][A::STRIDE];
   __shared__ __align__(16) typename A::Frag queries[A::kQShared ? RT * A::KC * 64 : 1];
@@ -936,11 +1007,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnPlan p, int blo
 
 }  // namespace
 
-template <int CACHE, int D, int RT, bool P16, bool MANY>
+template <int CACHE, int D, int RT, int PAGES, bool MANY>
 hipError_t run_attention(const AttnPlan& p, hipStream_t s) {
-  typedef Attn<CACHE, D, RT, P16, MANY> A;
+  typedef Attn<CACHE, D, RT, PAGES, MANY> A;
   const int64_t groups = (int64_t)(p.workers ? p.workers : p.items) * p.c.kv_heads;
-  launch_k(attention_kernel<CACHE, D, RT, P16, MANY>, dim3((unsigned)groups), 64 * kAttnWaves, 0, s, p);
+  launch_k(attention_kernel<CACHE, D, RT, PAGES, MANY>, dim3((unsigned)groups), 64 * kAttnWaves, 0, s, p);
   if (p.workers) {
     const int nrows = p.rows < A::R ? p.rows : A::R, blocks = (nrows + 3) / 4;
     launch_k(attention_join_kernel<typename A::T, D, A::R, A::TILE>,
