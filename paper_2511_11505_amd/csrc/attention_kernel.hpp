@@ -102,12 +102,12 @@ struct Item {
   int first, tiles;        // tiles of TILE tokens, at least one
 };
 template <int TILE, int R>
-__device__ __forceinline__ Item item_of(const AttnPlan& p, int item) {
+__device__ __forceinline__ Item item_of(const AttnPlan& p, int item, int length) {
   Item t;
   t.seq = p.row_groups == 1 ? item : item / p.row_groups;
   t.row0 = p.row_groups == 1 ? 0 : (item - t.seq * p.row_groups) * R;
   t.nrows = min(R, p.rows - t.row0);
-  t.len = min(max(p.a.lengths[t.seq], 0), p.c.max_pages * p.c.page_size);
+  t.len = min(max(length, 0), p.c.max_pages * p.c.page_size);
   int i0 = 0, i1 = p.a.n_new - 1;
   if (p.row_groups > 1) i0 = t.row0 / p.group, i1 = (t.row0 + t.nrows - 1) / p.group;
   const int at0 = t.len - p.a.n_new + i0, at1 = t.len - p.a.n_new + i1;
@@ -120,6 +120,11 @@ __device__ __forceinline__ Item item_of(const AttnPlan& p, int item) {
     t.tiles = (t.hi + TILE - 1) / TILE - t.first;
   }
   return t;
+}
+
+template <int TILE, int R>
+__device__ __forceinline__ Item item_of(const AttnPlan& p, int item) {
+  return item_of<TILE, R>(p, item, p.a.lengths[p.row_groups == 1 ? item : item / p.row_groups]);
 }
 
 template <int CACHE, int D, int RT, int PAGES, bool MANY>
@@ -844,7 +849,25 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
   int64_t at = 0, total = 0, left;     // tile `at` of the item; tiles left of this part
   int64_t part0 = 0;
   int parts = 0;
-  if (p.workers) {
+  int length = 0;      // of lane i's sequence, where there are at most 64 items of one row group
+  const bool few = p.items <= 64 && p.row_groups == 1;
+  if (p.workers && few) {
+    if (lane < p.items) length = p.a.lengths[lane];
+    const int64_t mine = lane < p.items ? item_of<A::TILE, A::R>(p, lane, length).tiles : 0;
+    int64_t incl = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t v = shfl_i64(incl, lane - d < 0 ? lane : lane - d);
+      if (lane >= d) incl += v;
+    }
+    total = lane_i64(incl, 63);
+    parts = (int)min((int64_t)p.workers, (total + kAttnMinTiles - 1) / kAttnMinTiles);
+    if (worker >= parts) return;
+    part0 = worker * total / parts;
+    left = (worker + 1) * total / parts - part0;
+    item = __builtin_ctzll(__ballot(part0 < incl));
+    at = part0 - lane_i64(incl - mine, item);
+  } else if (p.workers) {
     // tiles before each thread's items
     const int per = (p.items + 255) / 256, i0 = min(tid * per, p.items), i1 = min(i0 + per, p.items);
     int64_t mine = 0;
@@ -887,7 +910,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
 
   A s(p, lane, head, queries);
   while (left > 0) {
-    const Item it = item_of<A::TILE, A::R>(p, item);
+    const Item it = p.workers && few ? item_of<A::TILE, A::R>(p, item, lane_i(length, item)) : item_of<A::TILE, A::R>(p, item);
     const int from = (int)at;
     const int n = p.workers ? (int)min((int64_t)(it.tiles - from), left) : it.tiles;
     const bool whole = n == it.tiles;
@@ -960,49 +983,76 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
   }
 }
 
-// Rows of items that several parts hold: a wave a row, the parts in their order.
-template <typename T, int D, int R, int TILE>
+// Rows of items that several parts hold: a wave a row.  64 / (D / 4) of its lanes
+// have the same columns and take every so manyth part, four at once (the loads do
+// not wait for one another); their sums are added in a fixed order.
+template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnPlan p, int blocks) {
+  constexpr int LANES = D / 4, SETS = 64 / LANES, BATCH = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t id = blockIdx.x;
   const int row = (int)(id % blocks) * 4 + wave;
   const int head = (int)(id / blocks % p.c.kv_heads), item = (int)(id / blocks / p.c.kv_heads);
+  const int seq = item / p.row_groups, row0 = (item - seq * p.row_groups) * R;
+  if (row >= min(R, p.rows - row0)) return;
   const int2 span = p.span[item];
   if (span.x == span.y) return;
-  const Item it = item_of<TILE, R>(p, item);
-  if (row >= it.nrows) return;
-  // the statistics, a lane a part
-  const int n = span.y - span.x + 1;
-  auto index = [&](int i) {
-    return (((int64_t)(span.x + i) * p.c.kv_heads + head) * 2 + (i == 0 ? 1 : 0)) * R + row;
-  };
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, p.stat[index(i)].x);
-  m = wave_max(m);
-  constexpr int N = D / 64;
-  float o[N], sum = 0.f;
+  const int n = span.y - span.x + 1, set = lane / LANES, col = lane % LANES * 4;
+  float m = -INFINITY, sum = 0.f;
+  floatx4 o{0.f, 0.f, 0.f, 0.f};
   bool any = false;
+  for (int i0 = 0; i0 < n; i0 += SETS * BATCH) {
+    float2 st[BATCH];
+    floatx4 v[BATCH];
 #pragma unroll
-  for (int c = 0; c < N; ++c) o[c] = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const int64_t r = index(i);
-    const float2 st = p.stat[r];
-    const float e = st.x == -INFINITY ? 0.f : exp2_hw(st.x - m);
-    any |= !(st.y < 0.f);
-    sum += st.y < 0.f ? 0.f : e * st.y;
+    for (int j = 0; j < BATCH; ++j) {
+      const int i = i0 + j * SETS + set;
+      st[j] = make_float2(-INFINITY, -1.f), v[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (i < n) {
+        const int64_t r = (((int64_t)(span.x + i) * p.c.kv_heads + head) * 2 + (i == 0 ? 1 : 0)) * R + row;
+        st[j] = p.stat[r];
+        v[j] = *reinterpret_cast<const floatx4*>(p.part + r * D + col);
+      }
+    }
+    float top = m;
 #pragma unroll
-    for (int c = 0; c < N; ++c) o[c] += e * p.part[r * D + lane * N + c];
+    for (int j = 0; j < BATCH; ++j) top = fmaxf(top, st[j].x);
+    const float keep = m == -INFINITY ? 0.f : exp2_hw(m - top);
+    sum *= keep, o *= keep, m = top;
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const float e = st[j].x == -INFINITY ? 0.f : exp2_hw(st[j].x - m);
+      any |= !(st[j].y < 0.f);
+      sum += st[j].y < 0.f ? 0.f : e * st[j].y;
+      o += e * v[j];
+    }
+  }
+#pragma unroll
+  for (int d = LANES; d < 64; d *= 2) {
+    const float m2 = __shfl_xor(m, d), top = fmaxf(m, m2);
+    const float a = m == -INFINITY ? 0.f : exp2_hw(m - top), b = m2 == -INFINITY ? 0.f : exp2_hw(m2 - top);
+    // (both sides add the lower set's first)
+    const float s2 = __shfl_xor(sum, d);
+    const bool low = !(lane & d);
+    sum = low ? a * sum + b * s2 : b * s2 + a * sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float o2 = __shfl_xor(o[j], d);
+      o[j] = low ? a * o[j] + b * o2 : b * o2 + a * o[j];
+    }
+    any |= __shfl_xor((int)any, d) != 0;
+    m = top;
   }
   if (!any) sum = -1.f;
-  const int q = it.row0 + row, i = q / p.group, h = head * p.group + q - i * p.group;
-  const int64_t tok = (int64_t)it.seq * p.a.n_new + i;
+  const int q = row0 + row, i = q / p.group, h = head * p.group + q - i * p.group;
+  const int64_t tok = (int64_t)seq * p.a.n_new + i;
   if (lane == 0 && p.a.lse)
     p.a.lse[tok * p.a.q_heads + h] = sum < 0.f ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
+  if (set || col >= p.c.d) return;
+  T out[4];
 #pragma unroll
-  for (int c = 0; c < N; ++c)
-    if (lane * N + c < p.c.d)
-      ((T*)p.a.out.p)[tok * p.a.out.ts + h * p.a.out.hs + lane * N + c] = from_f32<T>(sum < 0.f ? 0.f : o[c] / sum);
+  for (int j = 0; j < 4; ++j) out[j] = from_f32<T>(sum < 0.f ? 0.f : o[j] / sum);
+  memcpy((T*)p.a.out.p + tok * p.a.out.ts + h * p.a.out.hs + col, out, sizeof(out));
 }
 
 }  // namespace
@@ -1014,7 +1064,7 @@ hipError_t run_attention(const AttnPlan& p, hipStream_t s) {
   launch_k(attention_kernel<CACHE, D, RT, PAGES, MANY>, dim3((unsigned)groups), 64 * kAttnWaves, 0, s, p);
   if (p.workers) {
     const int nrows = p.rows < A::R ? p.rows : A::R, blocks = (nrows + 3) / 4;
-    launch_k(attention_join_kernel<typename A::T, D, A::R, A::TILE>,
+    launch_k(attention_join_kernel<typename A::T, D, A::R>,
              dim3((unsigned)((int64_t)p.items * p.c.kv_heads * blocks)), 256, 0, s, p, blocks);
   }
   return hipGetLastError();
