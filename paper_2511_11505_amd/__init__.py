@@ -7,11 +7,13 @@ replicated-activation inference variant, the local rows, the gathered
 expert GEMMs, the partial Combine and the all-reduce stand-in.  Beside it
 stand the operators of the dense sublayer in the far-skip window, with their
 backward passes: the linear with its epilogue, the norm with the deferred
-add, and 8-bit checkpoints of activations.  This package
+add, and 8-bit checkpoints of activations; and those of the attention
+sublayer: rotary positions with their backward pass, the append to a paged
+key-value cache, and the attention of new tokens over it.  This package
 is its ctypes binding plus small owners of device buffers that order the
 calls: one block (block.py), stacked layers in the two-window schedule
-(stack.py), stacked replicated-activation layers (replicated.py) and the
-dense sublayer (sublayer.py).
+(stack.py), stacked replicated-activation layers (replicated.py), the
+dense sublayer (sublayer.py) and the attention sublayer (attention.py).
 """
 
 from . import _lib  # noqa: F401
@@ -38,3 +40,4 @@ from ._lib import (  # noqa: F401
     fs_rotary, fs_rotary_backward, fs_cache_append, fs_paged_attention_workspace, fs_paged_attention,
 )
 from .sublayer import DenseSublayer, checkpoint_buffers, linear_desc, norm_desc  # noqa: F401
+from .attention import AttentionSublayer, empty_cache  # noqa: F401

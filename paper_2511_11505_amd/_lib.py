@@ -718,6 +718,8 @@ def fs_rotary_backward(desc, rope, dout, positions, dx, stream=None):
 def fs_cache_append(cache, rope, q, k, v, seqs, positions, pages, q_out, stream=None):
     """q, q_out [tokens, q_heads, head_dim] or None; k, v [tokens, kv_heads,
     head_dim]; seqs [tokens] or None, positions [tokens] int32."""
+    if k is None:
+        _bad("k", "a tensor")
     dev, s = _here(stream)
     elem, d, n = _ELEM.get(cache.dtype), cache.head_dim, k.shape[0]
     rows, kv = (n, 0 if q is None else q.shape[1], d), (n, cache.kv_heads, d)

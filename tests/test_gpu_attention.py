@@ -469,3 +469,297 @@ def test_attention_scales():
     for scale in (0.0, -0.5, 40.0):
         check_attention("f32", 4, 2, 64, [5, 70, 33], 16, scale=scale)
         check_attention("bf16", 4, 2, 64, [5, 70, 33], 16, scale=scale)
+
+
+# ------------------------------------------- what does not reach, and what does
+def place_of(table, size, b, j):
+    return int(table[b, j // size]), j % size
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [16, 5])
+def test_attention_values_that_are_not_finite(kind, size):
+    """An infinite or NaN value reaches the queries that see it, in its column (in
+    its block of a coded cache), and no other."""
+    dtype, codes = kind.split()[0], "codes" in kind
+    for window in (0, 6):
+        g = gen(21)
+        lens, new, d = [40, 9], 5, 64
+        table, pages = pages_of(g, lens, size)
+        cache = Cache(g, pages, 2, size, d, dtype, codes)
+        q = heads(g, len(lens) * new, 6, d, dtype)
+        desc = fs.attention_desc(6, new, d ** -0.5, window)
+        ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, table) + 256,), dtype=torch.uint8, device=DEV)
+        lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        bad = [(0, 38, 0, 3, float("nan")), (0, 37, 1, 40, float("inf")), (1, 8, 0, 63, float("-inf")),
+               (1, 2, 1, 0, float("inf"))]
+        for b, j, h, c, value in bad:
+            pg, pl = place_of(table, size, b, j)
+            if codes:
+                cache.v[pg, h, pl, c // 32 * 32:c // 32 * 32 + 32] = 0x7F
+                cache.vs[pg, h, pl, c // 32] = 255
+            else:
+                cache.v[pg, h, pl, c] = value
+        out = Out(len(lens) * new, 6, d, dtype)
+        fs.fs_paged_attention(desc, cache.struct, q, lengths, table, out.view, ws)
+        torch.cuda.synchronize()
+        got = out.get()
+        want = np.zeros(got.shape)
+        for b, j, h, c, value in bad:
+            for i in range(new):
+                at = lens[b] - new + i
+                if j <= at and (not window or j > at - window):
+                    cols = slice(c // 32 * 32, c // 32 * 32 + 32) if codes else c
+                    want[b * new + i, h * 3:h * 3 + 3, cols] = np.nan if codes else value
+        assert np.array_equal(np.isnan(got), np.isnan(want)), np.argwhere(np.isnan(got) != np.isnan(want))[:5]
+        assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)]) and not np.isinf(got[~np.isinf(want)]).any()
+
+
+def test_attention_scores_that_are_not_finite():
+    """As the formula has them: a key of minus infinity has no weight, a row of
+    nothing else is 0 / 0, a NaN or plus infinity makes NaNs."""
+    g = gen(22)
+    table, pages = pages_of(g, [20, 3], 16)
+    for dtype in ("bf16", "f32"):
+        cache = Cache(g, pages, 4, 16, 64, dtype)
+        q = heads(g, 2, 4, 64, dtype)
+        q[:, :, 0] = 1.0
+        pg, pl = place_of(table, 16, 0, 7)
+        cache.k[pg, 0, pl, 0] = float("-inf")
+        cache.k[pg, 1, pl, 0] = float("inf")
+        cache.k[pg, 2, pl, 5] = float("nan")
+        for j in range(3):
+            a, b = place_of(table, 16, 1, j)
+            cache.k[a, 0, b, 0] = float("-inf")
+        out, lse = torch.empty((2, 4, 64), dtype=TORCH[dtype], device=DEV), torch.empty((2, 4), device=DEV)
+        lengths = torch.tensor([20, 3], dtype=torch.int32, device=DEV)
+        fs.fs_paged_attention(fs.attention_desc(4, 1, 0.125), cache.struct, q, lengths, table, out, None, lse=lse)
+        torch.cuda.synchronize()
+        nan = torch.isnan(out).all(2).tolist()
+        assert nan == [[False, True, True, False], [True, False, False, False]]
+        assert torch.isfinite(out[0, 0]).all() and torch.isfinite(out[0, 3]).all()
+        assert torch.isnan(lse[0, 1:3]).all() and lse[1, 0] == float("-inf") and torch.isfinite(lse[0, 0])
+
+
+def test_attention_lowest_values():
+    """Scores at the type's lowest value: finite, and even ones share their weight."""
+    low = torch.finfo(torch.float32).min
+    table = torch.tensor([[0]], dtype=torch.int32, device=DEV)
+    k, v = torch.zeros((1, 1, 16, 64), device=DEV), torch.randn((1, 1, 16, 64), generator=gen(1), device=DEV)
+    k[0, 0, :, 0] = low
+    q = torch.zeros((1, 1, 64), device=DEV)
+    q[..., 0] = 1.0
+    out, lse = torch.empty((1, 1, 64), device=DEV), torch.empty((1, 1), device=DEV)
+    lengths = torch.tensor([16], dtype=torch.int32, device=DEV)
+    fs.fs_paged_attention(fs.attention_desc(1, 1, 0.5), fs.kv_cache(k, v), q, lengths, table, out, None, lse=lse)
+    torch.cuda.synchronize()
+    near(f64(out)[0, 0], f64(v)[0, 0].mean(0), 32 * 2.0 ** -24 * np.abs(f64(v)[0, 0]).mean(0))
+
+
+# ------------------------------------------------ far places, streams, graphs
+@pytest.mark.parametrize("kind", ["bf16", "bf16 codes"])
+def test_places_past_32_bits(kind):
+    """Pages whose elements lie behind 2^32, of a cache that is mostly not touched."""
+    dtype, codes = kind.split()[0], "codes" in kind
+    kv, size, d = 8, 64, 128
+    pages = (1 << 32) // (kv * size * d) + 40
+    dt = torch.uint8 if codes else TORCH[dtype]
+    k, v = (torch.empty((pages, kv, size, d), dtype=dt, device=DEV) for _ in range(2))
+    scales = [torch.empty((pages, kv, size, 4), dtype=torch.uint8, device=DEV) for _ in range(2)] if codes else []
+    cache = fs.kv_cache(k, v, *scales, dtype=dtype)
+    g = gen(31)
+    n = 300
+    far = pages - 1 - torch.arange(5, dtype=torch.int32, device=DEV)[None]
+    rows = [heads(g, n, kv, d, dtype) for _ in range(2)]
+    pos, seqs = torch.arange(n, dtype=torch.int32, device=DEV), torch.zeros((n,), dtype=torch.int32, device=DEV)
+    fs.fs_cache_append(cache, None, None, *rows, seqs, pos, far, None)
+    q, lengths = heads(g, 1, 16, d, dtype), torch.tensor([n], dtype=torch.int32, device=DEV)
+    out = torch.empty((1, 16, d), dtype=TORCH[dtype], device=DEV)
+    desc = fs.attention_desc(16, 1, 0.1)
+    ws = torch.empty((max(256, fs.fs_paged_attention_workspace(desc, cache, far)),), dtype=torch.uint8, device=DEV)
+    fs.fs_paged_attention(desc, cache, q, lengths, far, out, ws)
+    # the same in a cache of five pages
+    near5 = torch.arange(4, -1, -1, dtype=torch.int32, device=DEV)[None]
+    small = Cache(g, 5, kv, size, d, dtype, codes)
+    fs.fs_cache_append(small.struct, None, None, *rows, seqs, pos, near5, None)
+    out2 = torch.empty_like(out)
+    fs.fs_paged_attention(desc, small.struct, q, lengths, near5, out2, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(k[-5:][:, :, :n % 64], small.k[:, :, :n % 64])
+    assert torch.equal(out, out2) and bool(torch.isfinite(out).all())
+
+
+def serving(g, sequences=6, pages=40, dtype="bf16", codes=False, new=1, rope_layout="halves", d=96, hd=32, h=6, kv=2,
+            size=8, window=0):
+    """An attention sublayer, its cache and page table."""
+    def w(m, n):
+        return (torch.randn((m, n), generator=g, device=DEV) * n ** -0.5).to(TORCH[dtype])
+
+    cache = fs.empty_cache(pages, size, kv, hd, dtype, codes)
+    for t in cache.tensors:
+        if t is not None:
+            t.fill_(0x7F if t.dtype == torch.uint8 else float("nan"))
+    freqs = fs.fs_rope_frequencies(hd).to(DEV)
+    params = [1 + 0.1 * torch.randn((d,), generator=g, device=DEV), None, w((h + 2 * kv) * hd, d),
+              0.1 * torch.randn(((h + 2 * kv) * hd,), generator=g, device=DEV), w(d, h * hd), None]
+    table = torch.randperm(pages, generator=g, device=DEV).int()[:sequences * (pages // sequences)].view(sequences, -1)
+    sub = fs.AttentionSublayer(sequences, cache, table.shape[1], *params, rope=fs.rope(freqs, rope_layout),
+                               new_tokens=new, window=window)
+    return sub, params, table, freqs
+
+
+@pytest.mark.parametrize("window", [0, 5])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "bf16 codes"])
+def test_sublayer(kind, window):
+    """Tokens one after another, and several at once, through the sublayer: each
+    pass's parts from what the part before it left, and the cache they left."""
+    dtype, codes = kind.split()[0], "codes" in kind
+    g = gen(41)
+    B, d, hd, h, kv, size = 6, 96, 32, 6, 2, 8
+    for new in (1, 4):
+        sub, params, table, freqs = serving(g, B, 40, dtype, codes, new, window=window)
+        tb = table.cpu().numpy()
+        lens = np.array([0, 3, 0, 7, 1, 20])
+        keys = {}
+        for step in range(5):
+            lens = lens + new
+            lens[2] = 0                          # a sequence that is idle
+            pos = (lens[:, None] - new + np.arange(new)).reshape(-1)
+            pos[pos < 0] = -1
+            x = torch.randn((B * new, d), generator=g, device=DEV).to(TORCH[dtype])
+            out = torch.empty_like(x)
+            lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+            if step == 0:                        # what came before this test's tokens
+                for b in range(B):
+                    n = int(lens[b]) - new
+                    if n > 0:
+                        rows = [heads(g, n, kv, hd, dtype) for _ in range(2)]
+                        fs.fs_cache_append(sub.cache, None, None, *rows, torch.full((n,), b, dtype=torch.int32, device=DEV),
+                                           torch.arange(n, dtype=torch.int32, device=DEV), table, None)
+            sub.forward(x, out, torch.tensor(pos, dtype=torch.int32, device=DEV), lengths, table)
+            torch.cuda.synchronize()
+            qkv, q, o = (f64(t) for t in sub.heads)
+            # the rotation
+            live = pos >= 0
+            want = O.rotary(qkv[:, :h], pos, freqs.cpu().numpy())
+            tol = turn_tol(qkv[:, :h], freqs, "halves", 0, 1.0, want, dtype)
+            near(q[live], want[live], tol[live])
+            assert (q[~live] == 0).all()
+            # the cache's new rows
+            k, v, *sc = sub.cache.tensors
+            kk, vv = ((f64(k), f64(v)) if not codes else
+                      tuple(O.decoded(a.cpu().numpy(), b.cpu().numpy()) for a, b in zip((k, v), sc)))
+            tk = O.rotary(qkv[:, h:h + kv], pos, freqs.cpu().numpy())
+            tv = qkv[:, h + kv:]
+            for t in np.flatnonzero(live):
+                pg, pl = O.place(tb, 40, size, t // new, pos[t])
+                if codes:
+                    assert np.array_equal(vv[pg, :, pl], O.decoded(*O.coded(tv[t])))
+                    assert np.abs(kk[pg, :, pl] - tk[t]).max() <= 2.0 ** -4 * np.abs(tk[t]).max() * (1 + 1e-6)
+                else:
+                    assert np.array_equal(vv[pg, :, pl], tv[t])
+                    near(kk[pg, :, pl], tk[t], turn_tol(qkv[t, h:h + kv], freqs, "halves", 0, 1.0, tk[t], dtype))
+                keys[(t // new, int(pos[t]))] = kk[pg, :, pl].copy()
+            for (b, p), row in keys.items():     # those of earlier passes are still there
+                pg, pl = O.place(tb, 40, size, b, p)
+                assert np.array_equal(kk[pg, :, pl], row)
+            # the attention, and the linear with the residual
+            want, _, mass, reach = O.attention(q, kk, vv, lens, tb, new, float(np.float32(hd ** -0.5)), window)
+            err = np.expm1((hd + 2) * U * reach) + 2.0 ** -21 + 40 * 2.0 ** -24 + 2.0 ** -20
+            tol = (2 * (err + (2.0 ** -8 if dtype == "bf16" else 0)))[..., None] * mass
+            near(o, want, tol + HALF[dtype] * (np.abs(want) + tol))
+            W, flat = f64(params[4]), o.reshape(B * new, -1)
+            want = f64(x) + flat @ W.T
+            tol = (h * hd + 2) * U * (np.abs(flat) @ np.abs(W).T + np.abs(f64(x)))
+            near(f64(out), want, tol + HALF[dtype] * (np.abs(want) + tol))
+
+
+def test_sublayer_one_by_one_and_at_once():
+    """Four tokens in one pass and one after another: in fp32 the same values to the
+    roundings of sums in another order (a row of 96 or 192 terms, four times)."""
+    g = gen(43)
+    one, _, table, _ = serving(g, 6, 40, "f32")
+    g = gen(43)
+    four, _, table4, _ = serving(g, 6, 40, "f32", new=4)
+    assert torch.equal(table, table4)
+    x = torch.randn((6, 4, 96), generator=gen(44), device=DEV)
+    out, outs = torch.empty((24, 96), device=DEV), []
+    pos = torch.arange(4, dtype=torch.int32, device=DEV).repeat(6)
+    four.forward(x.view(24, 96), out, pos, torch.full((6,), 4, dtype=torch.int32, device=DEV), table)
+    for i in range(4):
+        y = torch.empty((6, 96), device=DEV)
+        one.forward(x[:, i].contiguous(), y, torch.full((6,), i, dtype=torch.int32, device=DEV),
+                    torch.full((6,), i + 1, dtype=torch.int32, device=DEV), table)
+        outs.append(y)
+    torch.cuda.synchronize()
+    want = torch.stack(outs, 1).view(24, 96)
+    assert (out - want).norm() <= 4 * 192 * 2.0 ** -24 * want.norm()
+
+
+def test_graph():
+    """A captured step replayed, with eager work and synchronizations between,
+    while lengths, positions and inputs change where they are."""
+    g = gen(51)
+    for new, codes in ((1, False), (3, True)):
+        sub, _, table, _ = serving(g, 6, 60, "bf16", codes, new)
+        for t in sub.cache.tensors:          # (tokens that no step here writes)
+            if t is not None:
+                t.fill_(0x38) if codes else t.normal_(generator=g)
+        x, out = torch.empty((6 * new, 96), dtype=torch.bfloat16, device=DEV), torch.empty((6 * new, 96), dtype=torch.bfloat16, device=DEV)
+        pos, lengths = torch.zeros((6 * new,), dtype=torch.int32, device=DEV), torch.zeros((6,), dtype=torch.int32, device=DEV)
+
+        def step(n):
+            x.normal_(generator=g)
+            lengths.fill_(n)
+            pos.copy_((n - new + torch.arange(new, device=DEV, dtype=torch.int32)).repeat(6))
+
+        step(new)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            sub.forward(x, out, pos, lengths, table)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            sub.forward(x, out, pos, lengths, table)
+        for n in (new, 2 * new, 9 + new, 70, 71):
+            step(n)
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            out.zero_()
+            kept = [t.clone() for t in sub.cache.tensors if t is not None]
+            sub.forward(x, out, pos, lengths, table)
+            torch.cuda.synchronize()
+            assert torch.equal(got, out)
+            assert all(torch.equal(a, b) for a, b in zip(kept, [t for t in sub.cache.tensors if t is not None]))
+
+
+def test_two_streams():
+    """Calls at the same time on two streams, a workspace each."""
+    g = gen(61)
+    sets = []
+    for seed in (1, 2):
+        table, pages = pages_of(g, [900, 33, 2000], 16)
+        cache = Cache(g, pages, 2, 16, 128, "bf16", codes=seed == 2)
+        q = heads(g, 3, 8, 128, "bf16")
+        desc = fs.attention_desc(8, 1, 0.1)
+        ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, table),), dtype=torch.uint8, device=DEV)
+        sets.append((desc, cache, q, torch.tensor([900, 33, 2000], dtype=torch.int32, device=DEV), table, ws))
+    want, got = [], []
+    for desc, cache, q, lengths, table, ws in sets:
+        out = torch.empty((3, 8, 128), dtype=torch.bfloat16, device=DEV)
+        fs.fs_paged_attention(desc, cache.struct, q, lengths, table, out, ws)
+        want.append(out)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for s, (desc, cache, q, lengths, table, ws) in zip(streams, sets):
+        outs = [torch.zeros((3, 8, 128), dtype=torch.bfloat16, device=DEV) for _ in range(8)]
+        s.wait_stream(torch.cuda.current_stream())
+        for out in outs:
+            fs.fs_paged_attention(desc, cache.struct, q, lengths, table, out, ws, stream=s)
+        got.append(outs)
+    torch.cuda.synchronize()
+    for w, outs in zip(want, got):
+        assert all(torch.equal(w, o) for o in outs)
