@@ -983,24 +983,36 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
   }
 }
 
-// Rows of items that several parts hold: a wave a row.  64 / (D / 4) of its lanes
-// have the same columns and take every so manyth part, four at once (the loads do
-// not wait for one another); their sums are added in a fixed order.
-template <typename T, int D, int R>
+// A sum over parts: m, l (with `any` of them), o.
+struct Sum {
+  float m, l;
+  floatx4 o;
+  bool any;
+  __device__ __forceinline__ void add(float m2, float l2, floatx4 o2, bool any2) {
+    const float top = fmaxf(m, m2);
+    const float a = m == -INFINITY ? 0.f : exp2_hw(m - top), b = m2 == -INFINITY ? 0.f : exp2_hw(m2 - top);
+    l = a * l + b * l2, o = a * o + b * o2, m = top, any |= any2;
+  }
+};
+
+// Rows of items that several parts hold, ROWS to a workgroup: four, a wave each,
+// or one where there are many parts to an item.  A row's columns are D / 4 lanes;
+// so many sets of them take the parts in turn, four at once (the loads do not
+// wait for one another); the sets are added in a fixed order.
+template <typename T, int D, int R, int ROWS>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnPlan p, int blocks) {
-  constexpr int LANES = D / 4, SETS = 64 / LANES, BATCH = 4;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int LANES = D / 4, SETS = 256 / ROWS / LANES, BATCH = 4;
+  __shared__ float4 sums[ROWS][SETS][LANES];
+  __shared__ float3 stats[ROWS][SETS];
   const int64_t id = blockIdx.x;
-  const int row = (int)(id % blocks) * 4 + wave;
+  const int sub = threadIdx.x / (256 / ROWS), row = (int)(id % blocks) * ROWS + sub;
   const int head = (int)(id / blocks % p.c.kv_heads), item = (int)(id / blocks / p.c.kv_heads);
-  const int seq = item / p.row_groups, row0 = (item - seq * p.row_groups) * R;
-  if (row >= min(R, p.rows - row0)) return;
+  const int seq = p.row_groups == 1 ? item : item / p.row_groups, row0 = (item - seq * p.row_groups) * R;
   const int2 span = p.span[item];
   if (span.x == span.y) return;
-  const int n = span.y - span.x + 1, set = lane / LANES, col = lane % LANES * 4;
-  float m = -INFINITY, sum = 0.f;
-  floatx4 o{0.f, 0.f, 0.f, 0.f};
-  bool any = false;
+  const int n = row < min(R, p.rows - row0) ? span.y - span.x + 1 : 0;
+  const int set = threadIdx.x % (256 / ROWS) / LANES, lane = threadIdx.x % LANES, col = lane * 4;
+  Sum s{-INFINITY, 0.f, floatx4{0.f, 0.f, 0.f, 0.f}, false};
   for (int i0 = 0; i0 < n; i0 += SETS * BATCH) {
     float2 st[BATCH];
     floatx4 v[BATCH];
@@ -1014,44 +1026,30 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnPlan p, int blo
         v[j] = *reinterpret_cast<const floatx4*>(p.part + r * D + col);
       }
     }
-    float top = m;
-#pragma unroll
-    for (int j = 0; j < BATCH; ++j) top = fmaxf(top, st[j].x);
-    const float keep = m == -INFINITY ? 0.f : exp2_hw(m - top);
-    sum *= keep, o *= keep, m = top;
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
-      const float e = st[j].x == -INFINITY ? 0.f : exp2_hw(st[j].x - m);
-      any |= !(st[j].y < 0.f);
-      sum += st[j].y < 0.f ? 0.f : e * st[j].y;
-      o += e * v[j];
+      const bool none = st[j].y < 0.f;
+      s.add(st[j].x, none ? 0.f : st[j].y, v[j], !none);
     }
   }
-#pragma unroll
-  for (int d = LANES; d < 64; d *= 2) {
-    const float m2 = __shfl_xor(m, d), top = fmaxf(m, m2);
-    const float a = m == -INFINITY ? 0.f : exp2_hw(m - top), b = m2 == -INFINITY ? 0.f : exp2_hw(m2 - top);
-    // (both sides add the lower set's first)
-    const float s2 = __shfl_xor(sum, d);
-    const bool low = !(lane & d);
-    sum = low ? a * sum + b * s2 : b * s2 + a * sum;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float o2 = __shfl_xor(o[j], d);
-      o[j] = low ? a * o[j] + b * o2 : b * o2 + a * o[j];
-    }
-    any |= __shfl_xor((int)any, d) != 0;
-    m = top;
+  const int sets = min(SETS, n);
+  if (set > 0 && set < sets) {
+    sums[sub][set][lane] = make_float4(s.o[0], s.o[1], s.o[2], s.o[3]);
+    if (lane == 0) stats[sub][set] = make_float3(s.m, s.l, s.any ? 1.f : 0.f);
   }
-  if (!any) sum = -1.f;
+  __syncthreads();
+  if (set > 0 || col >= p.c.d || n == 0) return;
+  for (int i = 1; i < sets; ++i) {
+    const float4 o = sums[sub][i][lane];
+    s.add(stats[sub][i].x, stats[sub][i].y, floatx4{o.x, o.y, o.z, o.w}, stats[sub][i].z > 0.f);
+  }
   const int q = row0 + row, i = q / p.group, h = head * p.group + q - i * p.group;
   const int64_t tok = (int64_t)seq * p.a.n_new + i;
   if (lane == 0 && p.a.lse)
-    p.a.lse[tok * p.a.q_heads + h] = sum < 0.f ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
-  if (set || col >= p.c.d) return;
+    p.a.lse[tok * p.a.q_heads + h] = s.any ? (s.m + __log2f(s.l)) * 0.69314718055994531f : -INFINITY;
   T out[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) out[j] = from_f32<T>(sum < 0.f ? 0.f : o[j] / sum);
+  for (int j = 0; j < 4; ++j) out[j] = from_f32<T>(s.any ? s.o[j] / s.l : 0.f);
   memcpy((T*)p.a.out.p + tok * p.a.out.ts + h * p.a.out.hs + col, out, sizeof(out));
 }
 
@@ -1063,9 +1061,15 @@ hipError_t run_attention(const AttnPlan& p, hipStream_t s) {
   const int64_t groups = (int64_t)(p.workers ? p.workers : p.items) * p.c.kv_heads;
   launch_k(attention_kernel<CACHE, D, RT, PAGES, MANY>, dim3((unsigned)groups), 64 * kAttnWaves, 0, s, p);
   if (p.workers) {
-    const int nrows = p.rows < A::R ? p.rows : A::R, blocks = (nrows + 3) / 4;
-    launch_k(attention_join_kernel<typename A::T, D, A::R>,
-             dim3((unsigned)((int64_t)p.items * p.c.kv_heads * blocks)), 256, 0, s, p, blocks);
+    const int nrows = p.rows < A::R ? p.rows : A::R;
+    auto join = [&](auto kernel, int rows) {
+      const int blocks = (nrows + rows - 1) / rows;
+      launch_k(kernel, dim3((unsigned)((int64_t)p.items * p.c.kv_heads * blocks)), 256, 0, s, p, blocks);
+    };
+    // (512 parts of one item, 8 rows: 15 us with a row a workgroup, 45 with four; 32
+    // items of two or three parts, 32 rows, 8 heads: 6 us with four, 13 with one)
+    if (p.workers > 8 * p.items) join(attention_join_kernel<typename A::T, D, A::R, 1>, 1);
+    else join(attention_join_kernel<typename A::T, D, A::R, 4>, 4);
   }
   return hipGetLastError();
 }

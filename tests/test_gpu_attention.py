@@ -541,6 +541,34 @@ def test_attention_scores_that_are_not_finite():
         assert torch.isnan(lse[0, 1:3]).all() and lse[1, 0] == float("-inf") and torch.isfinite(lse[0, 0])
 
 
+@pytest.mark.parametrize("lens", [[2500], [2500] + [40] * 70])
+def test_attention_scores_that_are_not_finite_divided(lens):
+    """The same where a sequence is in several parts: a NaN in one of them reaches
+    its row, keys of minus infinity have no weight."""
+    g = gen(23)
+    table, pages = pages_of(g, lens, 16)
+    cache = Cache(g, pages, 4, 16, 64, "bf16")
+    q = heads(g, len(lens), 4, 64, "bf16")
+    q[:, :, 0] = 1.0
+    for j in range(1200):
+        a, b = place_of(table, 16, 0, j)
+        cache.k[a, 0, b, 0] = float("-inf")
+    for h, j, value in ((1, 1300, "nan"), (2, 60, "inf")):
+        a, b = place_of(table, 16, 0, j)
+        cache.k[a, h, b, 0] = float(value)
+    out, lse = torch.empty((len(lens), 4, 64), dtype=torch.bfloat16, device=DEV), torch.empty((len(lens), 4), device=DEV)
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    desc = fs.attention_desc(4, 1, 0.125)
+    ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, table),), dtype=torch.uint8, device=DEV)
+    fs.fs_paged_attention(desc, cache.struct, q, lengths, table, out, ws, lse=lse)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[0]).all(1).tolist() == [False, True, True, False] and torch.isfinite(out[0, [0, 3]]).all()
+    assert torch.isnan(lse[0]).tolist() == [False, True, True, False] and torch.isfinite(out[1:]).all()
+    k, v = cache.values()
+    want = O.attention(f64(q)[:1, :1], k[:, :1], v[:, :1], lens[:1], table.cpu().numpy()[:1], 1, 0.125)[0]
+    near(f64(out)[:1, :1], want, 2.0 ** -6 * np.abs(v).max())
+
+
 def test_attention_lowest_values():
     """Scores at the type's lowest value: finite, and even ones share their weight."""
     low = torch.finfo(torch.float32).min
