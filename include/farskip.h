@@ -844,7 +844,7 @@ typedef struct {
                           i / (q_heads / kv_heads) */
   int32_t new_tokens;  /* n >= 1: queries of each sequence, its last n tokens */
   int32_t window;      /* 0, or how many tokens a query sees, itself included */
-  float scale;         /* factor of q . k; finite */
+  float scale;         /* factor of q . k; |scale| <= 1e38 */
 } fs_attention_desc;
 
 /* Bytes of workspace of fs_paged_attention; of the page table only the sizes are

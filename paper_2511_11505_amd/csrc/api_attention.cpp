@@ -3,6 +3,7 @@
 // Every check runs on the host before anything is enqueued; no exception
 // leaves an entry.
 
+#include <algorithm>
 #include <cmath>
 #include <utility>
 
@@ -231,10 +232,10 @@ fs_status check_attention(const fs_attention_desc* d, const fs_kv_cache* c, cons
   if ((int64_t)t->sequences * d->new_tokens > kMaxTokens || d->new_tokens > kMaxTokens)
     return fail(FS_ERR_UNSUPPORTED, "sequences * new_tokens must be <= 2^24");
   // (rows of 16 queries of one key head, and a workgroup for each)
-  const int64_t items = (int64_t)t->sequences * (((int64_t)d->new_tokens * (d->q_heads / c->kv_heads) + 15) / 16);
+  const int64_t items = (int64_t)std::max(t->sequences, 1) * (((int64_t)d->new_tokens * (d->q_heads / c->kv_heads) + 15) / 16);
   if (items * c->kv_heads >= ((int64_t)1 << 23))
     return fail(FS_ERR_UNSUPPORTED, "sequences * new_tokens * q_heads: more than 2^23 groups of 16 rows");
-  if (!std::isfinite(d->scale)) return fail(FS_ERR_INVALID, "scale must be finite");
+  if (!(std::fabs(d->scale) <= 1e38f)) return fail(FS_ERR_INVALID, "scale must be within +-1e38");
   return FS_OK;
 }
 

@@ -96,6 +96,8 @@ hipError_t launch_attention(int dtype, const AttnArgs& a, const PagedCache& c, v
   const Shape h = shape_of(dtype, a.q_heads, a.n_new, c);
   AttnPlan p{};
   p.a = a, p.c = c;
+  // (a window as long as the longest sequence hides nothing)
+  if (a.window >= (int64_t)c.max_pages * c.page_size) p.a.window = 0;
   p.group = h.group, p.rows = h.rows, p.row_groups = h.row_groups, p.items = (int)h.items, p.workers = h.workers;
   p.scale2 = (float)(a.scale * M_LOG2E);
   if (h.workers) {

@@ -198,7 +198,7 @@ def _append_c(c, q=None, k=B, v=C, positions=D, out=None, heads=4, tokens=3, str
     (dict(abi_version=8), L.FS_ERR_INVALID), (dict(q_heads=0), L.FS_ERR_INVALID), (dict(q_heads=3), L.FS_ERR_INVALID),
     (dict(q_heads=2 ** 16 + 2), L.FS_ERR_UNSUPPORTED), (dict(new_tokens=0), L.FS_ERR_INVALID),
     (dict(new_tokens=2 ** 24), L.FS_ERR_UNSUPPORTED), (dict(window=-1), L.FS_ERR_INVALID),
-    (dict(scale=NAN), L.FS_ERR_INVALID), (dict(scale=INF), L.FS_ERR_INVALID)])
+    (dict(scale=NAN), L.FS_ERR_INVALID), (dict(scale=INF), L.FS_ERR_INVALID), (dict(scale=-3e38), L.FS_ERR_INVALID)])
 def test_attention_descriptor(kw, status):
     refuse(status, "", fs.fs_paged_attention, attn(**kw), cache(), A, B, pages(), C, WS)
     refuse(status, "", fs.fs_paged_attention_workspace, attn(**kw), cache(), pages())
@@ -230,6 +230,8 @@ def test_many_rows():
     refuse(L.FS_ERR_UNSUPPORTED, "groups of 16 rows", fs.fs_paged_attention_workspace, attn(2 ** 16, new_tokens=2 ** 11), c,
            pages(sequences=2))
     assert fs.fs_paged_attention_workspace(attn(4, new_tokens=2 ** 20), c, pages(sequences=1)) == 0
+    refuse(L.FS_ERR_UNSUPPORTED, "groups of 16 rows", fs.fs_paged_attention_workspace, attn(2 ** 16, new_tokens=2 ** 24), c,
+           pages(sequences=0))
 
 
 def test_binding_checks():

@@ -424,7 +424,7 @@ def test_attention_rows(kind, h, kv, new):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "bf16 codes"])
-@pytest.mark.parametrize("window", [1, 5, 16, 33, 200, 5000])
+@pytest.mark.parametrize("window", [1, 5, 16, 33, 200, 5000, 2 ** 31 - 1])
 @pytest.mark.parametrize("new", [1, 3])
 def test_attention_window(kind, window, new):
     check_attention(kind, 4, 2, 128, LENGTHS["mid"], 16, new=new, window=window)
