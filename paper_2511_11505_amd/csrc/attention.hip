@@ -10,6 +10,11 @@ namespace {
 
 constexpr int kCus = 256;
 constexpr int kMaxGroups = 1 << 16;
+// From here on a wave has a row tile to itself and nothing is joined: a prompt of
+// 2048 tokens of 64 query and 8 key heads 311 us, with four row tiles a workgroup, its
+// waves dividing the tokens, 883 (512 tokens after 3584, two sequences: 543 and 545).
+// Fewer rows read the cache fewer times with four tiles.
+constexpr int kPromptTiles = 16, kPromptWaves = 1024;
 
 int width_of(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
@@ -37,13 +42,18 @@ Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
   h.group = q_heads / c.kv_heads;
   h.rows = n_new * h.group;
   h.rt = row_tiles(dtype, h.width, h.rows);
+  const int tiles = (h.rows + 15) / 16;
+  h.workers = 0;
+  if (n_new > 1 && tiles > kPromptTiles && (int64_t)c.sequences * tiles * c.kv_heads >= kPromptWaves) {
+    h.rt = 1, h.row_groups = tiles, h.items = (int64_t)c.sequences * tiles;
+    return h;
+  }
   h.row_groups = (h.rows + 16 * h.rt - 1) / (16 * h.rt);
   h.items = (int64_t)c.sequences * h.row_groups;
   // A sequence of at most four tiles a wave is not worth a second launch;
   // beyond kAttnMaxItems, or that many workgroups, there is enough to fill the chip.
   const int tile = dtype == 0 ? 16 : 32;
   const int64_t most = ((int64_t)c.max_pages * c.page_size + tile - 1) / tile;
-  h.workers = 0;
   if (h.items <= kAttnMaxItems && h.items * c.kv_heads <= kMaxGroups && most > 4 * kAttnWaves) {
     const int64_t parts = (h.items * most + kAttnMinTiles - 1) / kAttnMinTiles;
     h.workers = (kCus * attn_groups_per_cu(h.width, h.rt) + c.kv_heads - 1) / c.kv_heads;
@@ -57,9 +67,11 @@ int64_t part_rows(const Shape& h, const PagedCache& c) { return (int64_t)h.worke
 
 template <int CACHE, int D, int RT, int PAGES>
 hipError_t run_new(const AttnPlan& p, hipStream_t s) {
-  if constexpr (RT == 1)
-    if (p.a.n_new == 1) return run_attention<CACHE, D, RT, PAGES, false>(p, s);
-  return run_attention<CACHE, D, RT, PAGES, true>(p, s);
+  if constexpr (RT == 1) {
+    if (p.a.n_new == 1) return run_attention<CACHE, D, RT, PAGES, NEW_ONE>(p, s);
+    if (!p.workers && p.row_groups > kPromptTiles) return run_attention<CACHE, D, RT, PAGES, NEW_PROMPT>(p, s);
+  }
+  return run_attention<CACHE, D, RT, PAGES, NEW_SOME>(p, s);
 }
 template <int CACHE, int D, int RT>
 hipError_t run_pages(const AttnPlan& p, hipStream_t s) {

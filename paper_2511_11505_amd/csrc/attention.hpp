@@ -12,6 +12,10 @@ enum { CACHE_BF16 = 0, CACHE_F32 = 1, CACHE_CODES_BF16 = 2, CACHE_CODES_F32 = 3 
 // fewer blocks in a row than the kernel's width has.
 enum { PAGES_ANY = 0, PAGES_GROUPS = 1, PAGES_GROUPS_SHORT = 2 };
 
+// New tokens: one, with rows for one row tile; several; so many (a prompt's) that
+// the rows fill the chip, a wave a row tile.
+enum { NEW_ONE = 0, NEW_SOME = 1, NEW_PROMPT = 2 };
+
 constexpr int kAttnWaves = 4;
 constexpr int kAttnMaxItems = 4096;    // of a divided call: 16 for each thread
 constexpr int kAttnMinTiles = 4;       // of a workgroup's part: one for each wave
@@ -31,8 +35,7 @@ struct AttnPlan {
   int2* span;              // [items]: first and last part
 };
 
-// MANY: more than one new token, or rows for more than one row tile.
-template <int CACHE, int D, int RT, int PAGES, bool MANY>
+template <int CACHE, int D, int RT, int PAGES, int NEW>
 hipError_t run_attention(const AttnPlan& p, hipStream_t s);
 
 }  // namespace fs

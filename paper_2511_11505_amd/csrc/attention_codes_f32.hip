@@ -4,29 +4,38 @@
 
 namespace fs {
 
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_ANY, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS_SHORT, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_ANY, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS_SHORT, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_ANY, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_ANY, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS, true>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS_SHORT, false>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS_SHORT, true>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_ANY, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_ANY, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_ANY, NEW_PROMPT>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS, NEW_PROMPT>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS_SHORT, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS_SHORT, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 1, PAGES_GROUPS_SHORT, NEW_PROMPT>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_ANY, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_GROUPS, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 64, 2, PAGES_GROUPS_SHORT, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_ANY, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_ANY, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_ANY, NEW_PROMPT>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS, NEW_PROMPT>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS_SHORT, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS_SHORT, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 1, PAGES_GROUPS_SHORT, NEW_PROMPT>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_ANY, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_GROUPS, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 128, 2, PAGES_GROUPS_SHORT, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_ANY, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_ANY, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_ANY, NEW_PROMPT>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS, NEW_PROMPT>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS_SHORT, NEW_ONE>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS_SHORT, NEW_SOME>(const AttnPlan&, hipStream_t);
+template hipError_t run_attention<CACHE_CODES_F32, 256, 1, PAGES_GROUPS_SHORT, NEW_PROMPT>(const AttnPlan&, hipStream_t);
 
 }  // namespace fs

@@ -86,20 +86,21 @@ __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2
 // to 8192 tokens, 6.0 and 5.4 TB/s).
 constexpr uint32_t kNone = 0x80000000u;
 constexpr int kOnce = 2;   // the non-temporal bit
-struct Buffer {
+template <int AUX>
+struct BufferT {
   __amdgpu_buffer_rsrc_t r;
-  __device__ __forceinline__ explicit Buffer(const void* p)
+  __device__ __forceinline__ explicit BufferT(const void* p)
       : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(kNone - 1), 0x20000)) {}
   __device__ __forceinline__ uint32_t load1(uint32_t off) const { return __builtin_amdgcn_raw_buffer_load_b8(r, off, 0, 0); }
   __device__ __forceinline__ uint32_t load2(uint32_t off) const { return __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0); }
   __device__ __forceinline__ uint32_t load4(uint32_t off) const { return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0); }
   __device__ __forceinline__ void load(u32x1_any& v, uint32_t off) const { v[0] = load4(off); }
   __device__ __forceinline__ void load(u32x2_any& v, uint32_t off) const {
-    const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kOnce);
+    const auto x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, AUX);
     v[0] = x[0], v[1] = x[1];
   }
   __device__ __forceinline__ void load(u32x4_any& v, uint32_t off) const {
-    const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kOnce);
+    const auto x = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, AUX);
     v[0] = x[0], v[1] = x[1], v[2] = x[2], v[3] = x[3];
   }
 };
@@ -137,9 +138,30 @@ __device__ __forceinline__ Item item_of(const AttnPlan& p, int item) {
   return item_of<TILE, R>(p, item, p.a.lengths[p.row_groups == 1 ? item : item / p.row_groups]);
 }
 
-template <int CACHE, int D, int RT, int PAGES, bool MANY>
+// The final row: out = o / l, lse; l < 0 where nothing was seen.
+template <typename T, int N>
+__device__ __forceinline__ void finish_row(const AttnPlan& p, const Item& it, int head, int row, int col, float m,
+                                           float l, const float (&o)[N]) {
+  const int r = it.row0 + row, i = r / p.group, h = head * p.group + r - i * p.group;
+  const int64_t tok = (int64_t)it.seq * p.a.n_new + i;
+  const bool none = l < 0.f;
+  if (col == 0 && p.a.lse) p.a.lse[tok * p.a.q_heads + h] = none ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+  T* dst = (T*)p.a.out.p + tok * p.a.out.ts + h * p.a.out.hs + col;
+#pragma unroll
+  for (int c = 0; c < N; c += 4) {
+    if (col + c >= p.c.d) break;
+    T v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = from_f32<T>(none ? 0.f : o[c + j] / l);
+    memcpy(dst + c, v, sizeof(v));
+  }
+}
+
+template <int CACHE, int D, int RT, int PAGES, int NEW>
 struct Attn {
   static constexpr bool P16 = PAGES != PAGES_ANY;
+  static constexpr bool MANY = NEW != NEW_ONE;
+  static constexpr int kCached = NEW == NEW_PROMPT ? 0 : kOnce;   // (a prompt's rows read the cache again and again)
   static constexpr bool kF32 = CACHE == CACHE_F32 || CACHE == CACHE_CODES_F32;
   static constexpr bool kCodes = CACHE == CACHE_CODES_BF16 || CACHE == CACHE_CODES_F32;
   static constexpr int ES = kCodes ? 1 : kF32 ? 4 : 2;       // bytes of a cache element
@@ -163,6 +185,7 @@ struct Attn {
   typedef typename RawT<VE * ES>::type VRaw;
 
   typedef uint32_t Frag __attribute__((ext_vector_type(4)));
+  typedef BufferT<kCached> Buffer;
 
   const AttnPlan& p;
   const int lane, q, g, head;
@@ -176,7 +199,7 @@ struct Attn {
   int lim[RT], low[RT];
 
   // queries: in registers, or where they are many in LDS (which the four waves share)
-  static constexpr bool kQShared = RT * KC * 4 > (kF32 ? 32 : 16);
+  static constexpr bool kQShared = NEW != NEW_PROMPT && RT * KC * 4 > (kF32 ? 32 : 16);
   Frag qf[kQShared ? 1 : RT][kQShared ? 1 : KC];
   Frag* qs;
   floatx4 o[RT][NO];
@@ -792,6 +815,38 @@ struct Attn {
     weights(pr, x.at, x.ok, x.full);
     add_values(x, pr, x.at, x.ok, x.full);
   }
+  // The item's sums to LDS: 16 rows of STRIDE.
+  __device__ __forceinline__ void put_sums(int t, float* to) const {
+#pragma unroll
+    for (int c = 0; c < VC; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < VE; j += 4)
+          *reinterpret_cast<floatx4*>(to + q * STRIDE + c * 16 * VE + (4 * g + r) * VE + j) =
+              floatx4{o[t][c * VE + j][r], o[t][c * VE + j + 1][r], o[t][c * VE + j + 2][r], o[t][c * VE + j + 3][r]};
+  }
+  // Of one wave that had the item to itself: through its own part of LDS, to whole
+  // rows.
+  __device__ __forceinline__ void finish(const Item& item, float* to) {
+    put_sums(0, to);
+    const float sum = row_sum(l[0]);
+    const float all = row_max((float)seen[0]) > 0.f ? sum : -1.f;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = i * 4 + g, col = q * NO;
+      const float mr = __shfl(m[0], row), lr = __shfl(all, row);
+      if (row < item.nrows) {
+        float v[NO];
+#pragma unroll
+        for (int c = 0; c < NO; ++c) v[c] = to[row * STRIDE + col + c];
+        finish_row<T, NO>(p, item, head, row, col, mr, lr, v);
+      }
+    }
+  }
   __device__ __forceinline__ void tiles(int from, int to) {
     if (from >= to) return;
     Tile a;
@@ -824,28 +879,9 @@ struct Attn {
   }
 };
 
-// The final row: out = o / l, lse; l < 0 where nothing was seen.
-template <typename T, int N>
-__device__ __forceinline__ void finish_row(const AttnPlan& p, const Item& it, int head, int row, int col, float m,
-                                           float l, const float (&o)[N]) {
-  const int r = it.row0 + row, i = r / p.group, h = head * p.group + r - i * p.group;
-  const int64_t tok = (int64_t)it.seq * p.a.n_new + i;
-  const bool none = l < 0.f;
-  if (col == 0 && p.a.lse) p.a.lse[tok * p.a.q_heads + h] = none ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
-  T* dst = (T*)p.a.out.p + tok * p.a.out.ts + h * p.a.out.hs + col;
-#pragma unroll
-  for (int c = 0; c < N; c += 4) {
-    if (col + c >= p.c.d) break;
-    T v[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = from_f32<T>(none ? 0.f : o[c + j] / l);
-    memcpy(dst + c, v, sizeof(v));
-  }
-}
-
-template <int CACHE, int D, int RT, int PAGES, bool MANY>
+template <int CACHE, int D, int RT, int PAGES, int NEW>
 __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void attention_kernel(AttnPlan p) {
-  typedef Attn<CACHE, D, RT, PAGES, MANY> A;
+  typedef Attn<CACHE, D, RT, PAGES, NEW> A;
   typedef typename A::T T;
   __shared__ __align__(16) float rows[kAttnWaves][16][A::STRIDE];
   __shared__ __align__(16) typename A::Frag queries[A::kQShared ? RT * A::KC * 64 : 1];
@@ -856,6 +892,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = (int)(blockIdx.x % p.c.kv_heads), worker = (int)(blockIdx.x / p.c.kv_heads);
   int item = worker;
+  if constexpr (NEW == NEW_PROMPT) {
+    // a wave an item; those that read most first
+    item = p.items - 1 - (worker * kAttnWaves + wave);
+    if (item < 0) return;
+  }
   int64_t at = 0, total = 0, left;     // tile `at` of the item; tiles left of this part
   int64_t part0 = 0;
   int parts = 0;
@@ -925,6 +966,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
     const int n = p.workers ? (int)min((int64_t)(it.tiles - from), left) : it.tiles;
     const bool whole = n == it.tiles;
     s.begin(it, wave);
+    if constexpr (NEW == NEW_PROMPT) {
+      s.tiles(it.first, it.first + it.tiles);
+      s.finish(it, &rows[wave][0][0]);
+      return;
+    }
     if constexpr (A::kQShared) __syncthreads();
     s.tiles(it.first + from + (int)((int64_t)n * wave / kAttnWaves),
             it.first + from + (int)((int64_t)n * (wave + 1) / kAttnWaves));
@@ -937,16 +983,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       if (t * 16 >= it.nrows) break;
-#pragma unroll
-      for (int c = 0; c < A::VC; ++c)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int j = 0; j < A::VE; j += 4) {
-            const floatx4 v{s.o[t][c * A::VE + j][r], s.o[t][c * A::VE + j + 1][r], s.o[t][c * A::VE + j + 2][r],
-                            s.o[t][c * A::VE + j + 3][r]};
-            *reinterpret_cast<floatx4*>(&rows[wave][s.q][c * 16 * A::VE + (4 * s.g + r) * A::VE + j]) = v;
-          }
+      s.put_sums(t, &rows[wave][0][0]);
       const float l = row_sum(s.l[t]);
       const bool seen = row_max((float)s.seen[t]) > 0.f;
       if (s.g == 0) stats[wave][s.q] = make_float2(s.m[t], seen ? l : -1.f);
@@ -1065,11 +1102,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnPlan p, int blo
 
 }  // namespace
 
-template <int CACHE, int D, int RT, int PAGES, bool MANY>
+template <int CACHE, int D, int RT, int PAGES, int NEW>
 hipError_t run_attention(const AttnPlan& p, hipStream_t s) {
-  typedef Attn<CACHE, D, RT, PAGES, MANY> A;
-  const int64_t groups = (int64_t)(p.workers ? p.workers : p.items) * p.c.kv_heads;
-  launch_k(attention_kernel<CACHE, D, RT, PAGES, MANY>, dim3((unsigned)groups), 64 * kAttnWaves, 0, s, p);
+  typedef Attn<CACHE, D, RT, PAGES, NEW> A;
+  const int64_t parts = p.workers ? p.workers : NEW == NEW_PROMPT ? (p.items + kAttnWaves - 1) / kAttnWaves : p.items;
+  const int64_t groups = parts * p.c.kv_heads;
+  launch_k(attention_kernel<CACHE, D, RT, PAGES, NEW>, dim3((unsigned)groups), 64 * kAttnWaves, 0, s, p);
   if (p.workers) {
     const int nrows = p.rows < A::R ? p.rows : A::R;
     auto join = [&](auto kernel, int rows) {

@@ -432,6 +432,26 @@ def test_attention_window(kind, window, new):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size,window", [(16, 0), (7, 0), (16, 30)])
+def test_attention_prompts(kind, size, window):
+    """So many new tokens that each wave has rows of its own: a sequence with tokens
+    before them, one of them alone, shorter ones, an empty one."""
+    lens = [150, 70, 69, 3, 0, 71, 70, 100, 12, 90, 70, 33]
+    check_attention(kind, 20, 5, 64, lens, size, new=70, window=window)
+    if not window:
+        check_attention(kind, 20, 5, 72, lens, size, new=70)
+        check_attention(kind, 20, 5, 136, lens, size, new=70)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_attention_many_rows(kind):
+    """Row groups of one key head, divided and not."""
+    check_attention(kind, 20, 1, 256, [400, 90], 16, new=17)
+    check_attention(kind, 20, 1, 64, [90], 16, new=60)
+    check_attention(kind, 300, 1, 128, [333], 16)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("lens", ["long", "one"])
 def test_attention_divided(kind, lens):
     """Sequences in several parts, and parts of several sequences."""
@@ -482,9 +502,10 @@ def test_attention_values_that_are_not_finite(kind, size):
     """An infinite or NaN value reaches the queries that see it, in its column (in
     its block of a coded cache), and no other."""
     dtype, codes = kind.split()[0], "codes" in kind
-    for window in (0, 6):
+    # (the last ones: a wave a row tile)
+    for window, lens, new in ((0, [40, 9], 5), (6, [40, 9], 5), (0, [240, 9] + [232] * 10, 232)):
         g = gen(21)
-        lens, new, d = [40, 9], 5, 64
+        d = 64
         table, pages = pages_of(g, lens, size)
         cache = Cache(g, pages, 2, size, d, dtype, codes)
         q = heads(g, len(lens) * new, 6, d, dtype)
