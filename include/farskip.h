@@ -807,7 +807,8 @@ typedef struct {
   int64_t page_stride;  /* in elements, multiples of 8; place_stride <= 2^20 */
   int64_t head_stride;
   int64_t place_stride;
-  uint8_t* k_scales;    /* [n_pages, kv_heads, page_size, ceil(head_dim / 32)] with codes */
+  uint8_t* k_scales;    /* [n_pages, kv_heads, page_size, ceil(head_dim / 32)] with codes; 8-byte
+                           aligned */
   uint8_t* v_scales;
 } fs_kv_cache;
 

@@ -190,10 +190,14 @@ fs_status check_cache_memory(const fs_kv_cache* c, const CacheArrs& m) {
     if (!aligned_to(m.a[i].p, c->codes ? 8 : 16))
       return fail(FS_ERR_INVALID, std::string(m.a[i].name) + (c->codes ? " must be 8-byte aligned" : " must be 16-byte aligned"));
   }
-  if (c->page_stride % 8 || c->head_stride % 8 || c->place_stride % 8)
-    return fail(FS_ERR_INVALID, "cache: strides must be multiples of 8");
-  if (c->place_stride > (1 << 20)) return fail(FS_ERR_UNSUPPORTED, "cache: place_stride must be <= 2^20");
+  const int64_t counts[] = {c->n_pages, c->kv_heads, c->page_size};
+  const int64_t strides[] = {c->page_stride, c->head_stride, c->place_stride};
+  for (int i = 0; i < 3; ++i)
+    if (counts[i] > 1 && strides[i] % 8) return fail(FS_ERR_INVALID, "cache: strides must be multiples of 8");
+  if (c->page_size > 1 && c->place_stride > (1 << 20)) return fail(FS_ERR_UNSUPPORTED, "cache: place_stride must be <= 2^20");
   if (c->codes && (!c->k_scales || !c->v_scales)) return fail(FS_ERR_INVALID, "cache: codes without scales");
+  if (c->codes && (!aligned_to(c->k_scales, 8) || !aligned_to(c->v_scales, 8)))
+    return fail(FS_ERR_INVALID, "cache: scales must be 8-byte aligned");
   for (int i = 0; i < 4; ++i)
     for (int j = i + 1; j < 4; ++j) TRY(no_overlap(m.a[i], m.a[j]));
   return FS_OK;

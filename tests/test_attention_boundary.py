@@ -153,7 +153,8 @@ def _heads(kw, i=0):
 
 
 def test_codes_need_scales():
-    for kw in (dict(k_scales=None), dict(v_scales=None), dict(v_scales=3 << 40), dict(k=(1 << 40) + 4)):
+    for kw in (dict(k_scales=None), dict(v_scales=None), dict(v_scales=3 << 40), dict(k=(1 << 40) + 4), dict(k_scales=(3 << 40) + 4),
+               dict(v_scales=(4 << 40) + 1)):
         refuse(L.FS_ERR_INVALID, "", fs.fs_paged_attention, attn(), cache(1, **kw), A, B, pages(), C, WS)
 
 
@@ -222,6 +223,22 @@ def test_attention_arguments():
         a = dict(dict(out=C, ws=WS, lse=None), **kw)
         refuse(L.FS_ERR_INVALID, "overlap", at, d, c, A, B, long, a["out"], a["ws"], lse=a["lse"])
     at(d, c, None, None, pages(sequences=0), None, None, stream=0)
+
+
+def test_cache_views():
+    """Keys and values beside one another in a page or in a place; strides that no
+    second element has are not looked at.  (The workspace is refused last.)"""
+    views = [dict(k=1 << 40, v=(1 << 40) + 2 * 1024, page_stride=2048),
+             dict(k=1 << 40, v=(1 << 40) + 2 * 64, page_stride=2048, place_stride=128, head_stride=32),
+             dict(n_pages=1, page_stride=3), dict(kv_heads=1, head_stride=-1, page_stride=512),
+             dict(page_size=1, place_stride=1 << 50, head_stride=32, page_stride=64)]
+    for kw in views:
+        heads = kw.get("kv_heads", 2) * 2
+        refuse(L.FS_ERR_WORKSPACE, "", fs.fs_paged_attention, attn(heads), cache(**kw), A, B,
+               pages(max_pages=1 << 16, ldt=1 << 16), C, (D, 0))
+    # beside one another, but too near
+    for kw in (dict(views[0], v=(1 << 40) + 2 * 1016), dict(views[0], v=(1 << 40) + 2 * 1032), dict(views[1], page_stride=1976)):
+        refuse(L.FS_ERR_INVALID, "overlap", fs.fs_paged_attention, attn(), cache(**kw), A, B, pages(), C, WS)
 
 
 def test_many_rows():

@@ -812,3 +812,158 @@ def test_two_streams():
     torch.cuda.synchronize()
     for w, outs in zip(want, got):
         assert all(torch.equal(w, o) for o in outs)
+
+
+def test_graph_divided():
+    """A captured call whose lengths change between replays, from nothing to what
+    every workgroup has a part of, with eager calls on the same workspace between."""
+    g = gen(71)
+    lens = [2000, 1500, 0, 900, 2048]
+    table, pages = pages_of(g, [2048] * 5, 16)
+    for kind in ("bf16", "f32", "bf16 codes"):
+        dtype, codes = kind.split()[0], "codes" in kind
+        cache = Cache(g, pages, 2, 16, 128, dtype, codes)
+        q = heads(g, 5, 6, 128, dtype)
+        desc = fs.attention_desc(6, 1, 0.1)
+        need = fs.fs_paged_attention_workspace(desc, cache.struct, table)
+        assert need > 0
+        ws = torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV)
+        lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        out, eager = (torch.empty((5, 6, 128), dtype=TORCH[dtype], device=DEV) for _ in range(2))
+        lse = torch.empty((5, 6), device=DEV)
+        fs.fs_paged_attention(desc, cache.struct, q, lengths, table, out, ws, lse=lse)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            fs.fs_paged_attention(desc, cache.struct, q, lengths, table, out, ws, lse=lse)
+        for step in ([0] * 5, [1, 0, 2048, 17, 16], lens, [2048] * 5, [3, 3, 3, 3, 3], lens):
+            lengths.copy_(torch.tensor(step, dtype=torch.int32))
+            out.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            fs.fs_paged_attention(desc, cache.struct, q, lengths, table, eager, ws)
+            torch.cuda.synchronize()
+            assert torch.equal(out, eager), step
+            assert [bool(torch.isinf(r).all()) for r in lse] == [n == 0 for n in step]
+
+
+# --------------------------------------------------- calls at the edges
+def plain_call(cache, q, lengths, table, heads_, new=1, window=0):
+    desc = fs.attention_desc(heads_, new, 0.125, window)
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device=DEV)
+    lse = torch.full(q.shape[:2], 7.0, device=DEV)
+    ws = torch.empty((max(256, fs.fs_paged_attention_workspace(desc, cache, table)),), dtype=torch.uint8, device=DEV)
+    fs.fs_paged_attention(desc, cache, q, torch.tensor(lengths, dtype=torch.int32, device=DEV), table, out, ws, lse=lse)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def test_lengths_out_of_range():
+    """Negative lengths are 0, ones above the page table's reach end there."""
+    g = gen(81)
+    table, pages = pages_of(g, [600, 600, 600], 16)
+    cache = Cache(g, pages, 2, 16, 64, "bf16")
+    q = heads(g, 3, 4, 64, "bf16")
+    reach = table.shape[1] * 16
+    a = plain_call(cache.struct, q, [-5, 2 ** 31 - 1, -2 ** 31], table, 4)
+    b = plain_call(cache.struct, q, [0, reach, 0], table, 4)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert bool((a[0][0] == 0).all()) and bool(torch.isfinite(a[1][1]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nothing_there(dtype):
+    """A page table without columns, a cache without pages, a step without rows."""
+    g = gen(82)
+    q = heads(g, 3, 4, 64, dtype)
+    cache = Cache(g, 4, 2, 16, 64, dtype)
+    none = torch.empty((3, 0), dtype=torch.int32, device=DEV)
+    empty = fs.kv_cache(*(torch.empty((0, 2, 16, 64), dtype=TORCH[dtype], device=DEV) for _ in range(2)))
+    table = torch.zeros((3, 40), dtype=torch.int32, device=DEV)
+    for c, t in ((cache.struct, none), (empty, table), (empty, table[:, :3])):
+        out, lse = plain_call(c, q, [5, 0, 600], t, 4)
+        assert bool((out == 0).all()) and bool((lse == float("-inf")).all())
+        before = cache.k.clone()
+        k, v = heads(g, 3, 2, 64, dtype), heads(g, 3, 2, 64, dtype)
+        pos = torch.tensor([0, 1, 700], dtype=torch.int32, device=DEV)
+        qo = torch.empty_like(q)
+        fs.fs_cache_append(c, None, q, k, v, None, pos, t, qo)
+        torch.cuda.synchronize()
+        assert torch.equal(qo, q) and torch.equal(cache.k, before)
+    fs.fs_cache_append(cache.struct, None, None, k[:0], v[:0], None, pos[:0], table, None)
+    fs.fs_rotary(fs.rotary_desc(0, 4, 64, dtype), None, q[:0], pos[:0], q[:0])
+    out = torch.empty_like(q)
+    fs.fs_rotary(fs.rotary_desc(3, 4, 64, dtype), None, q, pos, out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, q)
+
+
+def test_undivided_many_sequences():
+    """More sequences than a divided call takes, one of them long."""
+    g = torch.Generator().manual_seed(5)
+    lens = torch.randint(0, 9, (4200,), generator=g).tolist()
+    lens[4100] = 650
+    check_attention("bf16", 1, 1, 64, lens, 16)
+
+
+@pytest.mark.parametrize("size", [1, 5, 16])
+@pytest.mark.parametrize("kind", ["bf16 codes", "f32 codes"])
+@pytest.mark.parametrize("d", [8, 32, 72, 96, 136, 192, 200])
+def test_last_scale_bytes(kind, d, size):
+    """Every place of a cache in use: rows of few scale bytes at the end of theirs,
+    which lie at the end of an allocation's part."""
+    dtype = kind.split()[0]
+    g = gen(83 + d)
+    n = 80
+    table, pages = pages_of(g, [n], size, spare=0)
+    table.copy_(torch.arange(pages, dtype=torch.int32, device=DEV).flip(0) if size == 5 else torch.arange(pages, dtype=torch.int32, device=DEV))
+    c = Cache(g, pages, 1, size, d, dtype, True)
+    # the scales between bytes that would be seen as NaNs
+    for x in (0, 1):
+        s = (c.ks, c.vs)[x]
+        full = torch.full((s.numel() + 512,), 255, dtype=torch.uint8, device=DEV)
+        view = full[256:256 + s.numel()].view(s.shape)
+        view.copy_(s)
+        if x == 0:
+            c.ks = view
+        else:
+            c.vs = view
+    c.struct = fs.kv_cache(c.k, c.v, c.ks, c.vs, dtype=dtype)
+    q = heads(g, 1, 2, d, dtype)
+    out, lse = plain_call(c.struct, q, [n], table, 2)
+    k, v = c.values()
+    want, want_lse, mass, reach = O.attention(f64(q), k, v, [n], table.cpu().numpy(), 1, 0.125)
+    err = np.expm1((d + 2) * U * reach) + 2.0 ** -21 + n * 2.0 ** -24 + 2.0 ** -20
+    tol = (2 * (err + (2.0 ** -8 if dtype == "bf16" else 0)))[..., None] * mass
+    near(f64(out), want, tol + HALF[dtype] * (np.abs(want) + tol))
+
+
+def test_append_the_same_place_twice():
+    """Every element is one of the two tokens', what is beside stays."""
+    g = gen(84)
+    table = torch.tensor([[1, 0]], dtype=torch.int32, device=DEV)
+    cache = Cache(g, 3, 2, 16, 64, "bf16")
+    before = cache.k.clone()
+    k, v = heads(g, 2, 2, 64, "bf16"), heads(g, 2, 2, 64, "bf16")
+    at = torch.full((2,), 18, dtype=torch.int32, device=DEV)
+    fs.fs_cache_append(cache.struct, None, None, k, v, torch.zeros_like(at), at, table, None)
+    torch.cuda.synchronize()
+    got = cache.k[0, :, 2]
+    assert bool(((got == k[0]) | (got == k[1])).all())
+    cache.k[0, :, 2] = before[0, :, 2]
+    assert torch.equal(cache.k, before)
+
+
+def test_keys_and_values_of_one_tensor():
+    """A cache as [pages, 2, kv_heads, page, head_dim] and as [pages, page, 2,
+    kv_heads, head_dim], against one of two tensors."""
+    g = gen(85)
+    table, pages = pages_of(g, [50, 33], 16)
+    two = Cache(g, pages, 2, 16, 64, "bf16")
+    q = heads(g, 2, 4, 64, "bf16")
+    want = plain_call(two.struct, q, [50, 33], table, 4)
+    one = torch.stack((two.k, two.v), 1)
+    other = torch.stack((two.k.transpose(1, 2), two.v.transpose(1, 2)), 2).contiguous()
+    for k, v in ((one[:, 0], one[:, 1]), (other[:, :, 0].transpose(1, 2), other[:, :, 1].transpose(1, 2))):
+        got = plain_call(fs.kv_cache(k, v), q, [50, 33], table, 4)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
