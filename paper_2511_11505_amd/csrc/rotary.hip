@@ -84,10 +84,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs g, PagedCache pc
   __shared__ __align__(16) float2 table[4][kMaxPairs];
   __shared__ __align__(16) T stage[FAST ? 1 : 4][FAST ? 1 : kUnroll][FAST ? 1 : 64 * 8];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  const int token = (int)(id / splits);
+  const uint32_t id = blockIdx.x * 4 + wave;
+  const int token = (int)(id / (uint32_t)splits);
   if (token >= g.tokens) return;
-  int batch = (int)(id % splits) * per_split;
+  int batch = (int)(id % (uint32_t)splits) * per_split;
   const int last = min(batch + per_split, bt.q + 2 * bt.kv);
 
   const int pairs = g.rope.rot / 2;
