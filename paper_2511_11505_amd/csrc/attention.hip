@@ -58,6 +58,7 @@ Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
     const int64_t parts = (h.items * most + kAttnMinTiles - 1) / kAttnMinTiles;
     h.workers = (kCus * attn_groups_per_cu(h.width, h.rt) + c.kv_heads - 1) / c.kv_heads;
     if (parts < h.workers) h.workers = (int)parts;
+    if (h.workers < 2) h.workers = 0;   // (one part has nothing to divide)
   }
   return h;
 }

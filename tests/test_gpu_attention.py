@@ -470,6 +470,12 @@ def test_attention_many_sequences(kind):
     check_attention(kind, 2, 1, 64, lens, 16)
 
 
+def test_attention_many_key_heads():
+    """Key heads that fill the chip alone: parts of whole sequences, and none."""
+    check_attention("bf16", 300, 300, 8, [700, 30], 16)
+    check_attention("f32", 520, 520, 8, [700, 30], 16)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32 codes"])
 def test_attention_strides(kind):
     check_attention(kind, 6, 2, 80, [50, 130, 0], 16, order="tokens", gap=8, pad=3, lead=1)
