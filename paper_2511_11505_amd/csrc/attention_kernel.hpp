@@ -111,6 +111,7 @@ struct Item {
   int lo, hi;              // tokens that any of its rows sees: [lo, hi)
   int lo_all, hi_all;      // tokens that all of them see
   int first, tiles;        // tiles of TILE tokens, at least one
+  int slots;               // what it counts for when work is divided
 };
 template <int TILE, int R>
 __device__ __forceinline__ Item item_of(const AttnPlan& p, int item, int length) {
@@ -130,6 +131,8 @@ __device__ __forceinline__ Item item_of(const AttnPlan& p, int item, int length)
     t.first = t.lo / TILE;
     t.tiles = (t.hi + TILE - 1) / TILE - t.first;
   }
+  // (starting and ending an item takes about as long as that many tiles)
+  t.slots = max(t.tiles, kAttnMinTiles);
   return t;
 }
 
@@ -910,14 +913,14 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
     item = p.items - 1 - (worker * kAttnWaves + wave);
     if (item < 0) return;
   }
-  int64_t at = 0, total = 0, left;     // tile `at` of the item; tiles left of this part
+  int64_t at = 0, total = 0, left;     // slot `at` of the item; slots left of this part
   int64_t part0 = 0;
   int parts = 0;
   int length = 0;      // of lane i's sequence, where there are at most 64 items of one row group
   const bool few = p.items <= 64 && p.row_groups == 1;
   if (p.workers && few) {
     if (lane < p.items) length = p.a.lengths[lane];
-    const int64_t mine = lane < p.items ? item_of<A::TILE, A::R>(p, lane, length).tiles : 0;
+    const int64_t mine = lane < p.items ? item_of<A::TILE, A::R>(p, lane, length).slots : 0;
     int64_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -932,10 +935,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
     item = __builtin_ctzll(__ballot(part0 < incl));
     at = part0 - lane_i64(incl - mine, item);
   } else if (p.workers) {
-    // tiles before each thread's items
+    // slots before each thread's items
     const int per = (p.items + 255) / 256, i0 = min(tid * per, p.items), i1 = min(i0 + per, p.items);
     int64_t mine = 0;
-    for (int i = i0; i < i1; ++i) mine += item_of<A::TILE, A::R>(p, i).tiles;
+    for (int i = i0; i < i1; ++i) mine += item_of<A::TILE, A::R>(p, i).slots;
     int64_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -957,7 +960,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
     int64_t excl = before + incl - mine;
     if (part0 >= excl && part0 < excl + mine)
       for (int i = i0; i < i1; ++i) {
-        const int n = item_of<A::TILE, A::R>(p, i).tiles;
+        const int n = item_of<A::TILE, A::R>(p, i).slots;
         if (part0 < excl + n) {
           found[0] = i, found[1] = part0 - excl;
           break;
@@ -976,8 +979,15 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
   while (left > 0) {
     const Item it = p.workers && few ? item_of<A::TILE, A::R>(p, item, lane_i(length, item)) : item_of<A::TILE, A::R>(p, item);
     const int from = (int)at;
-    const int n = p.workers ? (int)min((int64_t)(it.tiles - from), left) : it.tiles;
+    const int take = p.workers ? (int)min((int64_t)(it.slots - from), left) : it.slots;
+    const int n = min(from + take, it.tiles) - from;
     const bool whole = n == it.tiles;
+    left -= p.workers ? take : 1;
+    const int64_t start = part0;
+    part0 += take;
+    at = 0;
+    ++item;
+    if (n <= 0) continue;    // (slots behind the last tile)
     s.begin(it, wave);
     if constexpr (NEW == NEW_PROMPT) {
       s.tiles(it.first, it.first + it.tiles);
@@ -989,8 +999,8 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
             it.first + from + (int)((int64_t)n * (wave + 1) / kAttnWaves));
     if (p.workers && from == 0 && head == 0 && tid == 0) {
       // the parts that hold this item: the last part that starts at or before a tile
-      const int64_t t0 = part0, t1 = part0 + it.tiles - 1;
-      p.span[item] = make_int2((int)(((t0 + 1) * parts - 1) / total), (int)(((t1 + 1) * parts - 1) / total));
+      const int64_t t0 = start, t1 = start + it.tiles - 1;
+      p.span[item - 1] = make_int2((int)(((t0 + 1) * parts - 1) / total), (int)(((t1 + 1) * parts - 1) / total));
     }
     // the four waves' sums
 #pragma unroll
@@ -1036,10 +1046,6 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
       }
       __syncthreads();
     }
-    left -= p.workers ? n : 1;
-    part0 += n;
-    at = 0;
-    ++item;
   }
 }
 
