@@ -899,9 +899,9 @@ template <int CACHE, int D, int RT, int PAGES, int NEW>
 __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void attention_kernel(AttnPlan p) {
   typedef Attn<CACHE, D, RT, PAGES, NEW> A;
   typedef typename A::T T;
-  __shared__ __align__(16) float rows[kAttnWaves][16][A::STRIDE];
+  __shared__ __align__(16) float rows[kAttnWaves][A::R][A::STRIDE];
   __shared__ __align__(16) typename A::Frag queries[A::kQShared ? RT * A::KC * 64 : 1];
-  __shared__ float2 stats[kAttnWaves][16];
+  __shared__ float2 stats[kAttnWaves][A::R];
   __shared__ int64_t scan[kAttnWaves];
   __shared__ int64_t found[2];   // first item | its first tile
 
@@ -1002,50 +1002,51 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
       const int64_t t0 = start, t1 = start + it.tiles - 1;
       p.span[item - 1] = make_int2((int)(((t0 + 1) * parts - 1) / total), (int)(((t1 + 1) * parts - 1) / total));
     }
-    // the four waves' sums
+    // the four waves' sums: all of them to LDS, then a loop over the row tiles (not
+    // unrolled: what runs once an item waits for its instructions to be fetched)
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      if (t * 16 >= it.nrows) break;
-      s.put_sums(t, &rows[wave][0][0]);
+      s.put_sums(t, &rows[wave][t * 16][0]);
       const float l = row_sum(s.l[t]);
       const bool seen = row_max((float)s.seen[t]) > 0.f;
-      if (s.g == 0) stats[wave][s.q] = make_float2(s.m[t], seen ? l : -1.f);
-      __syncthreads();
-      constexpr int N = D / 16;
-      const int row = tid >> 4, col = (tid & 15) * N;
-      if (t * 16 + row < it.nrows) {
-        float m = -INFINITY, sum = 0.f, o[N];
-        bool any = false;
+      if (s.g == 0) stats[wave][t * 16 + s.q] = make_float2(s.m[t], seen ? l : -1.f);
+    }
+    __syncthreads();
+    constexpr int N = D / 16;
+    const int col = (tid & 15) * N;
+#pragma unroll 1
+    for (int row = tid >> 4; row < it.nrows; row += 16) {
+      float m = -INFINITY, sum = 0.f, o[N];
+      bool any = false;
 #pragma unroll
-        for (int w = 0; w < kAttnWaves; ++w) m = fmaxf(m, stats[w][row].x);
+      for (int w = 0; w < kAttnWaves; ++w) m = fmaxf(m, stats[w][row].x);
 #pragma unroll
-        for (int c = 0; c < N; ++c) o[c] = 0.f;
+      for (int c = 0; c < N; ++c) o[c] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kAttnWaves; ++w) {
-          const float2 st = stats[w][row];
-          const float e = st.x == -INFINITY ? 0.f : exp2_hw(st.x - m);
-          any |= !(st.y < 0.f);
-          sum += st.y < 0.f ? 0.f : e * st.y;
+      for (int w = 0; w < kAttnWaves; ++w) {
+        const float2 st = stats[w][row];
+        const float e = st.x == -INFINITY ? 0.f : exp2_hw(st.x - m);
+        any |= !(st.y < 0.f);
+        sum += st.y < 0.f ? 0.f : e * st.y;
 #pragma unroll
-          for (int c = 0; c < N; c += 4) {
-            const floatx4 v = *reinterpret_cast<const floatx4*>(&rows[w][row][col + c]);
+        for (int c = 0; c < N; c += 4) {
+          const floatx4 v = *reinterpret_cast<const floatx4*>(&rows[w][row][col + c]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[c + j] += e * v[j];
-          }
-        }
-        if (!any) sum = -1.f;
-        if (whole) {
-          finish_row<T, N>(p, it, head, t * 16 + row, col, m, sum, o);
-        } else {
-          const int64_t pr = (((int64_t)worker * p.c.kv_heads + head) * 2 + (from == 0 ? 1 : 0)) * A::R + t * 16 + row;
-#pragma unroll
-          for (int c = 0; c < N; c += 4)
-            *reinterpret_cast<floatx4*>(p.part + pr * D + col + c) = floatx4{o[c], o[c + 1], o[c + 2], o[c + 3]};
-          if (col == 0) p.stat[pr] = make_float2(m, sum);
+          for (int j = 0; j < 4; ++j) o[c + j] += e * v[j];
         }
       }
-      __syncthreads();
+      if (!any) sum = -1.f;
+      if (whole) {
+        finish_row<T, N>(p, it, head, row, col, m, sum, o);
+      } else {
+        const int64_t pr = (((int64_t)worker * p.c.kv_heads + head) * 2 + (from == 0 ? 1 : 0)) * A::R + row;
+#pragma unroll
+        for (int c = 0; c < N; c += 4)
+          *reinterpret_cast<floatx4*>(p.part + pr * D + col + c) = floatx4{o[c], o[c + 1], o[c + 2], o[c + 3]};
+        if (col == 0) p.stat[pr] = make_float2(m, sum);
+      }
     }
+    __syncthreads();
   }
 }
 
