@@ -24,11 +24,17 @@ int cache_of(int dtype, const PagedCache& c) {
 
 // Row tiles of an item: what the rows of a sequence need, up to what the
 // registers hold (a row tile takes D / 4 of them for its sums and D / 8, in fp32
-// D / 4, for its queries).
-int row_tiles(int dtype, int width, int rows) {
-  const int most = dtype == 0 ? (width == 256 ? 1 : 2) : (width == 256 ? 2 : 4);
-  const int need = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  return need < most ? need : most;
+// D / 4, for its queries).  Four leave one workgroup to a CU and start later, but
+// read a long bf16 cache once where two read it twice: 56 rows a key head, 8 of them,
+// four tiles | two, us: 32 sequences of 4096 tokens 153 | 167, 1 of 65536 87 | 106;
+// 8 of 4096 and 32 of 1024 (2^18 tokens and heads) 55 | 54 and 55 | 56, 8 of 512
+// 31 | 17, 256 of 512 249 | 185.  An 8-bit cache does not gain: 16 of 16384 213 | 200.
+bool four_tiles(const PagedCache& c, int64_t tokens) {
+  return !c.codes && tokens > 512 && (double)c.sequences * tokens * c.kv_heads > (1 << 18);
+}
+int row_tiles(int dtype, int width, int rows, const PagedCache& c, int64_t tokens) {
+  if (rows <= 16 || (dtype == 0 && width == 256)) return 1;
+  return rows <= 32 || dtype == 0 || width == 256 || !four_tiles(c, tokens) ? 2 : 4;
 }
 
 struct Shape {
@@ -41,7 +47,8 @@ Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
   h.width = width_of(c.d);
   h.group = q_heads / c.kv_heads;
   h.rows = n_new * h.group;
-  h.rt = row_tiles(dtype, h.width, h.rows);
+  const int64_t tokens = (int64_t)c.max_pages * c.page_size;
+  h.rt = row_tiles(dtype, h.width, h.rows, c, tokens);
   const int tiles = (h.rows + 15) / 16;
   h.workers = 0;
   if (n_new > 1 && tiles > kPromptTiles && (int64_t)c.sequences * tiles * c.kv_heads >= kPromptWaves) {
@@ -53,7 +60,7 @@ Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
   // A sequence of at most four tiles a wave is not worth a second launch;
   // beyond kAttnMaxItems, or that many workgroups, there is enough to fill the chip.
   const int tile = dtype == 0 ? 16 : 32;
-  const int64_t most = ((int64_t)c.max_pages * c.page_size + tile - 1) / tile;
+  const int64_t most = (tokens + tile - 1) / tile;
   if (h.items <= kAttnMaxItems && h.items * c.kv_heads <= kMaxGroups && most > 4 * kAttnWaves) {
     const int64_t parts = (h.items * most + kAttnMinTiles - 1) / kAttnMinTiles;
     h.workers = (kCus * attn_groups_per_cu(h.width, h.rt) + c.kv_heads - 1) / c.kv_heads;
@@ -90,7 +97,7 @@ hipError_t run_cache(int width, int rt, const AttnPlan& p, hipStream_t s) {
     return run_pages<CACHE, 256, 1>(p, s);
   }
   if (rt == 4) {
-    if constexpr (!f32) return width == 64 ? run_pages<CACHE, 64, 4>(p, s) : run_pages<CACHE, 128, 4>(p, s);
+    if constexpr (CACHE == CACHE_BF16) return width == 64 ? run_pages<CACHE, 64, 4>(p, s) : run_pages<CACHE, 128, 4>(p, s);
   }
   if (rt == 2) return width == 64 ? run_pages<CACHE, 64, 2>(p, s) : run_pages<CACHE, 128, 2>(p, s);
   return width == 64 ? run_pages<CACHE, 64, 1>(p, s) : run_pages<CACHE, 128, 1>(p, s);

@@ -766,8 +766,8 @@ struct Attn {
   // second being what rounding takes from it (then 2^-16 of it): reading the cache
   // bounds the kernel, the products are free (146.8 us for 146.1, error against 64
   // bits 1.7e-3 for 2.0e-3, the output's own rounding).  It is rounded to bf16 once
-  // (2^-8 of it) where the values have 8 bits (2% of the time) and with more than 32
-  // rows, where products bound it.
+  // (2^-8 of it) where the values have 8 bits (2% of the time) and with four row tiles,
+  // where products bound it.
   static constexpr bool kRest = CACHE == CACHE_BF16 && RT <= 2 && NEW != NEW_PROMPT;
   __device__ __forceinline__ void values(const Tile& x, const float (&pr)[RT][VT]) {
     if constexpr (kF32) {

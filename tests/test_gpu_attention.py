@@ -346,10 +346,10 @@ LENGTHS = {"small": [0, 1, 2, 15, 16, 17, 31, 33], "mid": [63, 64, 65, 300, 1, 0
 
 
 def check_attention(kind, h, kv, d, lens, size, new=1, window=0, pad=0, order="heads", gap=0, seed=0, scale=None,
-                    holes=(), lead=0):
+                    holes=(), lead=0, tokens=0):
     dtype, codes = kind.split()[0], "codes" in kind
     g = gen(seed + d + size + h)
-    table, pages = pages_of(g, lens, size)
+    table, pages = pages_of(g, lens, size, width=tokens // size)
     cache = Cache(g, pages, kv, size, d, dtype, codes, order, gap, poison=True)
     real = Cache(g, pages, kv, size, d, dtype, codes, order, gap)
     # only the places that hold tokens are not NaN
@@ -461,6 +461,24 @@ def test_attention_divided(kind, lens):
     check_attention(kind, 6, 3, 72, LENGTHS[lens], 9, new=2)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "bf16 codes"])
+@pytest.mark.parametrize("size", [16, 5])
+@pytest.mark.parametrize("d", [40, 64, 128])
+def test_attention_many_rows_of_a_long_table(kind, size, d):
+    """Over 32 rows a key head where the table has room for 2^18 tokens and heads:
+    short and long sequences, divided and not."""
+    for new, lens in ((4, [900, 0, 3, 64, 2500]), (7, [31, 1, 700])):
+        check_attention(kind, 33, 3, d, lens, size, new=new, tokens=40000)
+        check_attention(kind, 33, 3, d, lens, size, new=new, tokens=40000, window=45)
+
+
+def test_attention_many_rows_undivided():
+    g = torch.Generator().manual_seed(6)
+    lens = torch.randint(0, 9, (4200,), generator=g).tolist()
+    lens[4100] = 650
+    check_attention("bf16", 36, 1, 64, lens, 16)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32", "bf16 codes"])
 def test_attention_many_sequences(kind):
     """More sequences than the scan has threads, and more than are divided."""
@@ -510,11 +528,12 @@ def test_attention_values_that_are_not_finite(kind, size):
     """An infinite or NaN value reaches the queries that see it, in its column (in
     its block of a coded cache), and no other."""
     dtype, codes = kind.split()[0], "codes" in kind
-    # (the last ones: a wave a row tile)
-    for window, lens, new in ((0, [40, 9], 5), (6, [40, 9], 5), (0, [240, 9] + [232] * 10, 232)):
+    # (the third: a wave a row tile; the last: four row tiles a wave over a long table)
+    for window, lens, new, tokens in ((0, [40, 9], 5, 0), (6, [40, 9], 5, 0), (0, [240, 9] + [232] * 10, 232, 0),
+                                      (0, [40, 17], 15, 70000)):
         g = gen(21)
         d = 64
-        table, pages = pages_of(g, lens, size)
+        table, pages = pages_of(g, lens, size, width=tokens // size)
         cache = Cache(g, pages, 2, size, d, dtype, codes)
         q = heads(g, len(lens) * new, 6, d, dtype)
         desc = fs.attention_desc(6, new, d ** -0.5, window)
