@@ -767,7 +767,9 @@ struct Attn {
   // bounds the kernel, the products are free (146.8 us for 146.1, error against 64
   // bits 1.7e-3 for 2.0e-3, the output's own rounding).  It is rounded to bf16 once
   // (2^-8 of it) where the values have 8 bits (2% of the time) and with four row tiles,
-  // where products bound it.
+  // where products bound it.  The first number is cut, not rounded, and the second is
+  // at least 2^-17 of the weight: neither is below 0, nor 0 where the weight is not, so
+  // that an infinite value stays one.
   static constexpr bool kRest = CACHE == CACHE_BF16 && RT <= 2 && NEW != NEW_PROMPT;
   __device__ __forceinline__ void values(const Tile& x, const float (&pr)[RT][VT]) {
     if constexpr (kF32) {
@@ -789,8 +791,13 @@ struct Attn {
       for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          pf[t][i] = (__bf16)pr[t][i];
-          if constexpr (kRest) rest[t][i] = (__bf16)(pr[t][i] - (float)pf[t][i]);
+          if constexpr (kRest) {
+            const float cut = __uint_as_float(__float_as_uint(pr[t][i]) & 0xFFFF0000u);
+            pf[t][i] = (__bf16)cut;
+            rest[t][i] = (__bf16)fmaxf(pr[t][i] - cut, pr[t][i] * 0x1p-17f);
+          } else {
+            pf[t][i] = (__bf16)pr[t][i];
+          }
         }
 #pragma unroll
       for (int c = 0; c < VC; ++c) {

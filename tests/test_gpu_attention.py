@@ -563,6 +563,43 @@ def test_attention_values_that_are_not_finite(kind, size):
         assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)]) and not np.isinf(got[~np.isinf(want)]).any()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", [16, 5])
+@pytest.mark.parametrize("h,new", [(4, 1), (4, 3), (24, 1), (24, 4)])
+def test_attention_infinite_values_that_every_row_sees(kind, size, h, new):
+    """They stay what they are, where weights are rounded too: alone, against a NaN,
+    and with both signs."""
+    g = gen(24)
+    dtype, codes, d, kv, lens = kind.split()[0], "codes" in kind, 64, 2, [100, 700]
+    table, pages = pages_of(g, lens, size)
+    cache = Cache(g, pages, kv, size, d, dtype, codes)
+    q = heads(g, len(lens) * new, h, d, dtype)
+    inf, nan = float("inf"), float("nan")
+    want = np.zeros((len(lens), kv, d))
+    for b, j, head, c, value in [(0, 5, 0, 3, inf), (0, 40, 0, 9, -inf), (0, 41, 0, 9, -inf), (0, 63, 1, 20, inf),
+                                 (0, 2, 1, 20, -inf), (1, 0, 0, 33, -inf), (1, 555, 1, 63, inf), (1, 31, 1, 0, inf),
+                                 (1, 600, 1, 0, nan)]:
+        pg, pl = place_of(table, size, b, j)
+        if codes:      # (the format has no infinity; a scale of byte 255 makes a block of NaNs)
+            cache.v[pg, head, pl, c // 32 * 32:c // 32 * 32 + 32] = 0x7F
+            cache.vs[pg, head, pl, c // 32] = 255
+            want[b, head, c // 32 * 32:c // 32 * 32 + 32] = nan
+        else:
+            cache.v[pg, head, pl, c] = value
+            with np.errstate(invalid="ignore"):
+                want[b, head, c] += value
+    desc = fs.attention_desc(h, new, d ** -0.5)
+    ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, table) + 256,), dtype=torch.uint8, device=DEV)
+    out = Out(len(lens) * new, h, d, dtype)
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    fs.fs_paged_attention(desc, cache.struct, q, lengths, table, out.view, ws)
+    torch.cuda.synchronize()
+    got = out.get().reshape(len(lens), new, kv, h // kv, d)
+    want = np.broadcast_to(want[:, None, :, None], got.shape)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    assert np.isfinite(got[np.isfinite(want)]).all()
+
+
 def test_attention_scores_that_are_not_finite():
     """As the formula has them: a key of minus infinity has no weight, a row of
     nothing else is 0 / 0, a NaN or plus infinity makes NaNs."""
