@@ -10,11 +10,17 @@ namespace {
 
 constexpr int kCus = 256;
 constexpr int kMaxGroups = 1 << 16;
-// From here on a wave has a row tile to itself and nothing is joined: a prompt of
-// 2048 tokens of 64 query and 8 key heads 311 us, with four row tiles a workgroup, its
-// waves dividing the tokens, 883 (512 tokens after 3584, two sequences: 543 and 545).
-// Fewer rows read the cache fewer times with four tiles.
-constexpr int kPromptTiles = 16, kPromptWaves = 1024;
+// A prompt of more rows than that, enough of them for the waves below, is not
+// divided: a wave has two row tiles (in fp32 and past 128 columns one) to itself and
+// nothing is joined.  64 query and 8 key heads of 128 columns, this way | divided, us:
+// a prompt of 2048 tokens 172 | 551, of 8192 with 16 query heads 604 | 1312; 512 new
+// tokens of 4096, two sequences, 295 | 562, in fp32 1208 | 1614; 64 of 4096, six, 218 |
+// 243 (768 waves), 64 of 4096, four, 188 | 138 (512).  One row tile a wave took 308, 1172,
+// 534, -, 292 and 148, four 271, 946, 427: the products wait for the cache's tiles and
+// for the softmax.
+constexpr int kPromptTiles = 16;
+int prompt_tiles(int dtype, int width) { return dtype == 0 || width == 256 ? 1 : 2; }
+int prompt_waves(int dtype, int width) { return prompt_tiles(dtype, width) == 1 ? 1024 : 640; }
 
 int width_of(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
@@ -39,6 +45,7 @@ int row_tiles(int dtype, int width, int rows, const PagedCache& c, int64_t token
 
 struct Shape {
   int width, rt, group, rows, row_groups;
+  bool prompt;
   int64_t items;
   int workers;
 };
@@ -51,8 +58,11 @@ Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
   h.rt = row_tiles(dtype, h.width, h.rows, c, tokens);
   const int tiles = (h.rows + 15) / 16;
   h.workers = 0;
-  if (n_new > 1 && tiles > kPromptTiles && (int64_t)c.sequences * tiles * c.kv_heads >= kPromptWaves) {
-    h.rt = 1, h.row_groups = tiles, h.items = (int64_t)c.sequences * tiles;
+  const int alone = prompt_tiles(dtype, h.width), groups = (tiles + alone - 1) / alone;
+  h.prompt = n_new > 1 && tiles > kPromptTiles &&
+             (int64_t)c.sequences * groups * c.kv_heads >= prompt_waves(dtype, h.width);
+  if (h.prompt) {
+    h.rt = alone, h.row_groups = groups, h.items = (int64_t)c.sequences * groups;
     return h;
   }
   h.row_groups = (h.rows + 16 * h.rt - 1) / (16 * h.rt);
@@ -77,8 +87,9 @@ template <int CACHE, int D, int RT, int PAGES>
 hipError_t run_new(const AttnPlan& p, hipStream_t s) {
   if constexpr (RT == 1) {
     if (p.a.n_new == 1) return run_attention<CACHE, D, RT, PAGES, NEW_ONE>(p, s);
-    if (!p.workers && p.row_groups > kPromptTiles) return run_attention<CACHE, D, RT, PAGES, NEW_PROMPT>(p, s);
   }
+  if constexpr (RT == (CACHE == CACHE_F32 || CACHE == CACHE_CODES_F32 || D == 256 ? 1 : 2))
+    if (p.prompt) return run_attention<CACHE, D, RT, PAGES, NEW_PROMPT>(p, s);
   return run_attention<CACHE, D, RT, PAGES, NEW_SOME>(p, s);
 }
 template <int CACHE, int D, int RT>
@@ -119,6 +130,7 @@ hipError_t launch_attention(int dtype, const AttnArgs& a, const PagedCache& c, v
   // (a window as long as the longest sequence hides nothing)
   if (a.window >= (int64_t)c.max_pages * c.page_size) p.a.window = 0;
   p.group = h.group, p.rows = h.rows, p.row_groups = h.row_groups, p.items = (int)h.items, p.workers = h.workers;
+  p.prompt = h.prompt;
   p.scale2 = (float)(a.scale * M_LOG2E);
   if (h.workers) {
     const int64_t rows = part_rows(h, c);

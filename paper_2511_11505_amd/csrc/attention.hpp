@@ -28,6 +28,7 @@ struct AttnPlan {
   PagedCache c;
   int group, rows;         // query heads a key head; rows = n_new * group
   int row_groups, items;   // items = sequences * row_groups
+  bool prompt;             // a wave for each item
   int workers;             // parts, each of kv_heads workgroups; 0: one for each item
   float scale2;            // scale * log2(e)
   float* part;             // [workers * kv_heads * 2][rows of an item][D]

@@ -852,23 +852,28 @@ struct Attn {
   // Of one wave that had the item to itself: through its own part of LDS, to whole
   // rows.
   __device__ __forceinline__ void finish(const Item& item, float* to) {
-    put_sums(0, to);
-    const float sum = row_sum(l[0]);
-    const float all = row_max((float)seen[0]) > 0.f ? sum : -1.f;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      put_sums(t, to + t * 16 * STRIDE);
+      const float sum = row_sum(l[t]);
+      l[t] = row_max((float)seen[t]) > 0.f ? sum : -1.f;
+    }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = i * 4 + g, col = q * NO;
-      const float mr = __shfl(m[0], row), lr = __shfl(all, row);
-      if (row < item.nrows) {
-        float v[NO];
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int c = 0; c < NO; ++c) v[c] = to[row * STRIDE + col + c];
-        finish_row<T, NO>(p, item, head, row, col, mr, lr, v);
+      for (int i = 0; i < 4; ++i) {
+        const int at = i * 4 + g, row = t * 16 + at, col = q * NO;
+        const float mr = __shfl(m[t], at), lr = __shfl(l[t], at);
+        if (row < item.nrows) {
+          float v[NO];
+#pragma unroll
+          for (int c = 0; c < NO; ++c) v[c] = to[row * STRIDE + col + c];
+          finish_row<T, NO>(p, item, head, row, col, mr, lr, v);
+        }
       }
-    }
   }
   __device__ __forceinline__ void tiles(int from, int to) {
     if (from >= to) return;

@@ -445,6 +445,15 @@ def test_attention_prompts(kind, size, window):
         check_attention(kind, 20, 5, 136, lens, size, new=70)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "bf16 codes"])
+@pytest.mark.parametrize("size,window", [(16, 0), (7, 0), (16, 30), (5, 9)])
+@pytest.mark.parametrize("new,d", [(70, 64), (68, 40), (70, 128), (68, 72)])
+def test_attention_prompts_of_two_tiles(kind, size, window, new, d):
+    """The same with 32 rows a wave, and a last one with 24 or 16."""
+    lens = [150, new, new - 1, 3, 0, new + 1, new, 100, 12, 90, 70, 33]
+    check_attention(kind, 24, 6, d, lens, size, new=new, window=window)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_attention_many_rows(kind):
     """Row groups of one key head, divided and not."""
@@ -528,9 +537,10 @@ def test_attention_values_that_are_not_finite(kind, size):
     """An infinite or NaN value reaches the queries that see it, in its column (in
     its block of a coded cache), and no other."""
     dtype, codes = kind.split()[0], "codes" in kind
-    # (the third: a wave a row tile; the last: four row tiles a wave over a long table)
+    # (the third and the last: a wave has its rows to itself; the fourth: four row
+    # tiles a wave over a long table)
     for window, lens, new, tokens in ((0, [40, 9], 5, 0), (6, [40, 9], 5, 0), (0, [240, 9] + [232] * 10, 232, 0),
-                                      (0, [40, 17], 15, 70000)):
+                                      (0, [40, 17], 15, 70000), (0, [240, 9] + [232] * 16, 232, 0)):
         g = gen(21)
         d = 64
         table, pages = pages_of(g, lens, size, width=tokens // size)
