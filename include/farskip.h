@@ -729,10 +729,8 @@ fs_status fs_layer_norm_backward(const fs_norm_desc* desc, const void* dy, int64
  *               strides are faster.
  *   Rounding    Angles are taken in 64 bits; products, sums and softmax
  *               statistics are fp32; each output is rounded once.  The
- *               attention's weights meet a bf16 cache's values as two bf16
- *               numbers (2^-16 of a weight); with dtype FS_BF16 they are rounded to
- *               bf16 once (2^-8) for an 8-bit cache, and may be where a key head
- *               has more than 32 rows (query heads times new tokens).
+ *               attention's weights meet bf16 values (a bf16 cache's, and an 8-bit
+ *               one's with dtype FS_BF16) as two bf16 numbers (2^-16 of a weight).
  *   Overlap, Devices, Order, Graphs   as for the dense sublayer. */
 
 typedef enum {

@@ -762,15 +762,15 @@ struct Attn {
     }
   }
 
-  // O += V^T P^T.  In a bf16 cache a weight meets the values as two bf16 numbers, the
-  // second being what rounding takes from it (then 2^-16 of it): reading the cache
-  // bounds the kernel, the products are free (146.8 us for 146.1, error against 64
-  // bits 1.7e-3 for 2.0e-3, the output's own rounding).  It is rounded to bf16 once
-  // (2^-8 of it) where the values have 8 bits (2% of the time) and with four row tiles,
-  // where products bound it.  The first number is cut, not rounded, and the second is
+  // O += V^T P^T.  A weight meets bf16 values as two bf16 numbers, the second being
+  // what rounding takes from it (then 2^-16 of it).  Where reading the cache bounds the
+  // kernel the products are free; where they bound it, fewer bits were faster, us with
+  // two numbers | one: prompts of 2048 tokens 181 | 172, 512 of 4096 305 | 294, of an 8-bit
+  // cache 196 | 173 and 324 | 278; 8 tokens of 8 heads a key head 251 | 231.  One number
+  // leaves 2^-8 of a weight: an error against 64 bits of 2.0e-3 for 1.65e-3, the
+  // output's own rounding.  The first number is cut, not rounded, and the second is
   // at least 2^-17 of the weight: neither is below 0, nor 0 where the weight is not, so
   // that an infinite value stays one.
-  static constexpr bool kRest = CACHE == CACHE_BF16 && RT <= 2 && NEW != NEW_PROMPT;
   __device__ __forceinline__ void values(const Tile& x, const float (&pr)[RT][VT]) {
     if constexpr (kF32) {
 #pragma unroll
@@ -786,18 +786,14 @@ struct Attn {
                                                                       o[t][c * VE + j], 0, 0, 0);
         }
     } else {
-      bf16x8 pf[RT], rest[kRest ? RT : 1];
+      bf16x8 pf[RT], rest[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if constexpr (kRest) {
-            const float cut = __uint_as_float(__float_as_uint(pr[t][i]) & 0xFFFF0000u);
-            pf[t][i] = (__bf16)cut;
-            rest[t][i] = (__bf16)fmaxf(pr[t][i] - cut, pr[t][i] * 0x1p-17f);
-          } else {
-            pf[t][i] = (__bf16)pr[t][i];
-          }
+          const float cut = __uint_as_float(__float_as_uint(pr[t][i]) & 0xFFFF0000u);
+          pf[t][i] = (__bf16)cut;
+          rest[t][i] = (__bf16)fmaxf(pr[t][i] - cut, pr[t][i] * 0x1p-17f);
         }
 #pragma unroll
       for (int c = 0; c < VC; ++c) {
@@ -814,9 +810,8 @@ struct Attn {
           for (int t = 0; t < RT; ++t) {
             o[t][c * VE + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pf[t],
                                                                        o[t][c * VE + j], 0, 0, 0);
-            if constexpr (kRest)
-              o[t][c * VE + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), rest[t],
-                                                                         o[t][c * VE + j], 0, 0, 0);
+            o[t][c * VE + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), rest[t],
+                                                                       o[t][c * VE + j], 0, 0, 0);
           }
         }
       }

@@ -1041,3 +1041,39 @@ def test_keys_and_values_of_one_tensor():
     for k, v in ((one[:, 0], one[:, 1]), (other[:, :, 0].transpose(1, 2), other[:, :, 1].transpose(1, 2))):
         got = plain_call(fs.kv_cache(k, v), q, [50, 33], table, 4)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+# ------------------------------------------------- weights of 16 bits more
+@pytest.mark.parametrize("kind", ["bf16", "bf16 codes"])
+@pytest.mark.parametrize("h,kv,d,new,lens,tokens", [
+    (4, 2, 64, 1, [2, 4, 6, 10, 30, 600], 0), (8, 2, 128, 5, [6, 7, 10, 33], 0), (4, 2, 256, 1, [2, 4, 16, 40], 0),
+    (36, 1, 64, 2, [3, 5, 9, 41], 70000), (36, 1, 128, 2, [3, 5, 9, 41], 70000), (24, 1, 256, 1, [2, 6, 20], 0),
+    (128, 8, 64, 17, [17] * 8 + [24, 30], 0), (128, 8, 128, 17, [17] * 8 + [24, 30], 0)], ids=str)
+def test_attention_weights_of_sixteen_bits(kind, h, kv, d, new, lens, tokens):
+    """Pairs of tokens with almost the same key and opposite values: what is left of
+    their sum shows the weights' roundings, 2^-16 of each (were they bf16 numbers,
+    2^-9 of it would be left over).  One and several new tokens, four row tiles over
+    a long table, prompts."""
+    codes = "codes" in kind
+    g = gen(91 + d)
+    table, pages = pages_of(g, lens, 16, width=tokens // 16)
+    cache = Cache(g, pages, kv, 16, d, "bf16", codes)
+    cache.k[:, :, 1::2] = cache.k[:, :, ::2]
+    # (the first column: 0, and 2^-5)
+    cache.k[:, :, ::2, 0], cache.k[:, :, 1::2, 0] = (0, 0x10) if codes else (0.0, 2.0 ** -5)
+    if codes:
+        cache.v[:, :, 1::2] = cache.v[:, :, ::2] ^ 0x80
+        cache.ks.fill_(127)
+        cache.vs.fill_(127)
+    else:
+        cache.v[:, :, 1::2] = -cache.v[:, :, ::2]
+    q = heads(g, len(lens) * new, h, d, "bf16")
+    desc = fs.attention_desc(h, new, d ** -0.5)
+    ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, table) + 256,), dtype=torch.uint8, device=DEV)
+    out = Out(len(lens) * new, h, d, "bf16")
+    fs.fs_paged_attention(desc, cache.struct, q, torch.tensor(lens, dtype=torch.int32, device=DEV), table, out.view, ws)
+    torch.cuda.synchronize()
+    want, _, mass, reach = O.attention(f64(q), *cache.values(), lens, table.cpu().numpy(), new, float(np.float32(d ** -0.5)))
+    err = np.expm1((d + 2) * U * reach) + 2.0 ** -21 + max(lens) * 2.0 ** -24 + 2.0 ** -20 + 2.0 ** -16
+    tol = (2 * err)[..., None] * mass
+    near(out.get(), want, tol + HALF["bf16"] * (np.abs(want) + tol))
