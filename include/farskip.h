@@ -871,6 +871,17 @@ fs_status fs_paged_attention(const fs_attention_desc* desc, const fs_kv_cache* c
                              const fs_page_table* pages, void* out, int64_t tso, int64_t hso,
                              float* lse, void* ws, size_t ws_bytes, fs_stream stream);
 
+/* The same for queries at places of their own, as fs_cache_append takes them (a
+ * padded batch, whose tokens that are none may be anywhere): row r of sequence b is
+ * the query at position p = positions[r], at most the sequence's last place; p < 0: the
+ * query sees nothing.
+ *   positions  [sequences * n] int32, any order */
+fs_status fs_paged_attention_at(const fs_attention_desc* desc, const fs_kv_cache* cache,
+                                const void* q, int64_t tsq, int64_t hsq, const int32_t* positions,
+                                const int32_t* lengths, const fs_page_table* pages, void* out,
+                                int64_t tso, int64_t hso, float* lse, void* ws, size_t ws_bytes,
+                                fs_stream stream);
+
 /* Per-kernel timing with HIP events recorded on the launch stream around
  * selected kernels.  fs_profile_read synchronises those events.
  * FS_K_GATE_UP / FS_K_DOWN time the routed experts' passes (and

@@ -38,6 +38,7 @@ from ._lib import (  # noqa: F401
     FS_ROPE_HALVES, FS_ROPE_PAIRS, FS_ROPE_PLAIN, FS_ROPE_LINEAR, FS_ROPE_BASE, FS_ROPE_PARTS, fs_rope, fs_rotary_desc,
     fs_kv_cache, fs_page_table, fs_attention_desc, rope, kv_cache, rotary_desc, attention_desc, fs_rope_frequencies,
     fs_rotary, fs_rotary_backward, fs_cache_append, fs_paged_attention_workspace, fs_paged_attention,
+    fs_paged_attention_at,
 )
 from .sublayer import DenseSublayer, checkpoint_buffers, linear_desc, norm_desc  # noqa: F401
 from .attention import AttentionSublayer, empty_cache  # noqa: F401

@@ -156,6 +156,7 @@ _SIGS = {
                                _vp, _ppt, _vp, _i64, _i64, _vp]),
     "fs_paged_attention_workspace": (_i32, [_pad, _pkv, _ppt, ctypes.POINTER(_sz)]),
     "fs_paged_attention": (_i32, [_pad, _pkv, _vp, _i64, _i64, _vp, _ppt, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
+    "fs_paged_attention_at": (_i32, [_pad, _pkv, _vp, _i64, _i64, _vp, _vp, _ppt, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
     "fs_profile_enable": (_i32, [_i32]),
     "fs_profile_select": (_i32, [ctypes.c_uint32]),
     "fs_profile_read": (_i32, [_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i64)]),
@@ -747,6 +748,19 @@ def fs_paged_attention(desc, cache, q, lengths, pages, out, ws, lse=None, stream
                                      _ints(lengths, "lengths", t.sequences, dev), t,
                                      *_heads(out, "out", elem, shape, dev), _flat(lse, "lse", FS_F32, shape[:2], dev),
                                      wp, wb, s))
+
+
+def fs_paged_attention_at(desc, cache, q, positions, lengths, pages, out, ws, lse=None, stream=None):
+    """fs_paged_attention of queries at positions [sequences * new_tokens] int32."""
+    dev, s = _here(stream)
+    t, elem = _pages(pages, dev), _ELEM.get(cache.dtype)
+    shape = (t.sequences * desc.new_tokens, desc.q_heads, cache.head_dim)
+    wp, wb = _space(ws, dev)
+    _check(load().fs_paged_attention_at(desc, _on(cache, "cache", dev), *_heads(q, "q", elem, shape, dev),
+                                        _ints(positions, "positions", shape[0], dev),
+                                        _ints(lengths, "lengths", t.sequences, dev), t,
+                                        *_heads(out, "out", elem, shape, dev),
+                                        _flat(lse, "lse", FS_F32, shape[:2], dev), wp, wb, s))
 
 
 def fs_profile_enable(on=True):

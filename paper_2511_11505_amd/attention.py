@@ -8,7 +8,7 @@ tokens of a batch of sequences, over their paged key-value cache:
     h = norm(x);  q, k, v = h w_qkv^T + b_qkv;  k and v appended, q and k turned
     out = x + attention(q, cache) w_out^T + b_out
 
-through fs_layer_norm, fs_linear, fs_cache_append and fs_paged_attention.  All
+through fs_layer_norm, fs_linear, fs_cache_append and fs_paged_attention_at.  All
 arithmetic runs in the library's kernels; torch only allocates memory.  A
 sublayer's passes share its buffers and its workspace, so they run one after
 another, on one stream or ordered by events.
@@ -75,8 +75,10 @@ class AttentionSublayer:
     def forward(self, x, out, positions, lengths, pages, stream=None):
         """out [tokens, d] = x + sublayer(x); out may be x itself.  Token i of
         sequence b is row b * new_tokens + i; positions [tokens] int32: its place
-        in the sequence (negative: none); lengths [sequences] int32: tokens that
-        the sequence has with the new ones; pages [sequences, max_pages] int32."""
+        in the sequence (negative: none, as a padded batch has them first or last);
+        lengths [sequences] int32: tokens that the sequence has with the new ones;
+        pages [sequences, max_pages] int32.  Of a token that is none the attention
+        is 0."""
         gamma, beta, w_qkv, b_qkv, w_out, b_out = self.params
         qkv, q, o = self.heads
         h, kv = self.desc.q_heads, self.cache.kv_heads
@@ -84,6 +86,6 @@ class AttentionSublayer:
         L.fs_linear(self.qkv_desc, self.h, w_qkv, b_qkv, None, self.qkv, self.ws, stream=stream)
         L.fs_cache_append(self.cache, self.rope, qkv[:, :h], qkv[:, h:h + kv], qkv[:, h + kv:], self.seqs, positions,
                           pages, q, stream=stream)
-        L.fs_paged_attention(self.desc, self.cache, q, lengths, pages, o, self.ws, stream=stream)
+        L.fs_paged_attention_at(self.desc, self.cache, q, positions, lengths, pages, o, self.ws, stream=stream)
         L.fs_linear(self.out_desc, self.o, w_out, b_out, x, out, self.ws, stream=stream)
         return out

@@ -243,6 +243,46 @@ fs_status check_attention(const fs_attention_desc* d, const fs_kv_cache* c, cons
   return FS_OK;
 }
 
+// at: queries are at `positions`, else at their sequences' ends.
+fs_status paged_attention(const fs_attention_desc* d, const fs_kv_cache* cache, const void* q, int64_t tsq,
+                          int64_t hsq, bool at, const int32_t* positions, const int32_t* lengths, const fs_page_table* pages,
+                          void* out, int64_t tso, int64_t hso, float* lse, void* ws, size_t ws_bytes,
+                          fs_stream stream) {
+  TRY(check_attention(d, cache, pages));
+  if (pages->sequences == 0) return FS_OK;
+  const size_t es = elem(cache->dtype);
+  const int64_t t = (int64_t)pages->sequences * d->new_tokens;
+  const Arr Q = heads_of("q", q, es, t, d->q_heads, cache->head_dim, tsq, hsq);
+  const Arr O = heads_of("out", out, es, t, d->q_heads, cache->head_dim, tso, hso);
+  TRY(check_arr(Q));
+  TRY(check_arr(O));
+  if (at) NEED4(positions, "positions");
+  NEED4(lengths, "lengths");
+  OPT4(lse, "lse");
+  TRY(check_table(pages));
+  const CacheArrs m = arrs_of(cache);
+  TRY(check_cache_memory(cache, m));
+  const fs::PagedCache pc = cache_of(cache, pages);
+  const size_t need = fs::attention_ws_bytes(dt(cache->dtype), d->q_heads, d->new_tokens, pc);
+  if (ws_bytes < need) return fail(FS_ERR_WORKSPACE, "workspace smaller than fs_paged_attention_workspace");
+  if (need) NEED(ws, "ws");
+  const Arr outs[] = {O, flat_of("lse", lse, 4, lse ? t * d->q_heads : 0),
+                      flat_of("ws", ws, 1, (int64_t)need)};
+  const Arr ins[] = {Q, flat_of("positions", positions, 4, at ? t : 0),
+                     flat_of("lengths", lengths, 4, pages->sequences), table_of(pages), m.a[0], m.a[1],
+                     m.a[2], m.a[3]};
+  for (int i = 0; i < 3; ++i) {
+    for (const Arr& x : ins) TRY(no_overlap(outs[i], x));
+    for (int j = i + 1; j < 3; ++j) TRY(no_overlap(outs[i], outs[j]));
+  }
+  TRY(check_stream(stream));
+  fs::AttnArgs g{};
+  g.q_heads = d->q_heads, g.n_new = d->new_tokens, g.window = d->window, g.scale = d->scale;
+  g.q = {q, tsq, hsq}, g.out = {out, tso, hso}, g.lengths = lengths, g.positions = positions, g.lse = lse;
+  FS_HIP(fs::launch_attention(dt(cache->dtype), g, pc, ws, S(stream)), "paged_attention");
+  return FS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -351,38 +391,19 @@ fs_status fs_paged_attention_workspace(const fs_attention_desc* d, const fs_kv_c
 fs_status fs_paged_attention(const fs_attention_desc* d, const fs_kv_cache* cache, const void* q, int64_t tsq,
                              int64_t hsq, const int32_t* lengths, const fs_page_table* pages, void* out,
                              int64_t tso, int64_t hso, float* lse, void* ws, size_t ws_bytes, fs_stream stream) {
-  return entry([&]() -> fs_status {
-    TRY(check_attention(d, cache, pages));
-    if (pages->sequences == 0) return FS_OK;
-    const size_t es = elem(cache->dtype);
-    const int64_t t = (int64_t)pages->sequences * d->new_tokens;
-    const Arr Q = heads_of("q", q, es, t, d->q_heads, cache->head_dim, tsq, hsq);
-    const Arr O = heads_of("out", out, es, t, d->q_heads, cache->head_dim, tso, hso);
-    TRY(check_arr(Q));
-    TRY(check_arr(O));
-    NEED4(lengths, "lengths");
-    OPT4(lse, "lse");
-    TRY(check_table(pages));
-    const CacheArrs m = arrs_of(cache);
-    TRY(check_cache_memory(cache, m));
-    const fs::PagedCache pc = cache_of(cache, pages);
-    const size_t need = fs::attention_ws_bytes(dt(cache->dtype), d->q_heads, d->new_tokens, pc);
-    if (ws_bytes < need) return fail(FS_ERR_WORKSPACE, "workspace smaller than fs_paged_attention_workspace");
-    if (need) NEED(ws, "ws");
-    const Arr outs[] = {O, flat_of("lse", lse, 4, lse ? t * d->q_heads : 0),
-                        flat_of("ws", ws, 1, (int64_t)need)};
-    const Arr ins[] = {Q, flat_of("lengths", lengths, 4, pages->sequences), table_of(pages), m.a[0], m.a[1],
-                       m.a[2], m.a[3]};
-    for (int i = 0; i < 3; ++i) {
-      for (const Arr& x : ins) TRY(no_overlap(outs[i], x));
-      for (int j = i + 1; j < 3; ++j) TRY(no_overlap(outs[i], outs[j]));
-    }
-    TRY(check_stream(stream));
-    fs::AttnArgs g{};
-    g.q_heads = d->q_heads, g.n_new = d->new_tokens, g.window = d->window, g.scale = d->scale;
-    g.q = {q, tsq, hsq}, g.out = {out, tso, hso}, g.lengths = lengths, g.lse = lse;
-    FS_HIP(fs::launch_attention(dt(cache->dtype), g, pc, ws, S(stream)), "paged_attention");
-    return FS_OK;
+  return entry([&] {
+    return paged_attention(d, cache, q, tsq, hsq, false, nullptr, lengths, pages, out, tso, hso, lse, ws, ws_bytes,
+                           stream);
+  });
+}
+
+fs_status fs_paged_attention_at(const fs_attention_desc* d, const fs_kv_cache* cache, const void* q, int64_t tsq,
+                                int64_t hsq, const int32_t* positions, const int32_t* lengths,
+                                const fs_page_table* pages, void* out, int64_t tso, int64_t hso, float* lse, void* ws,
+                                size_t ws_bytes, fs_stream stream) {
+  return entry([&] {
+    return paged_attention(d, cache, q, tsq, hsq, true, positions, lengths, pages, out, tso, hso, lse, ws, ws_bytes,
+                           stream);
   });
 }
 

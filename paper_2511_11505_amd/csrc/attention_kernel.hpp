@@ -109,10 +109,15 @@ struct BufferT {
 struct Item {
   int seq, row0, nrows, len;
   int lo, hi;              // tokens that any of its rows sees: [lo, hi)
-  int lo_all, hi_all;      // tokens that all of them see
+  int lo_all, hi_all;      // tokens that all of them see (but those that see nothing)
   int first, tiles;        // tiles of TILE tokens, at least one
   int slots;               // what it counts for when work is divided
 };
+// Place of query i of a sequence; negative: it sees nothing.
+__device__ __forceinline__ int query_place(const AttnPlan& p, int seq, int i, int len) {
+  if (__builtin_expect(!p.a.positions, 1)) return len - p.a.n_new + i;
+  return max(min(p.a.positions[(int64_t)seq * p.a.n_new + i], len - 1), -1);
+}
 template <int TILE, int R>
 __device__ __forceinline__ Item item_of(const AttnPlan& p, int item, int length) {
   Item t;
@@ -122,7 +127,18 @@ __device__ __forceinline__ Item item_of(const AttnPlan& p, int item, int length)
   t.len = min(max(length, 0), p.c.max_pages * p.c.page_size);
   int i0 = 0, i1 = p.a.n_new - 1;
   if (p.row_groups > 1) i0 = t.row0 / p.group, i1 = (t.row0 + t.nrows - 1) / p.group;
-  const int at0 = t.len - p.a.n_new + i0, at1 = t.len - p.a.n_new + i1;
+  int at0 = t.len - p.a.n_new + i0, at1 = t.len - p.a.n_new + i1;
+  if (__builtin_expect(p.a.positions != nullptr, 0)) {
+    // the first and the last place of its queries (they may be in any order, and none;
+    // one by one: unrolled, 4 new tokens of 192 or 256 columns took 656 us for 555)
+    at0 = t.len - 1, at1 = -1;
+#pragma unroll 1
+    for (int i = i0; i <= i1; ++i) {
+      const int at = query_place(p, t.seq, i, t.len);
+      at1 = max(at1, at);
+      if (at >= 0) at0 = min(at0, at);
+    }
+  }
   t.hi = at1 + 1, t.hi_all = at0 + 1;
   t.lo = p.a.window ? max(0, at0 + 1 - p.a.window) : 0;
   t.lo_all = p.a.window ? max(0, at1 + 1 - p.a.window) : 0;
@@ -263,7 +279,7 @@ struct Attn {
       const int r = t * 16 + q;
       const bool in = r < it.nrows;
       const int row = it.row0 + (in ? r : 0), i = row / p.group;
-      lim[t] = it.len - p.a.n_new + i;
+      lim[t] = query_place(p, it.seq, i, it.len);
       low[t] = p.a.window ? lim[t] - p.a.window : -1;
       const T* src = (const T*)p.a.q.p + ((int64_t)it.seq * p.a.n_new + i) * p.a.q.ts +
                      (int64_t)(head * p.group + row - i * p.group) * p.a.q.hs;
@@ -833,6 +849,9 @@ struct Attn {
     weights(pr, x.at, x.ok, x.full);
     add_values(x, pr, x.at, x.ok, x.full);
   }
+  // Whether the lane's row saw a token.  (In tiles that all rows see, those that see
+  // nothing go along; asked here: in the loop 8 new tokens of 64 rows a key head took 587 us for 251.)
+  __device__ __forceinline__ bool any_seen(int t) const { return row_max((float)seen[t]) > 0.f && lim[t] >= 0; }
   // The item's sums to LDS: 16 rows of STRIDE.
   __device__ __forceinline__ void put_sums(int t, float* to) const {
 #pragma unroll
@@ -851,7 +870,7 @@ struct Attn {
     for (int t = 0; t < RT; ++t) {
       put_sums(t, to + t * 16 * STRIDE);
       const float sum = row_sum(l[t]);
-      l[t] = row_max((float)seen[t]) > 0.f ? sum : -1.f;
+      l[t] = any_seen(t) ? sum : -1.f;
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -1015,7 +1034,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
     for (int t = 0; t < RT; ++t) {
       s.put_sums(t, &rows[wave][t * 16][0]);
       const float l = row_sum(s.l[t]);
-      const bool seen = row_max((float)s.seen[t]) > 0.f;
+      const bool seen = s.any_seen(t);
       if (s.g == 0) stats[wave][t * 16 + s.q] = make_float2(s.m[t], seen ? l : -1.f);
     }
     __syncthreads();

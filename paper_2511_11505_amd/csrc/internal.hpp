@@ -269,7 +269,8 @@ struct AttnArgs {
   float scale;
   HeadRows q, out;
   const int32_t* lengths;
-  float* lse;   // or null
+  const int32_t* positions;   // of the queries; null: each sequence's last n_new places
+  float* lse;                 // or null
 };
 size_t attention_ws_bytes(int dtype, int q_heads, int n_new, const PagedCache& c);
 hipError_t launch_attention(int dtype, const AttnArgs& a, const PagedCache& c, void* ws, hipStream_t s);

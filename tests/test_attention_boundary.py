@@ -307,3 +307,20 @@ def test_sizes_of_structs():
     """As the header lays them out."""
     assert [ctypes.sizeof(t) for t in (L.fs_rope, L.fs_rotary_desc, L.fs_kv_cache, L.fs_page_table,
                                        L.fs_attention_desc)] == [32, 20, 88, 24, 20]
+
+
+def test_attention_at_arguments():
+    """Positions are given, aligned, and apart from what is written."""
+    at, d, c, p = fs.fs_paged_attention_at, attn(), cache(), pages()
+    refuse(L.FS_ERR_INVALID, "positions must not be NULL", at, d, c, A, None, B, p, C, WS)
+    refuse(L.FS_ERR_INVALID, "positions", at, d, c, A, D + 2, B, p, C, WS)
+    refuse(L.FS_ERR_INVALID, "lengths", at, d, c, A, D, None, p, C, WS)
+    refuse(L.FS_ERR_INVALID, "positions must be", at, d, c, A, torch.zeros((3,)), B, p, C, WS)
+    refuse(L.FS_ERR_INVALID, "positions must be", at, attn(new_tokens=2), c, A, torch.zeros((3,), dtype=torch.int32), B, p, C, WS)
+    refuse(L.FS_ERR_INVALID, "overlap", at, d, c, A, C + 8, B, p, C, WS)
+    refuse(L.FS_ERR_INVALID, "overlap", at, d, c, A, D, B, p, C, WS, lse=D + 4)
+    long = pages(max_pages=1000, ldt=1000)
+    need = fs.fs_paged_attention_workspace(d, c, long)
+    refuse(L.FS_ERR_INVALID, "overlap", at, d, c, A, D, B, long, C, (D - 256, need))
+    refuse(L.FS_ERR_WORKSPACE, "workspace", at, d, c, A, D, B, long, C, (E, need - 1))
+    at(d, c, None, None, None, pages(sequences=0), None, None, stream=0)

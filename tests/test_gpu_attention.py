@@ -1077,3 +1077,84 @@ def test_attention_weights_of_sixteen_bits(kind, h, kv, d, new, lens, tokens):
     err = np.expm1((d + 2) * U * reach) + 2.0 ** -21 + max(lens) * 2.0 ** -24 + 2.0 ** -20 + 2.0 ** -16
     tol = (2 * err)[..., None] * mass
     near(out.get(), want, tol + HALF["bf16"] * (np.abs(want) + tol))
+
+
+# ----------------------------------------------- queries at places of their own
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("h,kv,d,new,window,size,lens", [
+    (4, 2, 64, 1, 0, 16, [5, 700, 33, 0]), (4, 2, 128, 3, 0, 16, [5, 700, 33, 0]), (4, 2, 128, 3, 9, 7, [5, 700, 33, 0]),
+    (12, 2, 72, 6, 40, 16, [90, 2, 300]), (20, 1, 64, 9, 0, 16, [900, 60]), (128, 8, 64, 17, 0, 16, [60, 17, 9] * 3 + [0]),
+    (128, 8, 40, 17, 20, 5, [60, 17, 9] * 3 + [40])], ids=str)
+def test_attention_at(kind, h, kv, d, new, window, size, lens):
+    """Queries at any place, in any order, some of them none (their rows NaNs), some
+    behind the last token; one token, several, row groups, a prompt's."""
+    dtype, codes = kind.split()[0], "codes" in kind
+    g = gen(95 + d + new)
+    table, pages = pages_of(g, lens, size)
+    cache = Cache(g, pages, kv, size, d, dtype, codes)
+    t = len(lens) * new
+    pos = torch.randint(-3, max(lens) + 5, (t,), generator=g, device=DEV, dtype=torch.int32).view(len(lens), new)
+    pos[0, 0], pos[1, -1], pos[-1, 0] = -2 ** 31, 2 ** 31 - 1, -1
+    if new > 1:
+        pos[0, 0:] = torch.arange(new, device=DEV, dtype=torch.int32)      # from the start, the last none
+        pos[0, -1:] = -1
+    q = heads(g, t, h, d, dtype)
+    last = np.repeat(lens, new) - 1
+    at = np.minimum(pos.reshape(-1).cpu().numpy(), last)
+    q[torch.tensor(at < 0, device=DEV)] = float("nan")
+    desc = fs.attention_desc(h, new, d ** -0.5, window)
+    ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, table) + 256,), dtype=torch.uint8, device=DEV)
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    out, lse = Out(t, h, d, dtype), torch.full((t, h), -77.0, device=DEV)
+    fs.fs_paged_attention_at(desc, cache.struct, q, pos.reshape(-1), lengths, table, out.view, ws, lse=lse)
+    torch.cuda.synchronize()
+    tb = np.repeat(table.cpu().numpy(), new, axis=0)
+    want, want_lse, mass, reach = O.attention(f64(q), *cache.values(), at + 1, tb, 1, float(np.float32(d ** -0.5)), window)
+    err = np.expm1((d + 2) * U * reach) + 2.0 ** -21 + max(lens) * 2.0 ** -24 + 2.0 ** -20
+    tol = (2 * (err + (2.0 ** -16 if dtype == "bf16" else 0)))[..., None] * mass
+    near(out.get(), want, tol + HALF[dtype] * (np.abs(want) + tol))
+    none = np.isneginf(want_lse)
+    assert np.array_equal(none, np.isneginf(f64(lse))) and (out.get()[none] == 0).all()
+    near(f64(lse)[~none], want_lse[~none], (2 * err + 2.0 ** -22 * np.abs(np.where(none, 0, want_lse)))[~none])
+    # at the places that the sequences' last tokens have: the same bits as without
+    q = torch.nan_to_num(q)
+    ends = torch.clamp_min(lengths[:, None] - new + torch.arange(new, device=DEV, dtype=torch.int32), -1)
+    a, b = Out(t, h, d, dtype), Out(t, h, d, dtype)
+    fs.fs_paged_attention_at(desc, cache.struct, q, ends.int().reshape(-1), lengths, table, a.view, ws)
+    fs.fs_paged_attention(desc, cache.struct, q, lengths, table, b.view, ws)
+    torch.cuda.synchronize()
+    assert np.array_equal(a.get(), b.get())
+
+
+@pytest.mark.parametrize("window", [0, 5])
+@pytest.mark.parametrize("side", ["last", "first", "between"])
+def test_sublayer_padded_batch(side, window):
+    """Ragged numbers of tokens, what is none of a sequence's rows last, first or in
+    between: as one after another, in fp32 to the roundings of sums in another
+    order (a row of 96 or 192 terms, four times)."""
+    g = gen(46)
+    one, _, table, _ = serving(g, 6, 40, "f32", window=window)
+    g = gen(46)
+    four, _, table4, _ = serving(g, 6, 40, "f32", new=4, window=window)
+    assert torch.equal(table, table4)
+    lens = torch.zeros((6,), dtype=torch.int32)
+    for step, counts in enumerate([[4, 3, 2, 1, 0, 4], [1, 2, 4, 0, 3, 4], [4, 0, 1, 3, 2, 2]]):
+        x = torch.randn((6, 4, 96), generator=gen(47 + step), device=DEV)
+        pos = torch.full((6, 4), -1, dtype=torch.int32)
+        for b, n in enumerate(counts):
+            rows = {"last": range(n), "first": range(4 - n, 4), "between": [0, 2, 3, 1][:n]}[side]
+            pos[b, sorted(rows)] = lens[b] + torch.arange(n, dtype=torch.int32)
+        after = lens + torch.tensor(counts, dtype=torch.int32)
+        out = torch.empty((24, 96), device=DEV)
+        four.forward(x.view(24, 96), out, pos.view(-1).to(DEV), after.to(DEV), table)
+        got = out.view(6, 4, 96)
+        for i in range(4):
+            live = (pos[:, i] >= 0).to(DEV)
+            y = torch.empty((6, 96), device=DEV)
+            now = torch.where(pos[:, i] >= 0, pos[:, i] + 1, lens).int()
+            one.forward(x[:, i].contiguous(), y, pos[:, i].contiguous().to(DEV), now.to(DEV), table)
+            torch.cuda.synchronize()
+            assert (got[live, i] - y[live]).norm() <= 4 * 192 * 2.0 ** -24 * y[live].norm()
+            assert torch.equal(got[~live, i], x[~live, i])          # (this sublayer has no b_out)
+            lens = torch.where(pos[:, i] >= 0, pos[:, i] + 1, lens)
+        assert torch.equal(lens.int(), after)
