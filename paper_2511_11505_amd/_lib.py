@@ -663,6 +663,8 @@ def kv_cache(k, v, k_scales=None, v_scales=None, dtype=None):
     dev = k.get_device()
     kind = {"f32": FS_F32, "bf16": FS_BF16, None: FS_F32 if k.dtype is _ELEM[FS_F32] else FS_BF16}.get(dtype, dtype)
     codes = k_scales is not None
+    if codes != (v_scales is not None):
+        _bad("k_scales and v_scales", "given together")
     if v.shape != k.shape or v.stride() != k.stride():
         _bad("v", "of k's shape and strides")
     for t, name in ((k, "k"), (v, "v")):

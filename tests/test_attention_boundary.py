@@ -324,3 +324,16 @@ def test_attention_at_arguments():
     refuse(L.FS_ERR_INVALID, "overlap", at, d, c, A, D, B, long, C, (D - 256, need))
     refuse(L.FS_ERR_WORKSPACE, "workspace", at, d, c, A, D, B, long, C, (E, need - 1))
     at(d, c, None, None, None, pages(sequences=0), None, None, stream=0)
+
+
+def test_kv_cache_refusals():
+    """Types, shapes and strides that do not go together, and scales of one half."""
+    k = torch.zeros((2, 3, 4, 8), dtype=torch.bfloat16)
+    s, c = torch.zeros((2, 3, 4, 1), dtype=torch.uint8), torch.zeros((2, 3, 4, 8), dtype=torch.uint8)
+    for args in ((k, k.float()), (k.float(), k), (k, k[:1]), (k, k.transpose(1, 2).contiguous().transpose(1, 2)),
+                 (k, k, s, s), (k, k, s, None), (k, k, None, s), (c, c, s, s[..., :0]), (c, c, s[:1], s), (c, c, s, None),
+                 (c, c, None, s), (c, c), (c, k, s, s), (c, c, s, s.int())):
+        with pytest.raises(L.FsError):
+            fs.kv_cache(*args)
+    with pytest.raises(L.FsError):
+        fs.kv_cache(k, k, dtype="f32")
