@@ -743,6 +743,8 @@ def fs_paged_attention(desc, cache, q, lengths, pages, out, ws, lse=None, stream
     """q, out [sequences * new_tokens, q_heads, head_dim]; lengths [sequences]
     int32; lse [sequences * new_tokens, q_heads] fp32 or None."""
     dev, s = _here(stream)
+    if pages is None:
+        _bad("pages", "a tensor or an fs_page_table")
     t, elem = _pages(pages, dev), _ELEM.get(cache.dtype)
     shape = (t.sequences * desc.new_tokens, desc.q_heads, cache.head_dim)
     wp, wb = _space(ws, dev)
@@ -755,6 +757,8 @@ def fs_paged_attention(desc, cache, q, lengths, pages, out, ws, lse=None, stream
 def fs_paged_attention_at(desc, cache, q, positions, lengths, pages, out, ws, lse=None, stream=None):
     """fs_paged_attention of queries at positions [sequences * new_tokens] int32."""
     dev, s = _here(stream)
+    if pages is None:
+        _bad("pages", "a tensor or an fs_page_table")
     t, elem = _pages(pages, dev), _ELEM.get(cache.dtype)
     shape = (t.sequences * desc.new_tokens, desc.q_heads, cache.head_dim)
     wp, wb = _space(ws, dev)

@@ -337,3 +337,13 @@ def test_kv_cache_refusals():
             fs.kv_cache(*args)
     with pytest.raises(L.FsError):
         fs.kv_cache(k, k, dtype="f32")
+
+
+def test_attention_needs_pages():
+    """Without a page table: a refusal that says so, from each entry."""
+    d, c = attn(), cache()
+    refuse(L.FS_ERR_INVALID, "pages must", fs.fs_paged_attention, d, c, A, B, None, C, WS)
+    refuse(L.FS_ERR_INVALID, "pages must", fs.fs_paged_attention_at, d, c, A, D, B, None, C, WS)
+    refuse(L.FS_ERR_INVALID, "pages must", fs.fs_paged_attention_workspace, d, c, None)
+    x = torch.zeros((3, 4, 32), dtype=torch.bfloat16)
+    refuse(L.FS_ERR_INVALID, "pages must", fs.fs_paged_attention, d, c, x, B, None, x, None)
