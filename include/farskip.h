@@ -848,8 +848,10 @@ typedef struct {
   float scale;         /* factor of q . k; |scale| <= 1e38 */
 } fs_attention_desc;
 
-/* Bytes of workspace of fs_paged_attention; of the page table only the sizes are
- * read.  The workspace is 16-byte aligned. */
+/* Bytes of workspace of fs_paged_attention and fs_paged_attention_at; of the page table
+ * only the sizes are read.  It is enough for narrower page tables (fewer max_pages) of as many
+ * sequences too; fewer sequences or other new_tokens may need more.  The workspace is 16-byte
+ * aligned. */
 fs_status fs_paged_attention_workspace(const fs_attention_desc* desc, const fs_kv_cache* cache,
                                        const fs_page_table* pages, size_t* bytes);
 

@@ -49,13 +49,14 @@ struct Shape {
   int64_t items;
   int workers;
 };
-Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c) {
+Shape shape_of(int dtype, int q_heads, int n_new, const PagedCache& c, int most_row_tiles = 4) {
   Shape h;
   h.width = width_of(c.d);
   h.group = q_heads / c.kv_heads;
   h.rows = n_new * h.group;
   const int64_t tokens = (int64_t)c.max_pages * c.page_size;
   h.rt = row_tiles(dtype, h.width, h.rows, c, tokens);
+  if (h.rt > most_row_tiles) h.rt = most_row_tiles;
   const int tiles = (h.rows + 15) / 16;
   h.workers = 0;
   const int alone = prompt_tiles(dtype, h.width), groups = (tiles + alone - 1) / alone;
@@ -116,11 +117,19 @@ hipError_t run_cache(int width, int rt, const AttnPlan& p, hipStream_t s) {
 
 }  // namespace
 
+// Enough for narrower page tables too (a program may cut its table to the longest
+// sequence that it has now): with the same row tiles these need no more, but they may have
+// two where this one has four.
 size_t attention_ws_bytes(int dtype, int q_heads, int n_new, const PagedCache& c) {
-  const Shape h = shape_of(dtype, q_heads, n_new, c);
-  if (!h.workers) return 0;
-  const int64_t rows = part_rows(h, c);
-  return up(rows * h.width * 4) + up(rows * 8) + up(h.items * 8);
+  size_t most = 0;
+  for (int rt : {2, 4}) {
+    const Shape h = shape_of(dtype, q_heads, n_new, c, rt);
+    if (!h.workers) continue;
+    const int64_t rows = part_rows(h, c);
+    const size_t bytes = up(rows * h.width * 4) + up(rows * 8) + up(h.items * 8);
+    if (bytes > most) most = bytes;
+  }
+  return most;
 }
 
 hipError_t launch_attention(int dtype, const AttnArgs& a, const PagedCache& c, void* ws, hipStream_t s) {

@@ -347,3 +347,18 @@ def test_attention_needs_pages():
     refuse(L.FS_ERR_INVALID, "pages must", fs.fs_paged_attention_workspace, d, c, None)
     x = torch.zeros((3, 4, 32), dtype=torch.bfloat16)
     refuse(L.FS_ERR_INVALID, "pages must", fs.fs_paged_attention, d, c, x, B, None, x, None)
+
+
+@pytest.mark.parametrize("codes,dtype", [(0, L.FS_BF16), (1, L.FS_BF16), (0, L.FS_F32), (1, L.FS_F32)])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_workspace_of_narrower_tables(d, codes, dtype):
+    """A workspace for a page table is enough for each narrower one."""
+    c = cache(codes, head_dim=d, dtype=dtype, place_stride=d, head_stride=16 * d, page_stride=32 * d, page_size=16)
+    for rows in (1, 8, 17, 32, 33, 64, 65, 200):
+        for sequences in (1, 3, 40, 700, 3000):
+            most = 0
+            for n in sorted({2 ** i + j for i in range(14) for j in (-1, 0, 1)} | {11000}):
+                p = pages(max_pages=n, ldt=n, sequences=sequences)
+                need = fs.fs_paged_attention_workspace(attn(2 * rows), c, p)
+                assert need >= most, (rows, sequences, n, need, most)
+                most = need

@@ -1158,3 +1158,24 @@ def test_sublayer_padded_batch(side, window):
             assert torch.equal(got[~live, i], x[~live, i])          # (this sublayer has no b_out)
             lens = torch.where(pos[:, i] >= 0, pos[:, i] + 1, lens)
         assert torch.equal(lens.int(), after)
+
+
+def test_attention_of_a_narrower_table():
+    """The same call with a page table that is cut to the longest sequence, on the
+    workspace of the whole one (of 33 rows a key head: with other row tiles): to the
+    roundings of sums in another order."""
+    g = gen(97)
+    lens = [300, 7, 33, 0] * 10
+    table, pages = pages_of(g, lens, 16, width=4375)
+    cache = Cache(g, pages, 2, 16, 64, "bf16")
+    q = heads(g, 40, 66, 64, "bf16")
+    desc, lengths = fs.attention_desc(66, 1, 0.125), torch.tensor(lens, dtype=torch.int32, device=DEV)
+    ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, table),), dtype=torch.uint8, device=DEV)
+    want, _, mass, reach = O.attention(f64(q), *cache.values(), lens, table.cpu().numpy()[:, :19], 1, 0.125)
+    err = np.expm1(66 * U * reach) + 2.0 ** -21 + 300 * 2.0 ** -24 + 2.0 ** -20 + 2.0 ** -16
+    tol = (2 * err)[..., None] * mass
+    for width in (4375, 2047, 512, 33, 19):
+        out = Out(40, 66, 64, "bf16")
+        fs.fs_paged_attention(desc, cache.struct, q, lengths, table[:, :width], out.view, ws)
+        torch.cuda.synchronize()
+        near(out.get(), want, tol + HALF["bf16"] * (np.abs(want) + tol))
