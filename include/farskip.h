@@ -731,6 +731,8 @@ fs_status fs_layer_norm_backward(const fs_norm_desc* desc, const void* dy, int64
  *               statistics are fp32; each output is rounded once.  The
  *               attention's weights meet bf16 values (a bf16 cache's, and an 8-bit
  *               one's with dtype FS_BF16) as two bf16 numbers (2^-16 of a weight).
+ *               What fp32 does not hold is an infinity: q . k, scale q . k, and a
+ *               row's sum of exp(s_j - max s) v_j.
  *   Overlap, Devices, Order, Graphs   as for the dense sublayer. */
 
 typedef enum {

@@ -1,8 +1,6 @@
 // Attention over a paged cache: which kernel runs, on how many workgroups.
 // (The kernels are in attention_kernel.hpp, instantiated in attention_*.hip.)
 
-#include <math.h>
-
 #include "attention.hpp"
 
 namespace fs {
@@ -140,7 +138,6 @@ hipError_t launch_attention(int dtype, const AttnArgs& a, const PagedCache& c, v
   if (a.window >= (int64_t)c.max_pages * c.page_size) p.a.window = 0;
   p.group = h.group, p.rows = h.rows, p.row_groups = h.row_groups, p.items = (int)h.items, p.workers = h.workers;
   p.prompt = h.prompt;
-  p.scale2 = (float)(a.scale * M_LOG2E);
   if (h.workers) {
     const int64_t rows = part_rows(h, c);
     char* w = (char*)ws;

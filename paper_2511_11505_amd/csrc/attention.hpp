@@ -30,9 +30,8 @@ struct AttnPlan {
   int row_groups, items;   // items = sequences * row_groups
   bool prompt;             // a wave for each item
   int workers;             // parts, each of kv_heads workgroups; 0: one for each item
-  float scale2;            // scale * log2(e)
   float* part;             // [workers * kv_heads * 2][rows of an item][D]
-  float2* stat;            // [workers * kv_heads * 2][rows of an item]: m, l
+  float2* stat;            // [workers * kv_heads * 2][rows of an item]: largest score, sum of weights
   int2* span;              // [items]: first and last part
 };
 

@@ -2,8 +2,7 @@
 //
 // For a query row q and the tokens j that it sees, out = sum_j e^(s_j) v_j /
 // sum_j e^(s_j), s_j = scale q . k_j, in one pass over the cache: the running
-// maximum m, the sum l and the sum of values are rescaled when m grows (in powers
-// of two, s times log2 e).
+// maximum m, the sum l and the sum of values are rescaled when m grows.
 //
 // Reading the cache once bounds it (a step of one token does 2 G operations a
 // byte in bf16, G query heads a key head), so all rows that read the same keys,
@@ -79,7 +78,12 @@ __device__ __forceinline__ float row_sum(float v) {
   const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-__device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
+// e^(a - b).  The difference is taken first: a score that fp32 holds may be one that it
+// does not hold times log2 e.
+__device__ __forceinline__ float exp_diff(float a, float b) {
+  return __builtin_amdgcn_exp2f((a - b) * 1.4426950408889634f);
+}
+__device__ __forceinline__ float lse_of(float m, float l) { return m + __log2f(l) * 0.69314718055994531f; }
 
 // Memory from a uniform address on; offsets at or above kNone read 0.  Rows are
 // loaded as what is read once: in bf16 148.7 us against 166.4 (64 sequences of up
@@ -164,7 +168,7 @@ __device__ __forceinline__ void finish_row(const AttnPlan& p, const Item& it, in
   const int r = it.row0 + row, i = r / p.group, h = head * p.group + r - i * p.group;
   const int64_t tok = (int64_t)it.seq * p.a.n_new + i;
   const bool none = l < 0.f;
-  if (col == 0 && p.a.lse) p.a.lse[tok * p.a.q_heads + h] = none ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+  if (col == 0 && p.a.lse) p.a.lse[tok * p.a.q_heads + h] = none ? -INFINITY : lse_of(m, l);
   T* dst = (T*)p.a.out.p + tok * p.a.out.ts + h * p.a.out.hs + col;
 #pragma unroll
   for (int c = 0; c < N; c += 4) {
@@ -589,6 +593,7 @@ struct Attn {
 
   // ---- one tile: scores, then weights, then the sums of values
   __device__ __forceinline__ void scores(const Tile& x, float (&pr)[RT][VT]) const {
+#pragma clang fp contract(off)   // a score is rounded before the maximum is taken from it
 #pragma unroll
     for (int u = 0; u < NG; ++u) {
       floatx4 s[RT];
@@ -614,7 +619,7 @@ struct Attn {
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) pr[t][u * 4 + r] = s[t][r] * p.scale2;
+        for (int r = 0; r < 4; ++r) pr[t][u * 4 + r] = s[t][r] * p.a.scale;
     }
   }
 
@@ -638,7 +643,7 @@ struct Attn {
       mx = fmaxf(m[t], row_max(mx));
       const float mu = mx == -INFINITY ? 0.f : mx;
       if (__any(mx > m[t])) {
-        const float scale = exp2_hw(m[t] - mu);
+        const float scale = exp_diff(m[t], mu);
         l[t] *= scale;
 #pragma unroll
         for (int n = 0; n < NO; ++n) o[t][n] *= scale;
@@ -647,7 +652,7 @@ struct Attn {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < VT; ++i) {
-        pr[t][i] = exp2_hw(pr[t][i] - mu);
+        pr[t][i] = exp_diff(pr[t][i], mu);
         sum += pr[t][i];
       }
       l[t] += sum;
@@ -1051,7 +1056,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
 #pragma unroll
       for (int w = 0; w < kAttnWaves; ++w) {
         const float2 st = stats[w][row];
-        const float e = st.x == -INFINITY ? 0.f : exp2_hw(st.x - m);
+        const float e = st.x == -INFINITY ? 0.f : exp_diff(st.x, m);
         any |= !(st.y < 0.f);
         sum += st.y < 0.f ? 0.f : e * st.y;
 #pragma unroll
@@ -1083,7 +1088,7 @@ struct Sum {
   bool any;
   __device__ __forceinline__ void add(float m2, float l2, floatx4 o2, bool any2) {
     const float top = fmaxf(m, m2);
-    const float a = m == -INFINITY ? 0.f : exp2_hw(m - top), b = m2 == -INFINITY ? 0.f : exp2_hw(m2 - top);
+    const float a = m == -INFINITY ? 0.f : exp_diff(m, top), b = m2 == -INFINITY ? 0.f : exp_diff(m2, top);
     l = a * l + b * l2, o = a * o + b * o2, m = top, any |= any2;
   }
 };
@@ -1139,7 +1144,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnPlan p, int blo
   const int q = row0 + row, i = q / p.group, h = head * p.group + q - i * p.group;
   const int64_t tok = (int64_t)seq * p.a.n_new + i;
   if (lane == 0 && p.a.lse)
-    p.a.lse[tok * p.a.q_heads + h] = s.any ? (s.m + __log2f(s.l)) * 0.69314718055994531f : -INFINITY;
+    p.a.lse[tok * p.a.q_heads + h] = s.any ? lse_of(s.m, s.l) : -INFINITY;
   T out[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) out[j] = from_f32<T>(s.any ? s.o[j] / s.l : 0.f);

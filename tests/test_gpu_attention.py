@@ -1179,3 +1179,51 @@ def test_attention_of_a_narrower_table():
         fs.fs_paged_attention(desc, cache.struct, q, lengths, table[:, :width], out.view, ws)
         torch.cuda.synchronize()
         near(out.get(), want, tol + HALF["bf16"] * (np.abs(want) + tol))
+
+
+# ------------------------------------------------------- the ends of fp32's range
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 3])
+def test_attention_scores_at_the_ends_of_the_range(dtype, new):
+    """Scores of up to fp32's largest value: even ones share their weight, and of others
+    the largest has it all; in a call of one part and in a divided one."""
+    g = gen(98)
+    big = float(torch.finfo(TORCH[dtype]).max)
+    lens = [40, 33, 2000]
+    table, pages = pages_of(g, lens, 16)
+    for tokens in (40, 2000):
+        cut = [min(n, tokens) for n in lens]
+        for value, other in ((-big, None), (big, None), (big, -big), (0.9 * big, big), (-big, -0.9 * big)):
+            cache = Cache(g, pages, 1, 16, 64, dtype)
+            cache.k.fill_(0.0)
+            cache.k[..., 0] = value
+            top = [7, 30, 5]
+            if other is not None:
+                for b, j in enumerate(top):
+                    pg, pl = place_of(table, 16, b, j)
+                    cache.k[pg, 0, pl, 0] = other
+            q = torch.zeros((3 * new, 2, 64), dtype=TORCH[dtype], device=DEV)
+            q[..., 0] = 1.0
+            desc = fs.attention_desc(2, new, 1.0)
+            out = torch.empty((3 * new, 2, 64), dtype=TORCH[dtype], device=DEV)
+            lse = torch.empty((3 * new, 2), device=DEV)
+            pg = table[:, :(tokens + 15) // 16].contiguous()
+            ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, pg) + 256,), dtype=torch.uint8, device=DEV)
+            fs.fs_paged_attention(desc, cache.struct, q, torch.tensor(cut, dtype=torch.int32, device=DEV), pg, out, ws, lse=lse)
+            torch.cuda.synchronize()
+            v = f64(cache.v)[:, 0]
+            for b, n in enumerate(cut):
+                for i in range(new):
+                    at = n - new + i
+                    rows = np.stack([v[place_of(table, 16, b, j)] for j in range(at + 1)])
+                    if other is None:
+                        seen, score = rows, value
+                    elif other > value:
+                        seen, score = rows[top[b]:top[b] + 1], other
+                    else:
+                        seen, score = np.delete(rows, top[b], 0), value
+                    want = seen.mean(0)
+                    tol = (2 * (len(seen) * 2.0 ** -24 + 2.0 ** -20 + 2.0 ** -16)) * np.abs(seen).mean(0)
+                    near(f64(out)[b * new + i], np.broadcast_to(want, (2, 64)), tol + HALF[dtype] * (np.abs(want) + tol))
+                    score = float(torch.tensor(score, dtype=TORCH[dtype]))
+                    near(f64(lse)[b * new + i], np.full((2,), score), 2.0 ** -23 * abs(score))
