@@ -865,7 +865,8 @@ fs_status fs_paged_attention_workspace(const fs_attention_desc* desc, const fs_k
  *   lse = ln sum_j exp(s_j)
  * A query that sees nothing (p < 0: a sequence shorter than n, or an empty one)
  * gets out = 0 and lse = -infinity.  What is held at places that a query does not
- * see does not reach it, NaNs included.
+ * see does not reach it, NaNs included; an infinite value that it sees stays one, however
+ * small its weight.
  *   q, out   [sequences * n, q_heads, head_dim] dtype, at most 2^24 tokens
  *   lengths  [sequences] int32: tokens in the cache; negative: 0, above max_pages *
  *            page_size: that

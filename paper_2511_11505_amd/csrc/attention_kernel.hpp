@@ -83,6 +83,15 @@ __device__ __forceinline__ float row_sum(float v) {
 __device__ __forceinline__ float exp_diff(float a, float b) {
   return __builtin_amdgcn_exp2f((a - b) * 1.4426950408889634f);
 }
+// The least factor of a rescaling, and the least weight among values that may be infinite
+// (the sum of weights takes it as it is): with 0, where e^x has no normal fp32 number, an
+// infinite value would become a NaN.  It adds at most 2^-126 of a value.
+constexpr float kLeast = 0x1p-126f;
+__device__ __forceinline__ float rescale(float m, float top) {
+  return m == -INFINITY ? 0.f : fmaxf(exp_diff(m, top), kLeast);
+}
+// A row's output of its sums; without a weight (every score minus infinity) it is 0 / 0.
+__device__ __forceinline__ float quotient(float o, float l) { return l == 0.f ? NAN : o / l; }
 __device__ __forceinline__ float lse_of(float m, float l) { return m + __log2f(l) * 0.69314718055994531f; }
 
 // Memory from a uniform address on; offsets at or above kNone read 0.  Rows are
@@ -175,7 +184,7 @@ __device__ __forceinline__ void finish_row(const AttnPlan& p, const Item& it, in
     if (col + c >= p.c.d) break;
     T v[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = from_f32<T>(none ? 0.f : o[c + j] / l);
+    for (int j = 0; j < 4; ++j) v[j] = from_f32<T>(none ? 0.f : quotient(o[c + j], l));
     memcpy(dst + c, v, sizeof(v));
   }
 }
@@ -623,6 +632,10 @@ struct Attn {
     }
   }
 
+  // The least weight: 0 where rows may see different tokens (what is not finite there
+  // does not come to the products); where one new token's rows do not see a token, its
+  // values are 0.  (Codes have no infinity.)
+  static __device__ __forceinline__ float least(bool all) { return all || !MANY ? kLeast : 0.f; }
   __device__ __forceinline__ void weights(float (&pr)[RT][VT], int tile, uint32_t okay, bool all) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -643,7 +656,7 @@ struct Attn {
       mx = fmaxf(m[t], row_max(mx));
       const float mu = mx == -INFINITY ? 0.f : mx;
       if (__any(mx > m[t])) {
-        const float scale = exp_diff(m[t], mu);
+        const float scale = rescale(m[t], mu);
         l[t] *= scale;
 #pragma unroll
         for (int n = 0; n < NO; ++n) o[t][n] *= scale;
@@ -652,8 +665,9 @@ struct Attn {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < VT; ++i) {
-        pr[t][i] = exp_diff(pr[t][i], mu);
-        sum += pr[t][i];
+        const float w = exp_diff(pr[t][i], mu);
+        sum += w;
+        pr[t][i] = kCodes ? w : fmaxf(w, least(all));
       }
       l[t] += sum;
     }
@@ -675,7 +689,7 @@ struct Attn {
         }
       }
     }
-    if (MANY && !all && p.a.n_new > 1) {
+    if (MANY && !all) {
       // Rows that see different tokens: a value that is not finite must not
       // reach, as 0 times itself, a row that does not see it.
       uint32_t bad = 0;
@@ -692,7 +706,7 @@ struct Attn {
         clear_infinities(x);
       }
     }
-    values(x, pr);
+    values(x, pr, all);
   }
 
   // What values that are not finite add to the rows that see them: a weight is
@@ -789,10 +803,9 @@ struct Attn {
   // two numbers | one: prompts of 2048 tokens 181 | 172, 512 of 4096 305 | 294, of an 8-bit
   // cache 196 | 173 and 324 | 278; 8 tokens of 8 heads a key head 251 | 231.  One number
   // leaves 2^-8 of a weight: an error against 64 bits of 2.0e-3 for 1.65e-3, the
-  // output's own rounding.  The first number is cut, not rounded, and the second is
-  // at least 2^-17 of the weight: neither is below 0, nor 0 where the weight is not, so
-  // that an infinite value stays one.
-  __device__ __forceinline__ void values(const Tile& x, const float (&pr)[RT][VT]) {
+  // output's own rounding.  The first number is cut, not rounded, and the second at
+  // least the least weight: neither is below 0, nor 0 where a value may be infinite.
+  __device__ __forceinline__ void values(const Tile& x, const float (&pr)[RT][VT], bool all) {
     if constexpr (kF32) {
 #pragma unroll
       for (int i = 0; i < VT; ++i)
@@ -814,7 +827,7 @@ struct Attn {
         for (int i = 0; i < 8; ++i) {
           const float cut = __uint_as_float(__float_as_uint(pr[t][i]) & 0xFFFF0000u);
           pf[t][i] = (__bf16)cut;
-          rest[t][i] = (__bf16)fmaxf(pr[t][i] - cut, pr[t][i] * 0x1p-17f);
+          rest[t][i] = (__bf16)(kCodes ? pr[t][i] - cut : fmaxf(pr[t][i] - cut, least(all)));
         }
 #pragma unroll
       for (int c = 0; c < VC; ++c) {
@@ -1056,7 +1069,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, attn_groups_per_cu(D, RT)) void at
 #pragma unroll
       for (int w = 0; w < kAttnWaves; ++w) {
         const float2 st = stats[w][row];
-        const float e = st.x == -INFINITY ? 0.f : exp_diff(st.x, m);
+        const float e = rescale(st.x, m);
         any |= !(st.y < 0.f);
         sum += st.y < 0.f ? 0.f : e * st.y;
 #pragma unroll
@@ -1088,7 +1101,7 @@ struct Sum {
   bool any;
   __device__ __forceinline__ void add(float m2, float l2, floatx4 o2, bool any2) {
     const float top = fmaxf(m, m2);
-    const float a = m == -INFINITY ? 0.f : exp_diff(m, top), b = m2 == -INFINITY ? 0.f : exp_diff(m2, top);
+    const float a = rescale(m, top), b = rescale(m2, top);
     l = a * l + b * l2, o = a * o + b * o2, m = top, any |= any2;
   }
 };
@@ -1147,7 +1160,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnPlan p, int blo
     p.a.lse[tok * p.a.q_heads + h] = s.any ? lse_of(s.m, s.l) : -INFINITY;
   T out[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) out[j] = from_f32<T>(s.any ? s.o[j] / s.l : 0.f);
+  for (int j = 0; j < 4; ++j) out[j] = from_f32<T>(s.any ? quotient(s.o[j], s.l) : 0.f);
   memcpy((T*)p.a.out.p + tok * p.a.out.ts + h * p.a.out.hs + col, out, sizeof(out));
 }
 

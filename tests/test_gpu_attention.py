@@ -1227,3 +1227,52 @@ def test_attention_scores_at_the_ends_of_the_range(dtype, new):
                     near(f64(out)[b * new + i], np.broadcast_to(want, (2, 64)), tol + HALF[dtype] * (np.abs(want) + tol))
                     score = float(torch.tensor(score, dtype=TORCH[dtype]))
                     near(f64(lse)[b * new + i], np.full((2,), score), 2.0 ** -23 * abs(score))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [16, 5])
+@pytest.mark.parametrize("h,new", [(2, 1), (2, 3), (36, 1), (36, 2)])
+def test_attention_infinite_values_of_small_weight(kind, size, h, new):
+    """An infinite value stays one however far its score is below the largest (a weight
+    that fp32 does not hold), in tiles that every row sees whole and in others, before
+    and after the largest score, in the same part of a divided call and in another;
+    finite ones there add nothing."""
+    g = gen(99)
+    inf, d = float("inf"), 64
+    lens = [20, 100, 1500, 1500, 1500, 1500]
+    table, pages = pages_of(g, lens, size, width=70000 // size)
+    for below in (80.0, 95.0, 120.0, 1000.0, 2.0 ** 20):
+        cache = Cache(g, pages, 1, size, d, kind)
+        cache.k[..., 0] = 0.0
+        cache.k[..., 1:] *= 0.01
+        q = heads(g, len(lens) * new, h, d, kind)
+        q[..., 0] = 1.0
+        # (sequence, token of the infinite value, its column, token of the largest score)
+        for b, j, c, top in [(0, 0, 3, 16), (1, 97, 9, 5), (2, 3, 20, 1400), (3, 1499 - new, 33, 2), (4, 700, 63, 703), (5, 60, 0, 30)]:
+            pg, pl = place_of(table, size, b, top)
+            cache.k[pg, 0, pl, 0] = below
+            pg, pl = place_of(table, size, b, j)
+            cache.v[pg, 0, pl, c] = inf if b % 2 else -inf
+        out = Out(len(lens) * new, h, d, kind)
+        # (short tables: few row tiles; long ones: many)
+        for width in (1500 // size + 1, 70000 // size):
+            t = table[:, :width]
+            desc = fs.attention_desc(h, new, 1.0)
+            ws = torch.empty((fs.fs_paged_attention_workspace(desc, cache.struct, t) + 256,), dtype=torch.uint8, device=DEV)
+            fs.fs_paged_attention(desc, cache.struct, q, torch.tensor(lens, dtype=torch.int32, device=DEV), t, out.view, ws)
+            torch.cuda.synchronize()
+            got = out.get().reshape(len(lens), new, h, d)
+            want = np.zeros((len(lens), d))
+            for b, c in enumerate([3, 9, 20, 33, 63, 0]):
+                want[b, c] = inf if b % 2 else -inf
+            want = np.broadcast_to(want[:, None, None], got.shape)
+            assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)]), (below, width, got[np.isinf(want)][:8])
+            assert np.isfinite(got[np.isfinite(want)]).all()
+            k, v = cache.values()
+            v = np.where(np.isfinite(v), v, 0.0)
+            fine, _, mass, reach = O.attention(f64(q), k, v, lens, table.cpu().numpy()[:, :1501], new, 1.0)
+            err = np.expm1((d + 2) * U * np.minimum(reach, 1000.0)) + 2.0 ** -20 + 1500 * 2.0 ** -24 + 2.0 ** -16
+            tol = (2 * err)[..., None] * mass
+            tol = (tol + HALF[kind] * (np.abs(fine) + tol)).reshape(got.shape)
+            ok = np.isfinite(want)
+            near(got[ok], fine.reshape(got.shape)[ok], tol[ok])
