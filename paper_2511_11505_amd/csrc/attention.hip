@@ -30,14 +30,23 @@ int cache_of(int dtype, const PagedCache& c) {
 // registers hold (a row tile takes D / 4 of them for its sums and D / 8, in fp32
 // D / 4, for its queries).  Four leave one workgroup to a CU and start later, but
 // read a long bf16 cache once where two read it twice: 56 rows a key head, 8 of them,
-// four tiles | two, us: 32 sequences of 4096 tokens 153 | 167, 1 of 65536 87 | 106;
-// 8 of 4096 and 32 of 1024 (2^18 tokens and heads) 55 | 54 and 55 | 56, 8 of 512
-// 31 | 17, 256 of 512 249 | 185.  An 8-bit cache does not gain: 16 of 16384 213 | 200.
+// four tiles | two, us: 32 sequences of 8192 tokens 273 | 312, of 4096 150 | 167, 1 of 65536
+// 89 | 109; 8 of 4096 and 32 of 1024 (2^18 tokens and heads) 58 | 58 and 58 | 57, 8 of 512
+// 31 | 17, 256 of 512 249 | 185.  With pages of 20 tokens two are faster (32 of 8192 tokens
+// 440 | 257, 1 of 65536 132 | 84), and an 8-bit cache does not gain: 16 of 16384 213 | 200.
 bool four_tiles(const PagedCache& c, int64_t tokens) {
-  return !c.codes && tokens > 512 && (double)c.sequences * tokens * c.kv_heads > (1 << 18);
+  return !c.codes && c.page_size % 16 == 0 && tokens > 512 &&
+         (double)c.sequences * tokens * c.kv_heads > (1 << 18);
+}
+// Past 128 columns two row tiles spill registers.  Where all 256 columns of codes in pages of whole
+// groups are read, one is faster: 4 new tokens, 8 heads a key head, 8 of them, two | one, us, 32
+// sequences of 8192 tokens 582 | 394, of 512 52 | 41, 8 of 512 49 | 21; with pages of 20 tokens
+// 527 | 562, of 192 columns 317 | 405, in bf16 544 | 643.
+bool one_tile(int dtype, int width, const PagedCache& c) {
+  return width == 256 && (dtype == 0 || (c.codes && c.page_size % 16 == 0 && c.d > 256 - 32));
 }
 int row_tiles(int dtype, int width, int rows, const PagedCache& c, int64_t tokens) {
-  if (rows <= 16 || (dtype == 0 && width == 256)) return 1;
+  if (rows <= 16 || one_tile(dtype, width, c)) return 1;
   return rows <= 32 || dtype == 0 || width == 256 || !four_tiles(c, tokens) ? 2 : 4;
 }
 
@@ -93,10 +102,17 @@ hipError_t run_new(const AttnPlan& p, hipStream_t s) {
 }
 template <int CACHE, int D, int RT>
 hipError_t run_pages(const AttnPlan& p, hipStream_t s) {
-  if (p.c.page_size % 16) return run_new<CACHE, D, RT, PAGES_ANY>(p, s);
-  if constexpr (CACHE == CACHE_CODES_BF16 || CACHE == CACHE_CODES_F32)
-    if (p.c.d <= D - 32) return run_new<CACHE, D, RT, PAGES_GROUPS_SHORT>(p, s);
-  return run_new<CACHE, D, RT, PAGES_GROUPS>(p, s);
+  constexpr bool codes = CACHE == CACHE_CODES_BF16 || CACHE == CACHE_CODES_F32;
+  // (what row_tiles does not choose is not built)
+  if constexpr (RT != 4)
+    if (p.c.page_size % 16) return run_new<CACHE, D, RT, PAGES_ANY>(p, s);
+  if constexpr (codes && D == 256 && RT == 2) {
+    return run_new<CACHE, D, RT, PAGES_GROUPS_SHORT>(p, s);
+  } else {
+    if constexpr (codes)
+      if (p.c.d <= D - 32) return run_new<CACHE, D, RT, PAGES_GROUPS_SHORT>(p, s);
+    return run_new<CACHE, D, RT, PAGES_GROUPS>(p, s);
+  }
 }
 template <int CACHE>
 hipError_t run_cache(int width, int rt, const AttnPlan& p, hipStream_t s) {

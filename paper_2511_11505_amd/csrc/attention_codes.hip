@@ -38,7 +38,6 @@ template hipError_t run_attention<CACHE_CODES_BF16, 256, 1, PAGES_GROUPS_SHORT, 
 template hipError_t run_attention<CACHE_CODES_BF16, 256, 1, PAGES_GROUPS_SHORT, NEW_SOME>(const AttnPlan&, hipStream_t);
 template hipError_t run_attention<CACHE_CODES_BF16, 256, 1, PAGES_GROUPS_SHORT, NEW_PROMPT>(const AttnPlan&, hipStream_t);
 template hipError_t run_attention<CACHE_CODES_BF16, 256, 2, PAGES_ANY, NEW_SOME>(const AttnPlan&, hipStream_t);
-template hipError_t run_attention<CACHE_CODES_BF16, 256, 2, PAGES_GROUPS, NEW_SOME>(const AttnPlan&, hipStream_t);
 template hipError_t run_attention<CACHE_CODES_BF16, 256, 2, PAGES_GROUPS_SHORT, NEW_SOME>(const AttnPlan&, hipStream_t);
 
 }  // namespace fs
