@@ -1276,3 +1276,35 @@ def test_attention_infinite_values_of_small_weight(kind, size, h, new):
             tol = (tol + HALF[kind] * (np.abs(fine) + tol)).reshape(got.shape)
             ok = np.isfinite(want)
             near(got[ok], fine.reshape(got.shape)[ok], tol[ok])
+
+
+@pytest.mark.parametrize("new", [1, 4])
+def test_sublayer_in_the_far_skip_window(new):
+    """The sublayer as the next layer of a block: BEGIN, the sublayer on the partial
+    input, FINISH into its output; twice, over the cache that grows.  The sublayer's
+    part as by itself."""
+    from workloads import CONFIGS, make_workload
+    cfg = CONFIGS["tiny"]
+    wl = make_workload(cfg, DEV)
+    blk = fs.MoEBlock(cfg, wl.w_router, None, wl.w_gate_up, wl.w_down, device=DEV)
+    n, d = cfg.n_tokens // new, cfg.hidden
+    pair = [serving(gen(53), n, 3 * n, "f32", new=new, d=d)[:3:2] for _ in range(2)]
+    (sub, table), (alone, table2) = pair
+    assert torch.equal(table, table2)
+    comm = torch.cuda.Stream()
+    partial, out, by_itself, routed = (torch.empty_like(wl.x) for _ in range(4))
+    for step in range(2):
+        pos = (step * new + torch.arange(new, dtype=torch.int32, device=DEV)).repeat(n)
+        lengths = torch.full((n,), (step + 1) * new, dtype=torch.int32, device=DEV)
+        blk.begin(wl.x, partial, comm=comm)
+        sub.forward(partial, out, pos, lengths, table)
+        nxt = out.clone()
+        blk.finish(wl.x, out, comm=comm)
+        alone.forward(partial, by_itself, pos, lengths, table)
+        L.fs_combine_unpack(blk.desc, blk.y_ret(), blk.t["slot_to_row"], blk.t["topk_w"], None, routed, None)
+        torch.cuda.synchronize()
+        assert torch.equal(nxt, by_itself) and torch.isfinite(out).all()
+        # FINISH adds the routed output, one rounding
+        both = f64(nxt) + f64(routed)
+        near(f64(out), both, 4 * U * (np.abs(f64(nxt)) + np.abs(f64(routed))))
+    blk.close()
