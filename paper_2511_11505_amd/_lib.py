@@ -720,7 +720,8 @@ def fs_rotary_backward(desc, rope, dout, positions, dx, stream=None):
 
 def fs_cache_append(cache, rope, q, k, v, seqs, positions, pages, q_out, stream=None):
     """q, q_out [tokens, q_heads, head_dim] or None; k, v [tokens, kv_heads,
-    head_dim]; seqs [tokens] or None, positions [tokens] int32."""
+    head_dim]; seqs [tokens] or None, positions [tokens] int32.  (q and k have to tell
+    their numbers of heads and tokens: an address does not.)"""
     if k is None:
         _bad("k", "a tensor")
     dev, s = _here(stream)

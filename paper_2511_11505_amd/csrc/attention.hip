@@ -11,10 +11,10 @@ constexpr int kMaxGroups = 1 << 16;
 // A prompt of more rows than that, enough of them for the waves below, is not
 // divided: a wave has two row tiles (in fp32 and past 128 columns one) to itself and
 // nothing is joined.  64 query and 8 key heads of 128 columns, this way | divided, us:
-// a prompt of 2048 tokens 172 | 551, of 8192 with 16 query heads 604 | 1312; 512 new
-// tokens of 4096, two sequences, 295 | 562, in fp32 1208 | 1614; 64 of 4096, six, 218 |
-// 243 (768 waves), 64 of 4096, four, 188 | 138 (512).  One row tile a wave took 308, 1172,
-// 534, -, 292 and 148, four 271, 946, 427: the products wait for the cache's tiles and
+// a prompt of 2048 tokens 188 | 579, of 8192 with 16 query heads 635 | 1356; 512 new
+// tokens of 4096, two sequences, 313 | 577, in fp32 1250 | 1645; 64 of 4096, six, 239 |
+// 257 (768 waves), five, 230 | 231 (640).  One row tile a wave took 317, 1192,
+// 544, -, 305 and 304, four 349, 1282, 546: the products wait for the cache's tiles and
 // for the softmax.
 constexpr int kPromptTiles = 16;
 int prompt_tiles(int dtype, int width) { return dtype == 0 || width == 256 ? 1 : 2; }

@@ -13,7 +13,7 @@ enum { CACHE_BF16 = 0, CACHE_F32 = 1, CACHE_CODES_BF16 = 2, CACHE_CODES_F32 = 3 
 enum { PAGES_ANY = 0, PAGES_GROUPS = 1, PAGES_GROUPS_SHORT = 2 };
 
 // New tokens: one, with rows for one row tile; several; so many (a prompt's) that
-// the rows fill the chip, a wave a row tile.
+// the rows fill the chip, a wave one or two row tiles to itself.
 enum { NEW_ONE = 0, NEW_SOME = 1, NEW_PROMPT = 2 };
 
 constexpr int kAttnWaves = 4;
@@ -21,6 +21,8 @@ constexpr int kAttnMaxItems = 4096;    // of a divided call: 16 for each thread
 constexpr int kAttnMinTiles = 4;       // of a workgroup's part: one for each wave
 
 // Workgroups a CU runs at once (four waves of 256 registers on each SIMD, or of 512).
+// (In fp32 two row tiles of 128 columns take 320 registers and 85 KB of LDS: one of the
+// two that are counted here.)
 constexpr int attn_groups_per_cu(int width, int row_tiles) { return width < 256 && row_tiles <= 2 ? 2 : 1; }
 
 struct AttnPlan {

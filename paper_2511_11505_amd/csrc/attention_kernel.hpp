@@ -24,19 +24,21 @@
 // A wave holds one tile of keys and one of values: the next keys are on their way
 // while the values are multiplied, the next values while the keys are; of small
 // tiles (8 KB with their values) it holds two (an 8-bit cache of 8 sequences of up
-// to 65536 tokens: 108 us with one, 95 with two).  At two waves a SIMD and 16 KB a
+// to 65536 tokens: 108 us with one, 95 with two, then).  At two waves a SIMD and 16 KB a
 // tile some 100 KB a CU are on their way.
 //
 // The tokens of all sequences are divided evenly over a fixed number of
-// workgroups, as many as the chip runs at once, whatever the lengths are (the host
+// workgroups, about as many as the chip runs at once, whatever the lengths are (the host
 // does not know them); a workgroup's part may hold the end of one sequence, whole
 // ones and the start of another.  Parts of a sequence are joined by a second
-// kernel in the order of the workgroups.
+// kernel in the order of the workgroups.  (Each part has a workgroup for every key head,
+// and their number is rounded up: where the key heads do not divide 512, or 256 with one
+// workgroup a CU, a few workgroups start only when others end.)
 //
 // Measured (MI355X, head_dim 128, 40 query and 8 key heads): 64 sequences of 20 to
-// 8192 tokens in bf16 147 us, 6.1 TB/s; 8 of 650 to 65536 in 8 bits 91.5 us, 5.3
-// TB/s; one of 1500 tokens 12.4 us, of which the kernel 6.8 and the join 4.4, both
-// a chain of dependent loads.
+// 8192 tokens in bf16 147 us, 6.1 TB/s; 8 of 650 to 65536 in 8 bits 92 us, 5.3
+// TB/s (reading alone goes at 6.5); one of 1500 tokens 11 to 13 us, of which the kernel 7
+// and the join 4.5, both a chain of dependent loads.
 #pragma once
 
 #include <type_traits>
