@@ -845,7 +845,8 @@ typedef struct {
   int32_t abi_version; /* FS_ABI_VERSION */
   int32_t q_heads;     /* a multiple of kv_heads, <= 2^16: head i reads key head
                           i / (q_heads / kv_heads) */
-  int32_t new_tokens;  /* n >= 1: queries of each sequence, its last n tokens */
+  int32_t new_tokens;  /* n >= 1: queries of each sequence, its last n tokens (or, with
+                          fs_paged_attention_at, any) */
   int32_t window;      /* 0, or how many tokens a query sees, itself included */
   float scale;         /* factor of q . k; |scale| <= 1e38 */
 } fs_attention_desc;

@@ -24,7 +24,7 @@
 // A wave holds one tile of keys and one of values: the next keys are on their way
 // while the values are multiplied, the next values while the keys are; of small
 // tiles (8 KB with their values) it holds two (an 8-bit cache of 8 sequences of up
-// to 65536 tokens: 108 us with one, 95 with two, then).  At two waves a SIMD and 16 KB a
+// to 65536 tokens took 108 us with one where it took 95 with two).  At two waves a SIMD and 16 KB a
 // tile some 100 KB a CU are on their way.
 //
 // The tokens of all sequences are divided evenly over a fixed number of
@@ -803,7 +803,8 @@ struct Attn {
   // what rounding takes from it (then 2^-16 of it).  Where reading the cache bounds the
   // kernel the products are free; where they bound it, fewer bits were faster, us with
   // two numbers | one: prompts of 2048 tokens 181 | 172, 512 of 4096 305 | 294, of an 8-bit
-  // cache 196 | 173 and 324 | 278; 8 tokens of 8 heads a key head 251 | 231.  One number
+  // cache 196 | 173 and 324 | 278; 8 tokens of 8 heads a key head 251 | 231 (274 with the
+  // least weight).  One number
   // leaves 2^-8 of a weight: an error against 64 bits of 2.0e-3 for 1.65e-3, the
   // output's own rounding.  The first number is cut, not rounded, and the second at
   // least the least weight: neither is below 0, nor 0 where a value may be infinite.
@@ -870,7 +871,8 @@ struct Attn {
     add_values(x, pr, x.at, x.ok, x.full);
   }
   // Whether the lane's row saw a token.  (In tiles that all rows see, those that see
-  // nothing go along; asked here: in the loop 8 new tokens of 64 rows a key head took 587 us for 251.)
+  // nothing go along.  Asked here: in the loop 8 new tokens of 64 rows a key head took
+  // 587 us for 251.)
   __device__ __forceinline__ bool any_seen(int t) const { return row_max((float)seen[t]) > 0.f && lim[t] >= 0; }
   // The item's sums to LDS: 16 rows of STRIDE.
   __device__ __forceinline__ void put_sums(int t, float* to) const {
